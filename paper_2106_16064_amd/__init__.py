@@ -3,4 +3,4 @@ behind the ``libdgsp`` C-ABI.  Importing the package loads nothing; the shared
 library is opened on the first call into :mod:`paper_2106_16064_amd.binding`,
 which raises if it has not been built (there is no CPU fallback)."""
 
-__all__ = ["binding", "workloads"]
+__all__ = ["binding", "layers", "workloads"]
