@@ -1,0 +1,313 @@
+// Host side of the gated feed-forward block: argument checks, how operands are laid out, tile shapes and launches.  The C-ABI is
+// documented in include/dgsp_layers.h.
+#include "layers_host.hpp"
+
+#include "gated_ff_kernels.hpp"
+
+namespace {
+
+using namespace dgsp;
+
+constexpr int64_t kMostWidth = (1LL << 22) - 8;         // 256 rows of it span less than 2^31 bytes (matrix_tiles.hpp)
+constexpr int64_t kAlign = 256;
+
+int64_t padded(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
+
+bool gated_extents(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type) {
+    return rows >= 0 && rows <= kMostRows && width >= 1 && width <= kMostWidth && hidden >= 1 && hidden <= kMostWidth &&
+           out_width >= 1 && out_width <= kMostWidth && known_type(type);
+}
+
+int planes_of(int type) { return type == DGSP_F32 ? 3 : 1; }
+
+// Hands out pieces of a buffer, or adds up what they need where there is none.
+class Pieces {
+public:
+    explicit Pieces(void* base) : base_(static_cast<char*>(base)) {}
+    void* take(int64_t bytes) {
+        void* p = base_ ? base_ + used_ : nullptr;
+        used_ += padded(bytes, kAlign);
+        return p;
+    }
+    int64_t used() const { return used_; }
+
+private:
+    char* base_;
+    int64_t used_ = 0;
+};
+
+// ---------------------------------------------------------------- how a product is cut
+
+enum TileSize { kSmall = 64, kMiddle = 128, kLarge = 256 };
+
+struct Cut {
+    int size;
+    int64_t tiles_m, tiles_n;
+    int splits;
+    int64_t split_depth;
+    int64_t groups(int batch) const { return tiles_m * tiles_n * batch * splits; }
+};
+
+constexpr int64_t kCus = 256;
+
+// The largest tiles of which there is one for every CU: a tile of 256 x 256 reads half as much per product as one of 128 x 128.  Where
+// even the small ones are fewer and the depth allows it, the depth is split, to two workgroups a CU of at least 512 each.
+Cut cut(int64_t m, int64_t n, int64_t depth, int batch, bool dual, bool may_split) {
+    Cut c{kSmall, 0, 0, 1, padded(std::max<int64_t>(depth, 1), kDepth)};
+    for (int size : {kLarge, kMiddle, kSmall}) {
+        c.size = size;
+        c.tiles_m = ceil_div(m, size);
+        c.tiles_n = ceil_div(n, dual ? size / 2 : size);
+        if (c.tiles_m * c.tiles_n * batch >= kCus) break;
+    }
+    const int64_t tiles = c.tiles_m * c.tiles_n * batch;
+    if (may_split && tiles < kCus && depth >= 1024) {
+        const int64_t splits = std::min<int64_t>(ceil_div(2 * kCus, tiles), depth / 512);
+        c.split_depth = padded(ceil_div(depth, splits), kDepth);
+        c.splits = (int)ceil_div(depth, c.split_depth);
+    }
+    return c;
+}
+
+bool launchable(const Cut& c, int batch) { return c.groups(batch) < (1LL << 32) / 512; }
+
+template <bool kDual>
+using Large = TileShape<256, 256, 2, 4, kDual>;
+template <bool kDual>
+using Middle = TileShape<128, 128, 2, 2, kDual>;
+template <bool kDual>
+using Small = TileShape<64, 64, 2, 2, kDual>;
+
+ProductArgs product_args(const Cut& c, int64_t m, int64_t n, int64_t depth, int planes, int batch) {
+    ProductArgs args{};
+    args.pairs = 1;
+    args.planes = planes;
+    args.m = m;
+    args.n = n;
+    args.depth = depth;
+    args.tiles_m = c.tiles_m;
+    args.tiles_n = c.tiles_n;
+    args.batch = batch;
+    args.splits = c.splits;
+    args.split_depth = c.split_depth;
+    return args;
+}
+
+int64_t partial_bytes(const Cut& c, int64_t m, int64_t n, int batch) {
+    return c.splits > 1 ? (int64_t)c.splits * batch * m * padded(n, 4) * 4 : 0;
+}
+
+template <typename E, bool kDual, bool kARows, bool kBRows, typename Out>
+void launch(const Cut& c, const ProductArgs& args, const Out& out, hipStream_t stream) {
+    const auto groups = (unsigned)c.groups(args.batch);
+    if (c.size == kLarge)
+        tile_kernel<E, Large<kDual>, kARows, kBRows, Out><<<groups, Large<kDual>::kThreads, 0, stream>>>(args, out);
+    else if (c.size == kMiddle)
+        tile_kernel<E, Middle<kDual>, kARows, kBRows, Out><<<groups, Middle<kDual>::kThreads, 0, stream>>>(args, out);
+    else
+        tile_kernel<E, Small<kDual>, kARows, kBRows, Out><<<groups, Small<kDual>::kThreads, 0, stream>>>(args, out);
+}
+
+// c[0 ... batch - 1] = the product
+template <typename T, typename E, bool kARows, bool kBRows>
+void product(const Cut& c, const ProductArgs& args, ProductOut<T> out, void* partial, hipStream_t stream) {
+    if (args.m == 0) return;
+    out.vectors = out.ld % 4 == 0 && aligned(out.c[0], 4 * sizeof(T)) && (args.batch < 2 || aligned(out.c[1], 4 * sizeof(T)));
+    out.partial = c.splits > 1 ? static_cast<float*>(partial) : nullptr;
+    launch<E, false, kARows, kBRows>(c, args, out, stream);
+    if (c.splits > 1) {
+        const int64_t quads = args.batch * args.m * ceil_div(args.n, 4);
+        join_kernel<T><<<(unsigned)std::min<int64_t>(ceil_div(quads, 256), 4096), 256, 0, stream>>>(args.m, args.n, args.batch, c.splits, out.partial, out);
+    }
+}
+
+// ---------------------------------------------------------------- operands
+
+int64_t laid_out_bytes(int64_t rows, int64_t cols, int type) { return rows * padded(cols, 8) * 2 * planes_of(type); }
+
+// Is the matrix of 16-bit elements, in whole 16-byte pieces?
+template <typename T>
+bool in_place(const void* p, int64_t rows, int64_t cols, int64_t ld) {
+    return sizeof(T) == 2 && cols % 8 == 0 && (rows == 1 || (ld % 8 == 0 && ld >= cols && ld <= kMostWidth)) && aligned(p, 16);
+}
+
+// The matrix as the products read it: in place where it can be (unless `copy`), else laid out in `piece`.
+template <typename T, typename E>
+Source source(const void* p, int64_t rows, int64_t cols, int64_t ld, void* piece, hipStream_t stream, bool copy = false) {
+    if (in_place<T>(p, rows, cols, ld) && !copy) return {static_cast<const uint16_t*>(p), rows, cols, rows == 1 ? cols : ld, 0};
+    const int64_t to_ld = padded(cols, 8), plane = rows * to_ld;
+    if (rows > 0)
+        lay_out_kernel<T, E><<<(unsigned)std::min<int64_t>(ceil_div(plane / 8, 256), 1 << 16), 256, 0, stream>>>(
+            rows, cols, static_cast<const T*>(p), ld, static_cast<E*>(piece), to_ld, plane);
+    return {static_cast<const uint16_t*>(piece), rows, to_ld, to_ld, sizeof(T) == 4 ? plane : 0};
+}
+
+template <typename E>
+Source source(const Planes<E>& planes, int64_t rows) {
+    return {reinterpret_cast<const uint16_t*>(planes.p), rows, planes.ld, planes.ld, planes.plane};
+}
+
+template <typename T, typename E>
+Planes<E> hidden_planes(void* p, int64_t rows, int64_t hidden) {
+    const int64_t ld = padded(hidden, 8);
+    return {static_cast<E*>(p), ld, sizeof(T) == 4 ? rows * ld : 0};
+}
+
+// what the forward pass leaves: act(g) and u act'(g) in 32 bits, and h
+struct Saved {
+    void *act, *mul, *h;
+    Saved(Pieces& pieces, int64_t rows, int64_t hidden, int type)
+        : act(pieces.take(rows * padded(hidden, 8) * 4)), mul(pieces.take(rows * padded(hidden, 8) * 4)),
+          h(pieces.take(laid_out_bytes(rows, hidden, type))) {}
+};
+
+struct ForwardPieces {
+    Cut up, down;
+    void *x, *gate, *up_weight, *down_weight, *h, *partial;
+    ForwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type, bool saved)
+        : up(cut(rows, hidden, width, 1, true, false)), down(cut(rows, out_width, hidden, 1, false, true)),
+          x(pieces.take(laid_out_bytes(rows, width, type))), gate(pieces.take(laid_out_bytes(hidden, width, type))),
+          up_weight(pieces.take(laid_out_bytes(hidden, width, type))), down_weight(pieces.take(laid_out_bytes(out_width, hidden, type))),
+          h(saved ? nullptr : pieces.take(laid_out_bytes(rows, hidden, type))), partial(pieces.take(partial_bytes(down, rows, out_width, 1))) {}
+};
+
+struct BackwardPieces {
+    Cut slope, dx, gates, down;
+    void *x, *gate, *up_weight, *down_weight, *dy, *dg, *du, *partial;
+    BackwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type, int batch)
+        : slope(cut(rows, hidden, out_width, 1, false, false)), dx(cut(rows, width, hidden, 1, false, true)),
+          gates(cut(hidden, width, rows, batch, false, true)), down(cut(out_width, hidden, rows, 1, false, true)),
+          x(pieces.take(laid_out_bytes(rows, width, type))), gate(pieces.take(laid_out_bytes(hidden, width, type))),
+          up_weight(pieces.take(laid_out_bytes(hidden, width, type))), down_weight(pieces.take(laid_out_bytes(out_width, hidden, type))),
+          dy(pieces.take(laid_out_bytes(rows, out_width, type))), dg(pieces.take(laid_out_bytes(rows, hidden, type))),
+          du(pieces.take(laid_out_bytes(rows, hidden, type))),
+          partial(pieces.take(std::max({partial_bytes(dx, rows, width, 1), partial_bytes(gates, hidden, width, batch),
+                                        partial_bytes(down, out_width, hidden, 1)}))) {}
+};
+
+template <typename F>
+int with_elements(int type, F&& f) {
+    if (type == DGSP_F32) return f(float{}, bf16_t{});
+    if (type == DGSP_BF16) return f(bf16_t{}, bf16_t{});
+    return f(f16_t{}, f16_t{});
+}
+
+}  // namespace
+
+extern "C" int64_t dgsp_gated_ff_saved_bytes(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type) {
+    if (!gated_extents(rows, width, hidden, out_width, type)) return 0;
+    Pieces pieces(nullptr);
+    Saved saved(pieces, rows, hidden, type);
+    return pieces.used();
+}
+
+extern "C" int64_t dgsp_gated_ff_workspace_bytes(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type) {
+    if (!gated_extents(rows, width, hidden, out_width, type)) return 0;
+    Pieces pieces(nullptr);
+    ForwardPieces need(pieces, rows, width, hidden, out_width, type, false);
+    return pieces.used();
+}
+
+extern "C" int64_t dgsp_gated_ff_backward_workspace_bytes(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type) {
+    if (!gated_extents(rows, width, hidden, out_width, type)) return 0;
+    Pieces one(nullptr), two(nullptr);
+    BackwardPieces need_one(one, rows, width, hidden, out_width, type, 1), need_two(two, rows, width, hidden, out_width, type, 2);
+    return std::max(one.used(), two.used());
+}
+
+extern "C" int dgsp_gated_ff(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type, int activation, const void* x,
+                             int64_t ldx, const void* w_gate, int64_t ldg, const void* w_up, int64_t ldu, const void* w_down, int64_t ldd,
+                             void* y, int64_t ldy, void* saved, void* workspace, int64_t workspace_bytes, void* stream) {
+    if (!gated_extents(rows, width, hidden, out_width, type) || activation < DGSP_ACT_SILU || activation > DGSP_ACT_RELU)
+        return DGSP_ERR_INVALID_ARG;
+    if (rows == 0) return DGSP_OK;
+    if (!readable(x, rows, width, ldx) || !readable(w_gate, hidden, width, ldg) || !readable(w_up, hidden, width, ldu) ||
+        !readable(w_down, out_width, hidden, ldd) || !writable(y, rows, out_width, ldy) || !aligned(saved, 16) || !workspace ||
+        !aligned(workspace, 16) || workspace_bytes < dgsp_gated_ff_workspace_bytes(rows, width, hidden, out_width, type))
+        return DGSP_ERR_INVALID_ARG;
+    Pieces pieces(workspace), kept(saved);
+    const ForwardPieces at(pieces, rows, width, hidden, out_width, type, saved != nullptr);
+    const Saved keep(kept, rows, hidden, type);
+    if (!launchable(at.up, 1) || !launchable(at.down, 1)) return DGSP_ERR_UNSUPPORTED;
+    return with_elements(type, [&](auto t, auto e) {
+        using T = decltype(t);
+        using E = decltype(e);
+        const auto on = static_cast<hipStream_t>(stream);
+        const int planes = planes_of(type);
+        const Planes<E> h = hidden_planes<T, E>(saved ? keep.h : at.h, rows, hidden);
+        ProductArgs args = product_args(at.up, rows, hidden, width, planes, 1);
+        args.a[0] = source<T, E>(x, rows, width, ldx, at.x, on);
+        args.b[0] = source<T, E>(w_gate, hidden, width, ldg, at.gate, on);
+        args.b[1] = source<T, E>(w_up, hidden, width, ldu, at.up_weight, on);
+        launch<E, true, true, true>(at.up, args, GatedUpOut<E>{h, saved ? static_cast<float*>(keep.act) : nullptr, saved ? static_cast<float*>(keep.mul) : nullptr,
+                                                               activation}, on);
+        args = product_args(at.down, rows, out_width, hidden, planes, 1);
+        args.a[0] = source(h, rows);
+        args.b[0] = source<T, E>(w_down, out_width, hidden, ldd, at.down_weight, on);
+        product<T, E, true, true>(at.down, args, {{static_cast<T*>(y), nullptr}, ldy, false, nullptr}, at.partial, on);
+        return launched();
+    });
+}
+
+extern "C" int dgsp_gated_ff_backward(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type, int activation,
+                                      const void* x, int64_t ldx, const void* w_gate, int64_t ldg, const void* w_up, int64_t ldu,
+                                      const void* w_down, int64_t ldd, const void* dy, int64_t lddy, const void* saved, void* dx,
+                                      void* dw_gate, void* dw_up, void* dw_down, void* workspace, int64_t workspace_bytes, void* stream) {
+    if (!gated_extents(rows, width, hidden, out_width, type) || activation < DGSP_ACT_SILU || activation > DGSP_ACT_RELU)
+        return DGSP_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 16) ||
+        workspace_bytes < dgsp_gated_ff_backward_workspace_bytes(rows, width, hidden, out_width, type))
+        return DGSP_ERR_INVALID_ARG;
+    if (rows > 0 && (!readable(x, rows, width, ldx) || !readable(w_gate, hidden, width, ldg) || !readable(w_up, hidden, width, ldu) ||
+                     !readable(w_down, out_width, hidden, ldd) || !readable(dy, rows, out_width, lddy) || !saved || !aligned(saved, 16)))
+        return DGSP_ERR_INVALID_ARG;
+    const int batch = dw_gate && dw_up ? 2 : 1;
+    Pieces pieces(workspace), kept(const_cast<void*>(saved));
+    const BackwardPieces at(pieces, rows, width, hidden, out_width, type, batch);
+    const Saved keep(kept, rows, hidden, type);
+    if (!launchable(at.slope, 1) || !launchable(at.dx, 1) || !launchable(at.gates, batch) || !launchable(at.down, 1))
+        return DGSP_ERR_UNSUPPORTED;
+    return with_elements(type, [&](auto t, auto e) {
+        using T = decltype(t);
+        using E = decltype(e);
+        const auto on = static_cast<hipStream_t>(stream);
+        const int planes = planes_of(type);
+        const bool gates = dx || dw_gate || dw_up;
+        const Source grad = source<T, E>(dy, rows, out_width, lddy, at.dy, on);
+        const Planes<E> dg = hidden_planes<T, E>(at.dg, rows, hidden), du = hidden_planes<T, E>(at.du, rows, hidden);
+        ProductArgs args;
+        if (gates && rows > 0) {
+            args = product_args(at.slope, rows, hidden, out_width, planes, 1);
+            args.a[0] = grad;
+            args.b[0] = source<T, E>(w_down, out_width, hidden, ldd, at.down_weight, on);
+            launch<E, false, true, false>(at.slope, args,
+                                          GatedSlopeOut<E>{static_cast<const float*>(keep.act), static_cast<const float*>(keep.mul), dg, du}, on);
+        }
+        if (dx) {
+            args = product_args(at.dx, rows, width, hidden, planes, 1);
+            args.pairs = 2;
+            args.a[0] = source(dg, rows);
+            args.a[1] = source(du, rows);
+            const bool alike = ldg == ldu && in_place<T>(w_gate, hidden, width, ldg) && in_place<T>(w_up, hidden, width, ldu);
+            args.b[0] = source<T, E>(w_gate, hidden, width, ldg, at.gate, on, !alike);
+            args.b[1] = source<T, E>(w_up, hidden, width, ldu, at.up_weight, on, !alike);
+            product<T, E, true, false>(at.dx, args, {{static_cast<T*>(dx), nullptr}, width, false, nullptr}, at.partial, on);
+        }
+        if (dw_gate || dw_up) {
+            args = product_args(at.gates, hidden, width, rows, planes, batch);
+            args.a[0] = source(dw_gate ? dg : du, rows);
+            args.a[1] = source(du, rows);
+            args.b[0] = source<T, E>(x, rows, width, ldx, at.x, on);
+            product<T, E, false, false>(at.gates, args, {{static_cast<T*>(dw_gate ? dw_gate : dw_up), static_cast<T*>(dw_up)}, width, false, nullptr},
+                                        at.partial, on);
+        }
+        if (dw_down) {
+            args = product_args(at.down, out_width, hidden, rows, planes, 1);
+            args.a[0] = grad;
+            const Planes<E> h = hidden_planes<T, E>(keep.h, rows, hidden);
+            args.b[0] = source(h, rows);
+            product<T, E, false, false>(at.down, args, {{static_cast<T*>(dw_down), nullptr}, hidden, false, nullptr}, at.partial, on);
+        }
+        return launched();
+    });
+}

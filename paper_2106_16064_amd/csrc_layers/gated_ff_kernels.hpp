@@ -1,40 +1,10 @@
-// The products of the gated feed-forward block: C = sum of A_s B_s over one or two pairs of operands, tiles of C in registers,
-// tiles of A and B in LDS, matrix instructions.
+// The gated feed-forward block on matrix_tiles.hpp: what becomes of the products of a tile, and how operands are laid out for it.
 #pragma once
 
 #include "../../include/dgsp_layers.h"
-#include "element_types.hpp"
+#include "matrix_tiles.hpp"
 
 namespace dgsp {
-
-template <typename T>
-struct Operand {                // element (i, k) at p[i * outer + k * inner]
-    const T* p;
-    int64_t outer, inner;
-};
-
-using f32x4 = float __attribute__((ext_vector_type(4)));
-
-template <typename T>
-struct Matrix;
-template <>
-struct Matrix<bf16_t> {
-    static constexpr int kLane = 8, kDepth = 32;        // elements per lane, depth of one instruction
-    using Fragment = bf16_t __attribute__((ext_vector_type(8)));
-    static __device__ f32x4 multiply(Fragment a, Fragment b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-};
-template <>
-struct Matrix<f16_t> {
-    static constexpr int kLane = 8, kDepth = 32;
-    using Fragment = f16_t __attribute__((ext_vector_type(8)));
-    static __device__ f32x4 multiply(Fragment a, Fragment b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-};
-template <>
-struct Matrix<float> {
-    static constexpr int kLane = 1, kDepth = 4;
-    using Fragment = float __attribute__((ext_vector_type(1)));
-    static __device__ f32x4 multiply(Fragment a, Fragment b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a[0], b[0], c, 0, 0, 0); }
-};
 
 // act(g) and its derivative
 __device__ __forceinline__ void activate(int kind, float g, float& value, float& slope) {
@@ -52,107 +22,158 @@ __device__ __forceinline__ void activate(int kind, float g, float& value, float&
     }
 }
 
-constexpr int kTile = 64, kTileDepth = 32, kTilePad = 8;
-
-// rows [i0, i0 + 64), depth [k0, k0 + 32) of an operand, zeros beyond its ends
-template <typename T>
-__device__ void stage(T (*lds)[kTileDepth + kTilePad], const Operand<T>& a, int64_t i0, int64_t n, int64_t k0, int64_t depth) {
-    for (int e = threadIdx.x; e < kTile * kTileDepth; e += 256) {
-        const int i = a.inner == 1 ? e / kTileDepth : e % kTile, k = a.inner == 1 ? e % kTileDepth : e / kTile;
-        lds[i][k] = i0 + i < n && k0 + k < depth ? a.p[(i0 + i) * a.outer + (k0 + k) * a.inner] : from_float<T>(0.0f);
-    }
-}
-
-// Four waves, each 32 x 32 of the tile: lane l holds row l % 16 and depths l / 16 * kLane ... of an operand's fragment, and
-// rows 4 * (l / 16) ... + 3 of column l % 16 of a result's.
-template <typename T, int kProducts>
-__device__ void tile_products(f32x4 (&acc)[kProducts][2][2], const Operand<T>& a, const Operand<T> (&b)[kProducts], int64_t m0, int64_t m,
-                              int64_t n0, int64_t n, int64_t depth) {
-    using M = Matrix<T>;
-    __shared__ T as[kTile][kTileDepth + kTilePad], bs[kProducts][kTile][kTileDepth + kTilePad];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
-    for (int64_t k0 = 0; k0 < depth; k0 += kTileDepth) {
-        __syncthreads();
-        stage(as, a, m0, m, k0, depth);
-        for (int p = 0; p < kProducts; ++p) stage(bs[p], b[p], n0, n, k0, depth);
-        __syncthreads();
-        for (int k = 0; k < kTileDepth; k += M::kDepth) {
-            typename M::Fragment fa[2], fb[2];
-            for (int i = 0; i < 2; ++i)
-                for (int j = 0; j < M::kLane; ++j) fa[i][j] = as[wm + 16 * i + lane % 16][k + lane / 16 * M::kLane + j];
-            for (int p = 0; p < kProducts; ++p) {
-                for (int i = 0; i < 2; ++i)
-                    for (int j = 0; j < M::kLane; ++j) fb[i][j] = bs[p][wn + 16 * i + lane % 16][k + lane / 16 * M::kLane + j];
-                for (int i = 0; i < 2; ++i)
-                    for (int j = 0; j < 2; ++j) acc[p][i][j] = M::multiply(fa[i], fb[j], acc[p][i][j]);
-            }
+// v as the sum of three bf16 numbers, each the rest rounded to nearest: what is left is below 2^-26 of v.  Where rounding would pass
+// the largest bf16 number the first one is cut off instead; what is not finite stays in the first one.
+__device__ __forceinline__ void split3(float v, bf16_t (&out)[3]) {
+    out[0] = (bf16_t)v;
+    float rest = v - (float)out[0];
+    if (!(fabsf((float)out[0]) < __builtin_inff())) {
+        if (fabsf(v) < __builtin_inff()) {
+            out[0] = __builtin_bit_cast(bf16_t, (uint16_t)(__builtin_bit_cast(uint32_t, v) >> 16));
+            rest = v - (float)out[0];
+        } else {
+            rest = 0.0f;
         }
     }
+    out[1] = (bf16_t)rest;
+    out[2] = (bf16_t)(rest - (float)out[1]);
 }
 
-// calls f(row, column, i, j, r) for the elements that this lane holds
-template <typename F>
-__device__ void each_element(int64_t m0, int64_t m, int64_t n0, int64_t n, F&& f) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
-    for (int i = 0; i < 2; ++i)
-        for (int j = 0; j < 2; ++j)
-            for (int r = 0; r < 4; ++r) {
-                const int64_t row = m0 + wm + 16 * i + lane / 16 * 4 + r, col = n0 + wn + 16 * j + lane % 16;
-                if (row < m && col < n) f(row, col, i, j, r);
+// A matrix that later products read, in planes of E.  ld is a multiple of 8.
+template <typename E>
+struct Planes {
+    E* p;
+    int64_t ld, plane;          // plane 0: one plane
+    // four neighbours
+    __device__ __forceinline__ void store(int64_t row, int64_t col, f32x4 v) const {
+        using E4 = E __attribute__((ext_vector_type(4)));
+        E* to = p + row * ld + col;
+        if (plane) {
+            if constexpr (sizeof(E) == 2 && !__is_same(E, f16_t)) {
+                E4 out[3];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    bf16_t parts[3];
+                    split3(v[r], parts);
+                    for (int q = 0; q < 3; ++q) out[q][r] = parts[q];
+                }
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<E4*>(to + q * plane) = out[q];
             }
-}
-
-// g, u and h = act(g) u, rows x hidden each; g and u are written only where the backward pass wants them
-template <typename T>
-__global__ __launch_bounds__(256) void gated_up_kernel(int64_t rows, int64_t width, int64_t hidden, int activation, Operand<T> x,
-                                                       Operand<T> w_gate, Operand<T> w_up, T* g, T* u, T* h) {
-    const int64_t tiles = (hidden + kTile - 1) / kTile, m0 = blockIdx.x / tiles * kTile, n0 = blockIdx.x % tiles * kTile;
-    f32x4 acc[2][2][2] = {};
-    const Operand<T> b[2] = {w_gate, w_up};
-    tile_products<T, 2>(acc, x, b, m0, rows, n0, hidden, width);
-    each_element(m0, rows, n0, hidden, [&](int64_t row, int64_t col, int i, int j, int r) {
-        const float gate = acc[0][i][j][r], up = acc[1][i][j][r];
-        float value, slope;
-        activate(activation, gate, value, slope);
-        const int64_t at = row * hidden + col;
-        if (g) {
-            g[at] = from_float<T>(gate);
-            u[at] = from_float<T>(up);
+        } else {
+            *reinterpret_cast<E4*>(to) = E4{from_float<E>(v[0]), from_float<E>(v[1]), from_float<E>(v[2]), from_float<E>(v[3])};
         }
-        h[at] = from_float<T>(value * up);
-    });
-}
-
-// dg and du in place of g and u, from dh = dy w_down
-template <typename T>
-__global__ __launch_bounds__(256) void gated_down_gradient_kernel(int64_t rows, int64_t hidden, int64_t out_width, int activation,
-                                                                  Operand<T> dy, Operand<T> w_down, const T* g, const T* u, T* dg, T* du) {
-    const int64_t tiles = (hidden + kTile - 1) / kTile, m0 = blockIdx.x / tiles * kTile, n0 = blockIdx.x % tiles * kTile;
-    f32x4 acc[1][2][2] = {};
-    const Operand<T> b[1] = {w_down};
-    tile_products<T, 1>(acc, dy, b, m0, rows, n0, hidden, out_width);
-    each_element(m0, rows, n0, hidden, [&](int64_t row, int64_t col, int i, int j, int r) {
-        const int64_t at = row * hidden + col;
-        float value, slope;
-        activate(activation, to_float(g[at]), value, slope);
-        const float dh = acc[0][i][j][r];
-        dg[at] = from_float<T>(dh * to_float(u[at]) * slope);
-        du[at] = from_float<T>(dh * value);
-    });
-}
-
-// c = a b^T, or a b^T + a2 b2^T
-template <typename T>
-__global__ __launch_bounds__(256) void product_kernel(int64_t m, int64_t n, int64_t depth, Operand<T> a, Operand<T> b, Operand<T> a2,
-                                                      Operand<T> b2, T* c, int64_t ldc) {
-    const int64_t tiles = (n + kTile - 1) / kTile, m0 = blockIdx.x / tiles * kTile, n0 = blockIdx.x % tiles * kTile;
-    f32x4 acc[1][2][2] = {};
-    for (int s = 0; s < 2; ++s) {
-        if (s && !a2.p) break;
-        const Operand<T> bs[1] = {s ? b2 : b};
-        tile_products<T, 1>(acc, s ? a2 : a, bs, m0, m, n0, n, depth);
     }
-    each_element(m0, m, n0, n, [&](int64_t row, int64_t col, int i, int j, int r) { c[row * ldc + col] = from_float<T>(acc[0][i][j][r]); });
+};
+
+// ---------------------------------------------------------------- laying out
+
+// `from`, rows x cols, as planes whose rows are padded to a multiple of 8 with zeros
+template <typename T, typename E>
+__global__ void lay_out_kernel(int64_t rows, int64_t cols, const T* from, int64_t ld, E* to, int64_t to_ld, int64_t plane) {
+    using E8 = E __attribute__((ext_vector_type(8)));
+    const int64_t chunks = to_ld / 8, step = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < rows * chunks; i += step) {
+        const int64_t row = i / chunks, col = (i - row * chunks) * 8;
+        const T* at = from + row * ld + col;
+        E8 out[3];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const T v = col + j < cols ? at[j] : (T)0.0f;
+            if constexpr (sizeof(T) == 4) {
+                bf16_t parts[3];
+                split3(v, parts);
+                for (int q = 0; q < 3; ++q) out[q][j] = parts[q];
+            } else {
+                out[0][j] = v;
+            }
+        }
+        for (int q = 0; q < (sizeof(T) == 4 ? 3 : 1); ++q) *reinterpret_cast<E8*>(to + q * plane + row * to_ld + col) = out[q];
+    }
+}
+
+// ---------------------------------------------------------------- products
+
+// h = act(g) u, and for the backward pass act(g) and u act'(g), which it multiplies by dh.  These two are kept in 32 bits: rounded to
+// 16 they would double the squared error of the gates' gradients, and the 8 bytes an element cost 3 % of a large block's step.
+template <typename E>
+struct GatedUpOut {
+    Planes<E> h;
+    float *act, *mul;           // null: not wanted
+    int activation;
+    __device__ __forceinline__ void store(const ProductArgs& args, const TileIndex&, int64_t m, int64_t n, f32x4 g, f32x4 u) const {
+        if (m >= args.m || n >= h.ld) return;
+        f32x4 value, slope;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float v, s;
+            activate(activation, g[r], v, s);
+            value[r] = v;
+            slope[r] = s;
+        }
+        if (act) {
+            *reinterpret_cast<f32x4*>(act + m * h.ld + n) = value;
+            *reinterpret_cast<f32x4*>(mul + m * h.ld + n) = slope * u;
+        }
+        h.store(m, n, value * u);
+    }
+};
+
+// dg = dh u act'(g) and du = dh act(g), dh = dy w_down
+template <typename E>
+struct GatedSlopeOut {
+    const float *act, *mul;
+    Planes<E> dg, du;
+    __device__ __forceinline__ void store(const ProductArgs& args, const TileIndex&, int64_t m, int64_t n, f32x4 dh) const {
+        if (m >= args.m || n >= dg.ld) return;
+        const f32x4 a = *reinterpret_cast<const f32x4*>(act + m * dg.ld + n), b = *reinterpret_cast<const f32x4*>(mul + m * dg.ld + n);
+        f32x4 g, u;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {                   // beyond the hidden width a transposed operand holds whatever lies there
+            g[r] = n + r < args.n ? dh[r] * b[r] : 0.0f;
+            u[r] = n + r < args.n ? dh[r] * a[r] : 0.0f;
+        }
+        dg.store(m, n, g);
+        du.store(m, n, u);
+    }
+};
+
+template <typename T>
+struct ProductOut {
+    T* c[2];                    // one per batch
+    int64_t ld;
+    bool vectors;               // four neighbours may be written at once
+    float* partial;             // not null: split results, [split][batch][m][n padded to 4]
+    __device__ __forceinline__ void store(const ProductArgs& args, const TileIndex& tile, int64_t m, int64_t n, f32x4 v) const {
+        using T4 = T __attribute__((ext_vector_type(4)));
+        if (m >= args.m || n >= args.n) return;
+        if (partial) {
+            const int64_t padded = (args.n + 3) / 4 * 4;
+            *reinterpret_cast<f32x4*>(partial + (((int64_t)tile.split * args.batch + tile.batch) * args.m + m) * padded + n) = v;
+            return;
+        }
+        T* to = c[tile.batch] + m * ld + n;
+        if (vectors && n + 4 <= args.n) {
+            *reinterpret_cast<T4*>(to) = T4{from_float<T>(v[0]), from_float<T>(v[1]), from_float<T>(v[2]), from_float<T>(v[3])};
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (n + r < args.n) to[r] = from_float<T>(v[r]);
+        }
+    }
+};
+
+// the sum of the splits, in order
+template <typename T>
+__global__ void join_kernel(int64_t m, int64_t n, int batch, int splits, const float* partial, ProductOut<T> out) {
+    const int64_t quads = (n + 3) / 4, count = m * quads, step = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < count * batch; i += step) {
+        const int64_t b = i / count, row = (i - b * count) / quads, col = (i % quads) * 4;
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(partial + 4 * (s * count * batch + i));
+        for (int r = 0; r < 4; ++r)
+            if (col + r < n) out.c[b][row * out.ld + col + r] = from_float<T>(sum[r]);
+    }
 }
 
 }  // namespace dgsp
