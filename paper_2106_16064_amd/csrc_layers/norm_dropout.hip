@@ -1,4 +1,4 @@
-// Host side of layer norm and dropout: argument checks and launches.  The C-ABI is documented in include/dgsp_layers.h.
+// Host side of layer norm and dropout: argument checks, how rows are held, launches.  The C-ABI is documented in include/dgsp_layers.h.
 #include "layers_host.hpp"
 
 #include <cmath>
@@ -23,10 +23,52 @@ bool make_mask(const dgsp_dropout_t* d, DropMask& mask) {
     return true;
 }
 
-constexpr int kThreads = 256;
+constexpr int64_t kCus = 256;
 
-// a wave per row, and several rows per wave where there are very many
-unsigned row_blocks(int64_t rows) { return (unsigned)std::min<int64_t>(ceil_div(rows, kThreads / 64), 1 << 20); }
+// How rows of a width are held: up to 512 elements a wave holds one or several, up to 8192 a workgroup holds one.
+struct Hold {
+    bool whole;             // a workgroup a row
+    int lanes, threads;
+    bool fits;
+    explicit Hold(int64_t width) {
+        const int64_t chunks = ceil_div(width, kChunk);
+        whole = chunks > 64;
+        fits = chunks <= 1024;
+        if (!whole) {
+            lanes = 1;
+            while (lanes < chunks) lanes *= 2;
+            threads = 256;
+        } else {
+            threads = lanes = (int)std::min<int64_t>(1024, ceil_div(chunks, 64) * 64);
+        }
+    }
+    int64_t rows_a_group() const { return whole ? 1 : threads / lanes; }
+};
+
+template <typename T, bool kAdd>
+void launch_norm(const Hold& hold, const NormArgs<T>& args, hipStream_t stream) {
+    const unsigned groups = (unsigned)std::min<int64_t>(ceil_div(args.rows, hold.rows_a_group()), kCus * 2048 / hold.threads);
+    if (hold.whole)
+        layer_norm_kernel<T, true, kAdd><<<groups, hold.threads, 0, stream>>>(args);
+    else
+        layer_norm_kernel<T, false, kAdd><<<groups, hold.threads, 0, stream>>>(args);
+}
+
+// Workgroups of the backward pass, each with sums of its own for the parameters: few enough that these are a small part of what is
+// read anyway.
+int64_t backward_groups(const Hold& hold, int64_t rows) {
+    if (!hold.fits) return std::min<int64_t>(std::max<int64_t>(rows, 1), 64);
+    const int64_t most = hold.whole ? kCus * std::max(1, 1024 / hold.threads) : kCus * 4;
+    return std::max<int64_t>(1, std::min(ceil_div(rows, hold.rows_a_group()), most));
+}
+
+template <typename T, bool kAdd>
+void launch_backward(const Hold& hold, const NormBackwardArgs<T>& args, int64_t groups, hipStream_t stream) {
+    if (hold.whole)
+        layer_norm_backward_kernel<T, true, kAdd><<<(unsigned)groups, hold.threads, 0, stream>>>(args);
+    else
+        layer_norm_backward_kernel<T, false, kAdd><<<(unsigned)groups, hold.threads, 0, stream>>>(args);
+}
 
 }  // namespace
 
@@ -40,12 +82,19 @@ extern "C" int dgsp_dropout(int64_t rows, int64_t width, int type, const dgsp_dr
     if (rows == 0 || width == 0) return DGSP_OK;
     if (!readable(x, rows, width, ldx) || (residual && !readable(residual, rows, width, ldr)) || !writable(y, rows, width, ldy))
         return DGSP_ERR_INVALID_ARG;
-    const int64_t groups = rows * ceil_div(width, kDropGroup);
-    const unsigned blocks = (unsigned)std::min<int64_t>(ceil_div(groups, kThreads), 1 << 20);
+    const int64_t chunks = ceil_div(width, kChunk), total = rows * chunks;
+    // four chunks a lane keep more loads in flight, where there is work for every lane of the machine
+    const int each = total >= kCus * 2048 * 4 ? 4 : 1;
+    const unsigned groups = (unsigned)std::min<int64_t>(ceil_div(total, kDropThreads * each), 1 << 23);
     return with_type(type, [&](auto element) {
         using T = decltype(element);
-        dropout_kernel<T><<<blocks, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
-            rows, width, mask, static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy);
+        const auto *in = static_cast<const T*>(x), *add = static_cast<const T*>(residual);
+        const auto on = static_cast<hipStream_t>(stream);
+        const Divisor divisor((uint32_t)chunks);
+        if (each == 4)
+            dropout_kernel<T, 4><<<groups, kDropThreads, 0, on>>>(rows, width, divisor, mask, in, ldx, add, ldr, static_cast<T*>(y), ldy);
+        else
+            dropout_kernel<T, 1><<<groups, kDropThreads, 0, on>>>(rows, width, divisor, mask, in, ldx, add, ldr, static_cast<T*>(y), ldy);
         return launched();
     });
 }
@@ -67,16 +116,23 @@ extern "C" int dgsp_layer_norm(int64_t rows, int64_t width, int type, int param_
         return DGSP_ERR_INVALID_ARG;
     return with_type(type, [&](auto element) {
         using T = decltype(element);
-        const NormInput<T> in{static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr, mask};
-        layer_norm_kernel<T><<<row_blocks(rows), kThreads, 0, static_cast<hipStream_t>(stream)>>>(
-            rows, width, in, weight, bias, param_type != type, eps, static_cast<T*>(y), ldy, static_cast<T*>(sum), lds, stats);
+        const Hold hold(width);
+        const auto on = static_cast<hipStream_t>(stream);
+        const NormArgs<T> args{rows,   width, hold.lanes, static_cast<const T*>(x), static_cast<const T*>(residual), ldx, ldr, mask, weight, bias, param_type != type,
+                               eps,    static_cast<T*>(y), static_cast<T*>(sum), ldy, lds, stats};
+        if (!hold.fits)
+            layer_norm_long_kernel<T><<<(unsigned)std::min<int64_t>(rows, kCus * 2), 1024, 0, on>>>(args);
+        else if (residual)
+            launch_norm<T, true>(hold, args, on);
+        else
+            launch_norm<T, false>(hold, args, on);
         return launched();
     });
 }
 
 extern "C" int64_t dgsp_layer_norm_backward_workspace_bytes(int64_t rows, int64_t width) {
     if (rows < 0 || width < 1) return 0;
-    return 2 * kNormSlices * width * 4;
+    return 2 * backward_groups(Hold(width), rows) * width * 4;
 }
 
 extern "C" int dgsp_layer_norm_backward(int64_t rows, int64_t width, int type, int param_type, const void* s, int64_t lds,
@@ -95,19 +151,25 @@ extern "C" int dgsp_layer_norm_backward(int64_t rows, int64_t width, int type, i
         return DGSP_ERR_INVALID_ARG;
     return with_type(type, [&](auto element) {
         using T = decltype(element);
+        const Hold hold(width);
         const auto on = static_cast<hipStream_t>(stream);
         const bool wide = param_type != type;
-        if (rows > 0)
-            layer_norm_backward_kernel<T><<<row_blocks(rows), kThreads, 0, on>>>(
-                rows, width, static_cast<const T*>(s), lds, stats, weight, wide, static_cast<const T*>(dy), lddy,
-                static_cast<const T*>(ds), ldds, mask, static_cast<T*>(dsum), static_cast<T*>(dx));
-        if (params) {
-            auto* partial = static_cast<float*>(workspace);
-            const unsigned columns = (unsigned)ceil_div(width, kThreads);
-            layer_norm_param_partials_kernel<T><<<dim3(columns, kNormSlices), kThreads, 0, on>>>(
-                rows, width, static_cast<const T*>(s), lds, stats, static_cast<const T*>(dy), lddy, partial);
-            layer_norm_param_sums_kernel<T><<<columns, kThreads, 0, on>>>(width, partial, dweight, dbias, wide);
+        const int64_t groups = backward_groups(hold, rows);
+        const NormBackwardArgs<T> args{rows, width, hold.lanes, static_cast<const T*>(s), static_cast<const T*>(dy), static_cast<const T*>(ds),
+                                       lds,  lddy,  ldds,       stats, weight, wide, mask, static_cast<T*>(dsum), static_cast<T*>(dx),
+                                       params ? static_cast<float*>(workspace) : nullptr};
+        if (rows > 0 && !hold.fits) {
+            layer_norm_backward_long_kernel<T><<<(unsigned)std::min<int64_t>(rows, kCus * 2), 1024, 0, on>>>(args);
+            if (params) layer_norm_long_params_kernel<T><<<dim3((unsigned)ceil_div(width, 256), (unsigned)groups), 256, 0, on>>>(args);
+        } else if (rows > 0) {
+            if (ds || dx)
+                launch_backward<T, true>(hold, args, groups, on);
+            else
+                launch_backward<T, false>(hold, args, groups, on);
         }
+        if (params)
+            layer_norm_params_kernel<T><<<(unsigned)ceil_div(2 * width, kParamColumns), kParamColumns * kParamSlices, 0, on>>>(
+                width, rows > 0 ? groups : 0, args.partial, dweight, dbias, wide);
         return launched();
     });
 }
