@@ -3,6 +3,7 @@
 #include "layers_host.hpp"
 
 #include "gated_ff_kernels.hpp"
+#include "narrow_ff.hpp"
 
 namespace {
 
@@ -17,6 +18,8 @@ bool gated_extents(int64_t rows, int64_t width, int64_t hidden, int64_t out_widt
     return rows >= 0 && rows <= kMostRows && width >= 1 && width <= kMostWidth && hidden >= 1 && hidden <= kMostWidth &&
            out_width >= 1 && out_width <= kMostWidth && known_type(type);
 }
+
+bool enough(const void* workspace, int64_t bytes, int64_t need) { return need == 0 || (workspace && aligned(workspace, 16) && bytes >= need); }
 
 int planes_of(int type) { return type == DGSP_F32 ? 3 : 1; }
 
@@ -195,14 +198,14 @@ int with_elements(int type, F&& f) {
 }  // namespace
 
 extern "C" int64_t dgsp_gated_ff_saved_bytes(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type) {
-    if (!gated_extents(rows, width, hidden, out_width, type)) return 0;
+    if (!gated_extents(rows, width, hidden, out_width, type) || narrow_fits(width, hidden, out_width, type)) return 0;
     Pieces pieces(nullptr);
     Saved saved(pieces, rows, hidden, type);
     return pieces.used();
 }
 
 extern "C" int64_t dgsp_gated_ff_workspace_bytes(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type) {
-    if (!gated_extents(rows, width, hidden, out_width, type)) return 0;
+    if (!gated_extents(rows, width, hidden, out_width, type) || narrow_fits(width, hidden, out_width, type)) return 0;
     Pieces pieces(nullptr);
     ForwardPieces need(pieces, rows, width, hidden, out_width, type, false);
     return pieces.used();
@@ -210,6 +213,7 @@ extern "C" int64_t dgsp_gated_ff_workspace_bytes(int64_t rows, int64_t width, in
 
 extern "C" int64_t dgsp_gated_ff_backward_workspace_bytes(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type) {
     if (!gated_extents(rows, width, hidden, out_width, type)) return 0;
+    if (narrow_fits(width, hidden, out_width, type)) return narrow_backward_bytes(rows, width, hidden, out_width);
     Pieces one(nullptr), two(nullptr);
     BackwardPieces need_one(one, rows, width, hidden, out_width, type, 1), need_two(two, rows, width, hidden, out_width, type, 2);
     return std::max(one.used(), two.used());
@@ -222,9 +226,11 @@ extern "C" int dgsp_gated_ff(int64_t rows, int64_t width, int64_t hidden, int64_
         return DGSP_ERR_INVALID_ARG;
     if (rows == 0) return DGSP_OK;
     if (!readable(x, rows, width, ldx) || !readable(w_gate, hidden, width, ldg) || !readable(w_up, hidden, width, ldu) ||
-        !readable(w_down, out_width, hidden, ldd) || !writable(y, rows, out_width, ldy) || !aligned(saved, 16) || !workspace ||
-        !aligned(workspace, 16) || workspace_bytes < dgsp_gated_ff_workspace_bytes(rows, width, hidden, out_width, type))
+        !readable(w_down, out_width, hidden, ldd) || !writable(y, rows, out_width, ldy) || !aligned(saved, 16) ||
+        !enough(workspace, workspace_bytes, dgsp_gated_ff_workspace_bytes(rows, width, hidden, out_width, type)))
         return DGSP_ERR_INVALID_ARG;
+    if (narrow_fits(width, hidden, out_width, type))
+        return narrow_forward({rows, width, hidden, out_width, type, activation, x, ldx, w_gate, ldg, w_up, ldu, w_down, ldd, y, ldy}, stream);
     Pieces pieces(workspace), kept(saved);
     const ForwardPieces at(pieces, rows, width, hidden, out_width, type, saved != nullptr);
     const Saved keep(kept, rows, hidden, type);
@@ -255,12 +261,15 @@ extern "C" int dgsp_gated_ff_backward(int64_t rows, int64_t width, int64_t hidde
                                       void* dw_gate, void* dw_up, void* dw_down, void* workspace, int64_t workspace_bytes, void* stream) {
     if (!gated_extents(rows, width, hidden, out_width, type) || activation < DGSP_ACT_SILU || activation > DGSP_ACT_RELU)
         return DGSP_ERR_INVALID_ARG;
-    if (!workspace || !aligned(workspace, 16) ||
-        workspace_bytes < dgsp_gated_ff_backward_workspace_bytes(rows, width, hidden, out_width, type))
+    if (!enough(workspace, workspace_bytes, dgsp_gated_ff_backward_workspace_bytes(rows, width, hidden, out_width, type)))
         return DGSP_ERR_INVALID_ARG;
+    const bool narrow = narrow_fits(width, hidden, out_width, type);
     if (rows > 0 && (!readable(x, rows, width, ldx) || !readable(w_gate, hidden, width, ldg) || !readable(w_up, hidden, width, ldu) ||
-                     !readable(w_down, out_width, hidden, ldd) || !readable(dy, rows, out_width, lddy) || !saved || !aligned(saved, 16)))
+                     !readable(w_down, out_width, hidden, ldd) || !readable(dy, rows, out_width, lddy) || (!saved && !narrow) || !aligned(saved, 16)))
         return DGSP_ERR_INVALID_ARG;
+    if (narrow)
+        return narrow_backward({rows, width, hidden, out_width, type, activation, x, ldx, w_gate, ldg, w_up, ldu, w_down, ldd, nullptr, 0, dy, lddy, dx,
+                                dw_gate, dw_up, dw_down, workspace}, stream);
     const int batch = dw_gate && dw_up ? 2 : 1;
     Pieces pieces(workspace), kept(const_cast<void*>(saved));
     const BackwardPieces at(pieces, rows, width, hidden, out_width, type, batch);

@@ -368,7 +368,8 @@ def test_gradients_of_one_result_alone():
 
 BLOCKS = [(1, 1, 1, 1), (1, 16, 32, 16), (2, 5, 3, 7), (3, 100, 33, 17), (17, 64, 64, 64), (16, 256, 512, 256), (31, 130, 66, 40), (33, 64, 128, 64),
           (64, 48, 200, 96), (65, 33, 129, 31), (100, 128, 96, 128), (128, 64, 256, 64), (200, 72, 136, 200), (257, 130, 258, 66), (300, 256, 300, 8),
-          (1000, 64, 128, 64), (1025, 40, 72, 40), (4, 1000, 2731, 1000), (520, 96, 520, 520), (37, 512, 1025, 100), (1, 2048, 1024, 2048), (9, 24, 4096, 24)]
+          (1000, 64, 128, 64), (1025, 40, 72, 40), (4, 1000, 2731, 1000), (520, 96, 520, 520), (37, 512, 1025, 100), (1, 2048, 1024, 2048), (9, 24, 4096, 24),
+          (300, 20, 200, 30), (500, 128, 128, 100), (77, 100, 64, 128), (4200, 32, 64, 32), (200, 64, 257, 64), (70, 129, 64, 32)]
 
 
 @pytest.mark.parametrize("activation", ["silu", "gelu", "relu"])
