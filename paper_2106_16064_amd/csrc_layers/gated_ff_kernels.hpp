@@ -22,23 +22,31 @@ __device__ __forceinline__ void activate(int kind, float g, float& value, float&
     }
 }
 
-// The same for results of 16 bits: exp2 and the reciprocal of the hardware (one unit in the last place of float each; the argument of the
-// exponential is off by g 2^-24), and erf to 1.5e-7 (Abramowitz, Stegun, Handbook of Mathematical Functions, 7.1.26).  A third of the
-// instructions.
-__device__ __forceinline__ void activate_short(int kind, float g, float& value, float& slope) {
+// The same for results of 16 bits, kCount numbers at once (one branch on the kind for all of them): exp2 and the reciprocal of the
+// hardware (one unit in the last place of float each; the argument of the exponential is off by g 2^-24), and erf to 1.5e-7 (Abramowitz,
+// Stegun, Handbook of Mathematical Functions, 7.1.26).  A third of the instructions.
+template <int kCount>
+__device__ __forceinline__ void activate_short(int kind, const float (&g)[kCount], float (&value)[kCount], float (&slope)[kCount]) {
     if (kind == DGSP_ACT_RELU) {
-        activate(kind, g, value, slope);
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) activate(DGSP_ACT_RELU, g[i], value[i], slope[i]);
     } else if (kind == DGSP_ACT_SILU) {
-        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g));
-        value = g * s;
-        slope = s * (1.0f + g * (1.0f - s));
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g[i]));
+            value[i] = g[i] * s;
+            slope[i] = s + value[i] * (1.0f - s);
+        }
     } else {
-        const float z = fabsf(g) * 0.70710678f, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * z);
-        const float e = __builtin_amdgcn_exp2f(-1.44269504f * (z * z));
-        const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
-        const float c = g < 0.0f ? tail : 1.0f - tail;
-        value = g * c;
-        slope = c + g * e * 0.39894228f;
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const float z = fabsf(g[i]) * 0.70710678f, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * z);
+            const float e = __builtin_amdgcn_exp2f(-1.44269504f * (z * z));
+            const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+            const float c = g[i] < 0.0f ? tail : 1.0f - tail;
+            value[i] = g[i] * c;
+            slope[i] = c + g[i] * e * 0.39894228f;
+        }
     }
 }
 

@@ -69,22 +69,33 @@ __device__ __forceinline__ void stage(uint16_t* lds, int lds_ld, int padded_rows
     }
 }
 
-// the fragments of 16 rows along the columns: lane l has row l % 16, columns 32 s + 8 (l / 16) ... + 7
-template <typename E, int kSteps>
-__device__ __forceinline__ void ask_rows(s16x8 (&out)[kSteps], const E* from, int64_t ld, int64_t row, int64_t rows, int64_t cols, int lane) {
+// The fragments of 16 rows along the columns: lane l has row l % 16, columns 32 s + 8 (l / 16) ... + 7.  `tile`: first of the wave's rows.
+// kFull: all columns are there and in whole 16-byte pieces; reads beyond the last row give 0 by the bounds of the buffer.
+template <typename E, int kSteps, bool kFull>
+__device__ __forceinline__ void ask_rows(s16x8 (&out)[kSteps], const E* from, int64_t ld, int64_t tile, int64_t rows, int64_t cols, int lane) {
+    if constexpr (kFull) {
+        const int64_t left = tile < rows ? ((rows - 1 - tile) * ld + cols) * 2 : 0;
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(from + (tile < rows ? tile * ld : 0)), 0,
+                                                                           (int)(left < 0x7fffffff ? left : 0x7fffffff), 0x00020000);
+        const int offset = (int)((lane % 16) * ld + 8 * (lane / 16)) * 2;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-        const int64_t col = 32 * s + 8 * (lane / 16);
-        out[s] = s16x8{};
-        if (row < rows && col < cols) out[s] = __builtin_bit_cast(s16x8, load_chunk(from + row * ld + col, cols - col).q[0]);
+        for (int s = 0; s < kSteps; ++s) out[s] = __builtin_bit_cast(s16x8, __builtin_amdgcn_raw_buffer_load_b128(r, offset + 64 * s, 0, 0));
+    } else {
+        const int64_t row = tile + lane % 16;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int64_t col = 32 * s + 8 * (lane / 16);
+            out[s] = s16x8{};
+            if (row < rows && col < cols) out[s] = __builtin_bit_cast(s16x8, load_chunk(from + row * ld + col, cols - col).q[0]);
+        }
     }
 }
 
 // four neighbours of a row
-template <typename E>
+template <typename E, bool kFull>
 __device__ __forceinline__ void store4(E* to, int64_t col, int64_t cols, f32x4 v) {
     using E4 = E __attribute__((ext_vector_type(4), aligned(2)));
-    if (col + 4 <= cols) {
+    if (kFull || col + 4 <= cols) {
         *reinterpret_cast<E4*>(to + col) = E4{from_float<E>(v[0]), from_float<E>(v[1]), from_float<E>(v[2]), from_float<E>(v[3])};
     } else {
 #pragma unroll
@@ -94,7 +105,7 @@ __device__ __forceinline__ void store4(E* to, int64_t col, int64_t cols, f32x4 v
 }
 
 // A wave takes 32 rows at a time and needs nothing of the others.
-template <typename E, int kP, int kH, int kWaves>
+template <typename E, int kP, int kH, int kWaves, bool kFull>
 __global__ __launch_bounds__(64 * kWaves) void narrow_forward_kernel(NarrowArgs<E> a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using Shape = NarrowShape<E, kP, kH, kWaves>;
@@ -104,12 +115,12 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_forward_kernel(NarrowArgs<
     stage(gate, Shape::kLdUp, kH, kP, a.w_gate, a.ldg, a.hidden, a.width);
     stage(up, Shape::kLdUp, kH, kP, a.w_up, a.ldu, a.hidden, a.width);
     stage(down, Shape::kLdDown, kP, kH, a.w_down, a.ldd, a.out_width, a.hidden);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane / 16, own = lane % 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane / 16, own = lane % 16;
     const int64_t step = (int64_t)gridDim.x * kWaves * 32;
     int64_t row0 = ((int64_t)blockIdx.x * kWaves + wave) * 32;
     s16x8 next[2][kSteps];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) ask_rows<E>(next[b], a.x, a.ldx, row0 + 16 * b + own, a.rows, a.width, lane);
+    for (int b = 0; b < 2; ++b) ask_rows<E, kSteps, kFull>(next[b], a.x, a.ldx, row0 + 16 * b, a.rows, a.width, lane);
     __syncthreads();
     for (; row0 < a.rows; row0 += step) {
         s16x8 x[2][kSteps];
@@ -118,7 +129,7 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_forward_kernel(NarrowArgs<
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) x[b][s] = next[b][s];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) ask_rows<E>(next[b], a.x, a.ldx, row0 + step + 16 * b + own, a.rows, a.width, lane);
+        for (int b = 0; b < 2; ++b) ask_rows<E, kSteps, kFull>(next[b], a.x, a.ldx, row0 + step + 16 * b, a.rows, a.width, lane);
         f32x4 y[kOut][2] = {};
 #pragma unroll 1
         for (int h0 = 0; h0 < kH; h0 += 32) {
@@ -136,17 +147,12 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_forward_kernel(NarrowArgs<
                         u[b] = multiply<E>(wu, x[b][s], u[b]);
                     }
                 }
+                float in[8], value[8], slope[8];
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    f32x4 value;
+                for (int i = 0; i < 8; ++i) in[i] = g[i / 4][i % 4];
+                activate_short(a.activation, in, value, slope);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float v, slope;
-                        activate_short(a.activation, g[b][r], v, slope);
-                        value[r] = v * u[b][r];
-                    }
-                    h[b][part] = pack<E>(value);
-                }
+                for (int b = 0; b < 2; ++b) h[b][part] = pack<E>(f32x4{value[4 * b], value[4 * b + 1], value[4 * b + 2], value[4 * b + 3]} * u[b]);
             }
 #pragma unroll
             for (int o = 0; o < kOut; ++o) {
@@ -161,7 +167,7 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_forward_kernel(NarrowArgs<
             const int64_t row = row0 + 16 * b + own;
             if (row >= a.rows) continue;
 #pragma unroll
-            for (int o = 0; o < kOut; ++o) store4(a.y + row * a.ldy, 16 * o + 4 * q, a.out_width, y[o][b]);
+            for (int o = 0; o < kOut; ++o) store4<E, kFull>(a.y + row * a.ldy, 16 * o + 4 * q, a.out_width, y[o][b]);
         }
     }
 #endif
@@ -170,8 +176,8 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_forward_kernel(NarrowArgs<
 // A workgroup takes 16 rows a wave.  For 32 hidden values at a time each wave makes g, u, dh and from them dg, du and h of its rows,
 // adds to dx, and leaves dg, du and h in LDS; then each wave adds the rows of all waves to its own blocks of the weights' gradients,
 // which stay in registers until the workgroup's last tile.
-template <typename E, int kP, int kH, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs<E> a) {
+template <typename E, int kP, int kH, int kWaves, bool kFull>
+__global__ __launch_bounds__(64 * kWaves) void narrow_backward_staged_kernel(NarrowArgs<E> a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using Shape = NarrowShape<E, kP, kH, kWaves>;
     constexpr int kSteps = kP / 32, kOut = kP / 16, kParts = kH / 32, kBlocks = 2 * kOut;
@@ -188,10 +194,10 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs
     const int64_t step = (int64_t)gridDim.x * Shape::kRows;
     f32x4 dw[kParts][3][kOwn] = {};
     s16x8 next_x[kSteps], next_dy[kSteps];
-    int64_t row = (int64_t)blockIdx.x * Shape::kRows + 16 * wave + own;
-    ask_rows<E>(next_x, a.x, a.ldx, row, a.rows, a.width, lane);
-    ask_rows<E>(next_dy, a.dy, a.lddy, row, a.rows, a.out_width, lane);
-    for (int64_t tile = (int64_t)blockIdx.x * Shape::kRows; tile < a.rows; tile += step, row += step) {
+    int64_t first = (int64_t)blockIdx.x * Shape::kRows + 16 * wave;
+    ask_rows<E, kSteps, kFull>(next_x, a.x, a.ldx, first, a.rows, a.width, lane);
+    ask_rows<E, kSteps, kFull>(next_dy, a.dy, a.lddy, first, a.rows, a.out_width, lane);
+    for (int64_t tile = (int64_t)blockIdx.x * Shape::kRows; tile < a.rows; tile += step, first += step) {
         s16x8 x[kSteps], dy[kSteps];
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
@@ -201,8 +207,8 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs
             *reinterpret_cast<s16x8*>(x_rows + at) = x[s];
             *reinterpret_cast<s16x8*>(dy_rows + at) = dy[s];
         }
-        ask_rows<E>(next_x, a.x, a.ldx, row + step, a.rows, a.width, lane);
-        ask_rows<E>(next_dy, a.dy, a.lddy, row + step, a.rows, a.out_width, lane);
+        ask_rows<E, kSteps, kFull>(next_x, a.x, a.ldx, first + step, a.rows, a.width, lane);
+        ask_rows<E, kSteps, kFull>(next_dy, a.dy, a.lddy, first + step, a.rows, a.out_width, lane);
         __syncthreads();                                               // the weights, and these rows, are there
         f32x4 dx[kOut] = {};
 #pragma unroll
@@ -221,14 +227,14 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs
                     dh = multiply<E>(join(read_column(rows, Shape::kLdDown, lane), read_column(rows + 4 * Shape::kLdDown, Shape::kLdDown, lane)),
                                      dy[s], dh);
                 }
+                float in[4] = {g[0], g[1], g[2], g[3]}, value[4], slope[4];
+                activate_short(a.activation, in, value, slope);
                 f32x4 gs, us, hs;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    float v, slope;
-                    activate_short(a.activation, g[r], v, slope);
-                    gs[r] = dh[r] * u[r] * slope;
-                    us[r] = dh[r] * v;
-                    hs[r] = v * u[r];
+                    gs[r] = dh[r] * u[r] * slope[r];
+                    us[r] = dh[r] * value[r];
+                    hs[r] = value[r] * u[r];
                 }
                 dg[part] = pack<E>(gs);
                 du[part] = pack<E>(us);
@@ -268,9 +274,9 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs
             }
             __syncthreads();                                           // and may be written over
         }
-        if (a.dx && row < a.rows) {
+        if (a.dx && first + own < a.rows) {
 #pragma unroll
-            for (int d = 0; d < kOut; ++d) store4(a.dx + row * a.width, 16 * d + 4 * q, a.width, dx[d]);
+            for (int d = 0; d < kOut; ++d) store4<E, kFull>(a.dx + (first + own) * a.width, 16 * d + 4 * q, a.width, dx[d]);
         }
     }
     if (!a.partial || wave * kOwn >= kBlocks) return;
@@ -286,6 +292,136 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs
                 to[kH * kP + (hid + 4 * q + r) * kP + col + own] = dw[p][1][i][r];
                 to[2 * kH * kP + (col + 4 * q + r) * kH + hid + own] = dw[p][2][i][r];
             }
+        }
+#endif
+}
+
+// The same with the weights in registers, where they and the sums fit: a wave takes 16 hidden values of all rows, so that it reads x and dy
+// where the kernel above reads weights, and the three gradients of its weights need nothing of other waves.  Here vertices are the rows of
+// g, u and dh, and the results are operands of a sum over the vertices where they lie.  dg and du go to LDS, transposed, for dx, of which
+// a wave takes 16 columns.
+template <typename E, int kP, int kWaves, bool kFull>
+__global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs<E> a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int kH = 16 * kWaves, kRows = 16 * kWaves, kSteps = kP / 32, kOut = kP / 16, kParts = kH / 32;
+    constexpr int kLd = kP + 8, kLdT = kRows + 8;
+    constexpr int kShare = kWaves / kOut > 0 ? kWaves / kOut : 1;          // waves that share 16 columns of dx
+    using Shape = NarrowShape<E, kP, kH, kWaves>;
+    __shared__ __attribute__((aligned(16))) uint16_t x_rows[kRows * kLd], dy_rows[kRows * kLd], dg_columns[kH * kLdT], du_columns[kH * kLdT];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane / 16, own = lane % 16;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+
+    // one element of a matrix, 0 beyond its ends
+    auto element = [](const E* w, int64_t ld, int64_t row, int64_t rows, int64_t col, int64_t cols) {
+        return row < rows && col < cols ? __builtin_bit_cast(short, w[row * ld + col]) : (short)0;
+    };
+    // weights: of this wave's hidden values along width and out_width, and of its columns of dx along hidden
+    s16x8 gate[kSteps], up[kSteps], down[kSteps], gate_columns[kParts], up_columns[kParts];
+    const int64_t hid = 16 * wave + own, col = 16 * (wave / kShare) + own;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t k = 32 * s + 8 * q + j;
+            gate[s][j] = element(a.w_gate, a.ldg, hid, a.hidden, k, a.width);
+            up[s][j] = element(a.w_up, a.ldu, hid, a.hidden, k, a.width);
+            down[s][j] = element(a.w_down, a.ldd, k, a.out_width, hid, a.hidden);
+        }
+#pragma unroll
+    for (int t = 0; t < kParts; ++t)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t k = 32 * t + 8 * q + j;
+            gate_columns[t][j] = element(a.w_gate, a.ldg, k, a.hidden, col, a.width);
+            up_columns[t][j] = element(a.w_up, a.ldu, k, a.hidden, col, a.width);
+        }
+
+    f32x4 dw[3][kOut] = {};
+    s16x8 next_x[kSteps], next_dy[kSteps];
+    int64_t tile = (int64_t)blockIdx.x * kRows;
+    auto ask = [&](int64_t at) {
+        ask_rows<E, kSteps, kFull>(next_x, a.x, a.ldx, at + 16 * wave, a.rows, a.width, lane);
+        ask_rows<E, kSteps, kFull>(next_dy, a.dy, a.lddy, at + 16 * wave, a.rows, a.out_width, lane);
+    };
+    auto leave = [&] {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int at = (16 * wave + own) * kLd + 32 * s + 8 * q;
+            *reinterpret_cast<s16x8*>(x_rows + at) = next_x[s];
+            *reinterpret_cast<s16x8*>(dy_rows + at) = next_dy[s];
+        }
+    };
+    ask(tile);
+    leave();
+    for (; tile < a.rows; tile += step) {
+        ask(tile + step);
+        __syncthreads();                                                    // x and dy are there, the last tile's dg and du are read
+#pragma unroll
+        for (int r0 = 0; r0 < kRows; r0 += 32) {
+            f32x4 g[2] = {}, u[2] = {}, dh[2] = {};
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    const int at = (r0 + 16 * b + own) * kLd + 32 * s + 8 * q;
+                    const s16x8 x = read8(x_rows + at), dy = read8(dy_rows + at);
+                    g[b] = multiply<E>(x, gate[s], g[b]);
+                    u[b] = multiply<E>(x, up[s], u[b]);
+                    dh[b] = multiply<E>(dy, down[s], dh[b]);
+                }
+            float in[8], value[8], slope[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) in[i] = g[i / 4][i % 4];
+            activate_short(a.activation, in, value, slope);
+            s16x4 dg[2], du[2], h[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const f32x4 v = {value[4 * b], value[4 * b + 1], value[4 * b + 2], value[4 * b + 3]};
+                const f32x4 m = {slope[4 * b], slope[4 * b + 1], slope[4 * b + 2], slope[4 * b + 3]};
+                h[b] = pack<E>(v * u[b]);
+                du[b] = pack<E>(dh[b] * v);
+                dg[b] = pack<E>(dh[b] * u[b] * m);
+                const int at = (16 * wave + own) * kLdT + r0 + 16 * b + 4 * q;
+                *reinterpret_cast<s16x4*>(dg_columns + at) = dg[b];
+                *reinterpret_cast<s16x4*>(du_columns + at) = du[b];
+            }
+            // the 32 vertices in the order of the results: 4 q ... 4 q + 3, 16 + 4 q ... + 3
+#pragma unroll
+            for (int c = 0; c < kOut; ++c) {
+                const int at = (r0 + 4 * q) * kLd + 16 * c;
+                const s16x8 x = join(read_column(x_rows + at, kLd, lane), read_column(x_rows + at + 16 * kLd, kLd, lane));
+                const s16x8 dy = join(read_column(dy_rows + at, kLd, lane), read_column(dy_rows + at + 16 * kLd, kLd, lane));
+                dw[0][c] = multiply<E>(join(dg[0], dg[1]), x, dw[0][c]);
+                dw[1][c] = multiply<E>(join(du[0], du[1]), x, dw[1][c]);
+                dw[2][c] = multiply<E>(dy, join(h[0], h[1]), dw[2][c]);
+            }
+        }
+        __syncthreads();                                                    // dg and du are there, x and dy are read
+        leave();
+        if (a.dx && wave / kShare < kOut) {
+#pragma unroll
+            for (int r0 = wave % kShare * 16; r0 < kRows; r0 += kShare * 16) {
+                f32x4 dx = {};
+#pragma unroll
+                for (int t = 0; t < kParts; ++t) {
+                    const int at = (32 * t + 8 * q) * kLdT + r0;
+                    dx = multiply<E>(gate_columns[t], join(read_column(dg_columns + at, kLdT, lane), read_column(dg_columns + at + 4 * kLdT, kLdT, lane)), dx);
+                    dx = multiply<E>(up_columns[t], join(read_column(du_columns + at, kLdT, lane), read_column(du_columns + at + 4 * kLdT, kLdT, lane)), dx);
+                }
+                const int64_t row = tile + r0 + own;
+                if (row < a.rows) store4<E, kFull>(a.dx + row * a.width, 16 * (wave / kShare) + 4 * q, a.width, dx);
+            }
+        }
+    }
+    if (!a.partial) return;
+    float* to = a.partial + (int64_t)blockIdx.x * Shape::kGradients;
+#pragma unroll
+    for (int c = 0; c < kOut; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            to[(16 * wave + 4 * q + r) * kP + 16 * c + own] = dw[0][c][r];
+            to[kH * kP + (16 * wave + 4 * q + r) * kP + 16 * c + own] = dw[1][c][r];
+            to[2 * kH * kP + (16 * c + 4 * q + r) * kH + 16 * wave + own] = dw[2][c][r];
         }
 #endif
 }
