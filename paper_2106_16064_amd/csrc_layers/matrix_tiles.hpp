@@ -37,6 +37,19 @@ __device__ __forceinline__ f32x4 multiply<f16_t>(s16x8 a, s16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
 }
 
+// c += a b in place.  The builtin leaves the compiler free to put each result into other registers than c's; with the accumulators
+// filling half of the registers, two thirds of them moved around and others were spilled.
+template <typename E>
+__device__ __forceinline__ void accumulate(s16x8 a, s16x8 b, f32x4& c);
+template <>
+__device__ __forceinline__ void accumulate<bf16_t>(s16x8 a, s16x8 b, f32x4& c) {
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
+}
+template <>
+__device__ __forceinline__ void accumulate<f16_t>(s16x8 a, s16x8 b, f32x4& c) {
+    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
+}
+
 // A matrix of 16-bit elements in memory, or three planes of one.  Address, ld, cols and plane are multiples of 8 elements, ld >= cols,
 // and 256 rows span less than 2^31 bytes.
 struct Source {
@@ -61,6 +74,7 @@ struct TileShape {
     // the first half of a tile's kN rows is of b[0], the second of b[1], for the same kN / 2 columns of two results
     static constexpr bool kDual = kDual_;
     static constexpr int kColumns = kDual ? kN / 2 : kN;
+    static constexpr int kWavesASimd = kM == 64 ? 4 : 2;
 };
 
 // Moves a stage of one operand to LDS: kRows elements along m or n.
@@ -69,59 +83,80 @@ struct Loader {
     static constexpr int kInstructions = kRows * kDepth * 2 / kWaveBytes / kWaves;
     static constexpr int kChunks = kAlongK ? kDepth / 8 : kRows / 8;        // of 16 bytes in a row of LDS
     static constexpr int kRowsEach = 64 / kChunks;                          // rows of LDS per instruction
-    uint32_t offset[kInstructions];
-    int chunk;                                                              // along k
+    // Which chunk a lane takes depends on the instruction in the first or in the second bit of its number, or not at all.
+    static constexpr int kPatternBit = kAlongK || kRows == 64 ? -1 : kRows == 256 ? 0 : 1;
+    static constexpr int kPatterns = kPatternBit < 0 ? 1 : 2;
+    uint32_t offset[kPatterns];             // of the lane in the rows of an instruction
+    int chunk;                              // along k
 
     static __device__ __forceinline__ int exchange(int k) { return ((k & 3) + 4 * ((k >> 3) & 3)) & (kRows / 16 - 1); }
 
-    // `row0`: the first row of LDS that this wave fills, as a row of the source's tile
+    // `row0`: the first row of LDS that this wave fills
     __device__ __forceinline__ void init(int lane, int row0, int64_t ld) {
+        const int row = lane / kChunks, c = lane % kChunks;
 #pragma unroll
-        for (int j = 0; j < kInstructions; ++j) {
-            const int row = row0 + j * kRowsEach + lane / kChunks, c = lane % kChunks;
-            const int from = kAlongK ? c ^ (row & 7) : (((c >> 1) ^ exchange(row)) << 1) + (c & 1);
-            offset[j] = (uint32_t)(row * ld + from * 8) * 2u;
-            chunk = from;
+        for (int p = 0; p < kPatterns; ++p) {
+            const int k = row0 + (kPatternBit > 0 ? p << kPatternBit : p) * kRowsEach + row;
+            chunk = kAlongK ? c ^ (k & 7) : (((c >> 1) ^ exchange(k)) << 1) + (c & 1);
+            offset[p] = (uint32_t)(row * ld + chunk * 8) * 2u;
         }
     }
 
-    // tile origin (row i0 along m or n, k0); `lds`: where the wave's rows begin
-    __device__ __forceinline__ void issue(const Source& s, int plane, int64_t i0, int64_t k0, char* lds) const {
-        const int64_t origin = (kAlongK ? i0 * s.ld + k0 : k0 * s.ld + i0), end = (s.rows - 1) * s.ld + s.cols;
-        const int64_t left = (end - origin) * 2;
-        const uint32_t bytes = left <= 0 ? 0u : left < 0x7fffffff ? (uint32_t)left : 0x7fffffffu;
-        const __amdgpu_buffer_rsrc_t r =
-            __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(s.p + plane * s.plane + origin), 0, bytes, 0x00020000);
-        const bool beyond = kAlongK && k0 + chunk * 8 >= s.cols;            // the next row lies there
+    // Where the wave's rows of a stage begin in the source and how much of it is left there; all lanes alike.
+    struct Cursor {
+        const char* at;
+        int64_t left;           // bytes
+        int depth_left;         // elements of a row, along k
+    };
+    // row i0 along m or n, k0; `row0`: the wave's first row of the tile
+    static __device__ __forceinline__ Cursor begin(const Source& s, int plane, int64_t i0, int64_t k0, int row0) {
+        const int64_t origin = kAlongK ? (i0 + row0) * s.ld + k0 : (k0 + row0) * s.ld + i0, end = (s.rows - 1) * s.ld + s.cols;
+        return {reinterpret_cast<const char*>(s.p + plane * s.plane + origin), (end - origin) * 2, (int)(s.cols - k0)};
+    }
+    // a stage on its way to `lds`, where the wave's rows begin
+    __device__ __forceinline__ void issue(Cursor& c, int64_t ld, char* lds) const {
+        const bool beyond = kAlongK && chunk * 8 >= c.depth_left;           // the next row lies there
+        const char* at = c.at;
+        int64_t left = c.left;
 #pragma unroll
-        for (int j = 0; j < kInstructions; ++j)
+        for (int j = 0; j < kInstructions; ++j) {
+            // in halves, as there are no 64-bit comparisons of scalars
+            const int high = (int)(left >> 32);
+            const uint32_t low = (uint32_t)left, some = high > 0 ? 0x7fffffffu : low < 0x7fffffffu ? low : 0x7fffffffu;
+            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, high < 0 ? 0u : some, 0x00020000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + j * kWaveBytes), 16,
-                                                     beyond ? kNowhere : offset[j], 0, 0, 0);
+                                                     beyond ? kNowhere : offset[kPatternBit < 0 ? 0 : j >> kPatternBit & 1], 0, 0, 0);
+            at += kRowsEach * 2 * ld;
+            left -= kRowsEach * 2 * ld;
+        }
+        const int64_t step = kAlongK ? kDepth * 2 : kDepth * 2 * ld;
+        c.at += step;
+        c.left -= step;
+        c.depth_left -= kDepth;
     }
 };
 
 // Reads fragments of a stage: for 16 elements along m or n and 32 k's, lane l has element l % 16 and k's 8 * (l / 16) ... + 7.
 template <int kRows, bool kAlongK, int kFrags>
 struct Reader {
-    uint32_t at[kAlongK ? 2 : kFrags];
+    uint32_t at;
     __device__ __forceinline__ void init(int lane, int first) {
         if constexpr (kAlongK) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) at[s] = (uint32_t)((first + lane % 16) * (kDepth * 2) + ((s * 4 + lane / 16) ^ (lane & 7)) * 16);
+            at = (uint32_t)((first + lane % 16) * (kDepth * 2) + (lane / 16 ^ (lane & 7)) * 16);
         } else {
             const int k = lane / 16 * 8 + lane % 16 / 4;
-#pragma unroll
-            for (int i = 0; i < kFrags; ++i)
-                at[i] = (uint32_t)(k * kRows * 2 + (((first / 16 + i) ^ Loader<kRows, false, 1>::exchange(k)) * 32) + (lane & 3) * 8);
+            at = (uint32_t)(k * kRows * 2 + ((first / 16 ^ Loader<kRows, false, 1>::exchange(k)) * 32) + (lane & 3) * 8);
         }
     }
+    // half s of the stage, 16 elements i; `first` is a multiple of 16 kFrags, so that the chunks' exchanges are those of `at`
     template <typename Lds>
     __device__ __forceinline__ s16x8 read(Lds* lds, int s, int i) const {
         if constexpr (kAlongK) {
-            return *reinterpret_cast<const s16x8*>(lds + at[s] + i * 16 * kDepth * 2);
+            return *reinterpret_cast<const s16x8*>(lds + (at ^ (s * 64)) + i * 16 * kDepth * 2);
         } else {
+            static_assert((kFrags & (kFrags - 1)) == 0);
             using P = __attribute__((address_space(3))) s16x4*;
-            auto* p = lds + at[i] + s * 32 * kRows * 2;
+            auto* p = lds + (at ^ (i * 32)) + s * 32 * kRows * 2;
             const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p);
             const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 4 * kRows * 2));
             return __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -188,69 +223,105 @@ struct TileProduct {
 #pragma unroll
             for (int i = 0; i < Shape::kFragsM; ++i) acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-        const int64_t steps = k_end > k_first ? (k_end - k_first + kDepth - 1) / kDepth : 0;
-        const int products = args.planes == 3 ? 6 : 1;
-        const int64_t total = steps * products * args.pairs;
+        const int steps = k_end > k_first ? (int)((k_end - k_first + kDepth - 1) / kDepth) : 0;
+        const int products = args.planes == 3 ? 6 : 1, total = steps * products * args.pairs;
+        if (total == 0) return;
         // products of planes (1,1) (0,2) (2,0) (0,1) (1,0) (0,0), two bits each
         constexpr uint32_t kPlanesA = 1u | 0u << 2 | 2u << 4 | 0u << 6 | 1u << 8 | 0u << 10;
         constexpr uint32_t kPlanesB = 1u | 2u << 2 | 0u << 4 | 1u << 6 | 0u << 8 | 0u << 10;
-        int pair = 0, product = 0;
-        int64_t k = k_first;
-        a_loader.init(lane, wave * kARowsEach, args.a[args.batch > 1 ? tile.batch : 0].ld);
-        b_loader.init(lane, b_wave * kBRowsEach, args.b[side].ld);
+        const int64_t a_ld = args.a[args.batch > 1 ? tile.batch : 0].ld, b_ld = args.b[side].ld;
+        a_loader.init(lane, wave * kARowsEach, a_ld);
+        b_loader.init(lane, b_wave * kBRowsEach, b_ld);
 
+        // stages are loaded in order: along the depth, then the next product of planes, then the next pair
+        int pair = 0, product = 0;
+        int stages_left = steps;
+        typename ALoader::Cursor a_at;
+        typename BLoader::Cursor b_at;
+        auto enter = [&] {
+            a_at = ALoader::begin(args.a[args.batch > 1 ? tile.batch : pair], args.planes == 3 ? (kPlanesA >> (2 * product)) & 3 : 0, i0, k_first, wave * kARowsEach);
+            b_at = BLoader::begin(args.b[Shape::kDual ? side : pair], args.planes == 3 ? (kPlanesB >> (2 * product)) & 3 : 0, j0, k_first, b_wave * kBRowsEach);
+        };
+        enter();
         auto load = [&](char* lds) {
-            const int plane_a = args.planes == 3 ? (kPlanesA >> (2 * product)) & 3 : 0, plane_b = args.planes == 3 ? (kPlanesB >> (2 * product)) & 3 : 0;
-            a_loader.issue(args.a[args.batch > 1 ? tile.batch : pair], plane_a, i0, k, lds + a_lds);
-            b_loader.issue(args.b[Shape::kDual ? side : pair], plane_b, j0, k, lds + b_lds);
-            k += kDepth;
-            if (k >= k_end) {
-                k = k_first;
+            if (stages_left == 0) {
                 if (++product == products) {
                     product = 0;
                     ++pair;
                 }
+                stages_left = steps;
+                enter();
+            }
+            --stages_left;
+            a_loader.issue(a_at, a_ld, lds + a_lds);
+            b_loader.issue(b_at, b_ld, lds + b_lds);
+        };
+        auto read_b = [&](const char* lds, int s, s16x8 (&f)[Shape::kFragsN]) {
+#pragma unroll
+            for (int j = 0; j < Shape::kFragsN; ++j) {
+                constexpr int kEach = Shape::kDual ? Shape::kFragsN / 2 : Shape::kFragsN;
+                f[j] = b_reader.read(lds + kABytes + j / kEach * (kBBytes / 2), s, j % kEach);     // the second half's rows lie kN / 2 rows on
             }
         };
-        auto compute = [&](const char* lds) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                s16x8 fa[Shape::kFragsM], fb[Shape::kFragsN];
-#pragma unroll
-                for (int i = 0; i < Shape::kFragsM; ++i) fa[i] = a_reader.read(lds, s, i);
-#pragma unroll
-                for (int j = 0; j < Shape::kFragsN; ++j) {
-                    constexpr int kEach = Shape::kDual ? Shape::kFragsN / 2 : Shape::kFragsN;
-                    const int half = j / kEach;                             // the second half's rows lie kN / 2 rows on
-                    fb[j] = b_reader.read(lds + kABytes + half * (kBBytes / 2), s, j % kEach);
-                }
-#pragma unroll
-                for (int j = 0; j < Shape::kFragsN; ++j)
-#pragma unroll
-                    for (int i = 0; i < Shape::kFragsM; ++i) acc[j][i] = multiply<E>(fb[j], fa[i], acc[j][i]);
-                __builtin_amdgcn_sched_barrier(0);      // the other half's fragments would not fit the registers
-            }
-        };
-        // what a wave has asked for has arrived, and all waves are here
+        // what this wave has asked for has arrived, and all waves are here
         auto arrive = [&] {
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
-        if (total > 0) load(first);
-        int64_t step = 0;
+        // A fragment of A is multiplied by all of B's and makes room for the one of the next half stage at once; B's have a second place.
+        // A little into the second half all waves have read the whole stage and the next one has arrived: from there on fragments are of
+        // the next one, and this one's buffer takes the one after that, which has a whole stage's time on its way.
+        constexpr int kEarly = Shape::kFragsM >= 8 ? 2 : 1;
+        s16x8 a[Shape::kFragsM], b_low[Shape::kFragsN], b_high[Shape::kFragsN];
+        auto multiply_row = [&](int i, const s16x8 (&b)[Shape::kFragsN]) {
+#pragma unroll
+            for (int j = 0; j < Shape::kFragsN; ++j) accumulate<E>(b[j], a[i], acc[j][i]);
+        };
+        load(first);
+        arrive();
+        if (total > 1) load(second);
+        read_b(first, 0, b_low);
+#pragma unroll
+        for (int i = 0; i < Shape::kFragsM; ++i) a[i] = a_reader.read(first, 0, i);
+        auto stage = [&](char* here, char* other, bool more) {
+            read_b(here, 1, b_high);
+#pragma unroll
+            for (int i = 0; i < Shape::kFragsM; ++i) {
+                multiply_row(i, b_low);
+                a[i] = a_reader.read(here, 1, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < kEarly; ++i) multiply_row(i, b_high);
+            __builtin_amdgcn_sched_barrier(0);
+            arrive();
+            if (more) load(here);
+            read_b(other, 0, b_low);
+#pragma unroll
+            for (int i = 0; i < kEarly; ++i) a[i] = a_reader.read(other, 0, i);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = kEarly; i < Shape::kFragsM; ++i) {
+                multiply_row(i, b_high);
+                a[i] = a_reader.read(other, 0, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        int step = 0;
         for (; step + 2 <= total; step += 2) {
-            arrive();
-            load(second);
-            compute(first);
-            arrive();
-            if (step + 2 < total) load(first);
-            compute(second);
+            stage(first, second, step + 2 < total);
+            stage(second, first, step + 3 < total);
         }
-        if (step < total) {
-            arrive();
-            compute(first);
-        }
+        if (step < total) stage(first, second, false);
+        // other instructions may read a result 11 cycles after its matrix instruction has begun; the compiler does not see these
+#pragma unroll
+        for (int i = 0; i < Shape::kFragsM; ++i)
+#pragma unroll
+            for (int j = 0; j < Shape::kFragsN; ++j) {
+                if (i == 0 && j == 0) asm volatile("s_nop 15\n\ts_nop 15" : "+v"(acc[0][0]));
+                asm volatile("" : "+v"(acc[j][i]));
+            }
     }
 
     // hands the elements to out.store(args, tile, m, n, four neighbours along n), or out.store(..., four of each result) of a dual tile
@@ -273,9 +344,9 @@ struct TileProduct {
     }
 };
 
-// A workgroup per tile.  Two waves a SIMD, or four where tiles are small.
+// A workgroup per tile.
 template <typename E, typename Shape, bool kARows, bool kBRows, typename Out>
-__global__ __launch_bounds__(Shape::kThreads, Shape::kM == 64 ? 4 : 2) void tile_kernel(ProductArgs args, Out out) {
+__global__ __launch_bounds__(Shape::kThreads, Shape::kWavesASimd) void tile_kernel(ProductArgs args, Out out) {
 #if defined(__HIP_DEVICE_COMPILE__)         // the host's half knows neither buffers nor matrix instructions
     const TileIndex tile = tile_of(args);
     TileProduct<E, Shape, kARows, kBRows> product;
