@@ -245,7 +245,7 @@ extern "C" int dgsp_gated_ff(int64_t rows, int64_t width, int64_t hidden, int64_
         args.a[0] = source<T, E>(x, rows, width, ldx, at.x, on);
         args.b[0] = source<T, E>(w_gate, hidden, width, ldg, at.gate, on);
         args.b[1] = source<T, E>(w_up, hidden, width, ldu, at.up_weight, on);
-        launch<E, true, true, true>(at.up, args, GatedUpOut<E>{h, saved ? static_cast<float*>(keep.act) : nullptr, saved ? static_cast<float*>(keep.mul) : nullptr,
+        launch<E, true, true, true>(at.up, args, GatedUpOut<E, sizeof(T) == 2>{h, saved ? static_cast<float*>(keep.act) : nullptr, saved ? static_cast<float*>(keep.mul) : nullptr,
                                                                activation}, on);
         args = product_args(at.down, rows, out_width, hidden, planes, 1);
         args.a[0] = source(h, rows);

@@ -73,9 +73,9 @@ struct Planes {
     E* p;
     int64_t ld, plane;          // plane 0: one plane
     // four neighbours
-    __device__ __forceinline__ void store(int64_t row, int64_t col, f32x4 v) const {
+    __device__ __forceinline__ void store(int64_t at, f32x4 v) const {
         using E4 = E __attribute__((ext_vector_type(4)));
-        E* to = p + row * ld + col;
+        E* to = p + at;
         if (plane) {
             if constexpr (sizeof(E) == 2 && !__is_same(E, f16_t)) {
                 E4 out[3];
@@ -124,26 +124,40 @@ __global__ void lay_out_kernel(int64_t rows, int64_t cols, const T* from, int64_
 
 // h = act(g) u, and for the backward pass act(g) and u act'(g), which it multiplies by dh.  These two are kept in 32 bits: rounded to
 // 16 they would double the squared error of the gates' gradients, and the 8 bytes an element cost 3 % of a large block's step.
-template <typename E>
+// kShort: of a 16-bit type.
+template <typename E, bool kShort>
 struct GatedUpOut {
     Planes<E> h;
     float *act, *mul;           // null: not wanted
     int activation;
-    __device__ __forceinline__ void store(const ProductArgs& args, const TileIndex&, int64_t m, int64_t n, f32x4 g, f32x4 u) const {
-        if (m >= args.m || n >= h.ld) return;
-        f32x4 value, slope;
+    template <int kEach>
+    __device__ __forceinline__ Nothing ask(const ProductArgs&, int64_t, int64_t) const {
+        return {};
+    }
+    template <int kEach>
+    __device__ __forceinline__ void row(const ProductArgs& args, const TileIndex&, int64_t m, int64_t n, Nothing, const f32x4 (&v)[kEach][2]) const {
+        if (m >= args.m) return;
+        float g[4 * kEach], value[4 * kEach], slope[4 * kEach];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float v, s;
-            activate(activation, g[r], v, s);
-            value[r] = v;
-            slope[r] = s;
+        for (int i = 0; i < 4 * kEach; ++i) g[i] = v[i / 4][0][i % 4];
+        if constexpr (kShort) {
+            activate_short(activation, g, value, slope);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4 * kEach; ++i) activate(activation, g[i], value[i], slope[i]);
         }
-        if (act) {
-            *reinterpret_cast<f32x4*>(act + m * h.ld + n) = value;
-            *reinterpret_cast<f32x4*>(mul + m * h.ld + n) = slope * u;
+        const int64_t at = m * h.ld + n;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            if (n + 16 * j >= h.ld) break;
+            const f32x4 a = {value[4 * j], value[4 * j + 1], value[4 * j + 2], value[4 * j + 3]};
+            const f32x4 b = {slope[4 * j], slope[4 * j + 1], slope[4 * j + 2], slope[4 * j + 3]};
+            if (act) {
+                *reinterpret_cast<f32x4*>(act + at + 16 * j) = a;
+                *reinterpret_cast<f32x4*>(mul + at + 16 * j) = b * v[j][1];
+            }
+            h.store(at + 16 * j, a * v[j][1]);
         }
-        h.store(m, n, value * u);
     }
 };
 
@@ -152,17 +166,40 @@ template <typename E>
 struct GatedSlopeOut {
     const float *act, *mul;
     Planes<E> dg, du;
-    __device__ __forceinline__ void store(const ProductArgs& args, const TileIndex&, int64_t m, int64_t n, f32x4 dh) const {
-        if (m >= args.m || n >= dg.ld) return;
-        const f32x4 a = *reinterpret_cast<const f32x4*>(act + m * dg.ld + n), b = *reinterpret_cast<const f32x4*>(mul + m * dg.ld + n);
-        f32x4 g, u;
+    template <int kEach>
+    struct Kept {
+        f32x4 act[kEach], mul[kEach];
+    };
+    template <int kEach>
+    __device__ __forceinline__ Kept<kEach> ask(const ProductArgs& args, int64_t m, int64_t n) const {
+        Kept<kEach> out;
+        const int64_t at = m * dg.ld + n;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {                   // beyond the hidden width a transposed operand holds whatever lies there
-            g[r] = n + r < args.n ? dh[r] * b[r] : 0.0f;
-            u[r] = n + r < args.n ? dh[r] * a[r] : 0.0f;
+        for (int j = 0; j < kEach; ++j) {
+            const bool inside = m < args.m && n + 16 * j < dg.ld;
+            out.act[j] = inside ? *reinterpret_cast<const f32x4*>(act + at + 16 * j) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            out.mul[j] = inside ? *reinterpret_cast<const f32x4*>(mul + at + 16 * j) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        dg.store(m, n, g);
-        du.store(m, n, u);
+        return out;
+    }
+    template <int kEach>
+    __device__ __forceinline__ void row(const ProductArgs& args, const TileIndex&, int64_t m, int64_t n, const Kept<kEach>& kept,
+                                        const f32x4 (&v)[kEach][1]) const {
+        if (m >= args.m) return;
+        const int64_t at = m * dg.ld + n;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            if (n + 16 * j >= dg.ld) break;
+            f32x4 g, u;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {               // beyond the hidden width a transposed operand holds whatever lies there
+                const bool inside = n + 16 * j + r < args.n;
+                g[r] = inside ? v[j][0][r] * kept.mul[j][r] : 0.0f;
+                u[r] = inside ? v[j][0][r] * kept.act[j][r] : 0.0f;
+            }
+            dg.store(at + 16 * j, g);
+            du.store(at + 16 * j, u);
+        }
     }
 };
 
@@ -172,21 +209,30 @@ struct ProductOut {
     int64_t ld;
     bool vectors;               // four neighbours may be written at once
     float* partial;             // not null: split results, [split][batch][m][n padded to 4]
-    __device__ __forceinline__ void store(const ProductArgs& args, const TileIndex& tile, int64_t m, int64_t n, f32x4 v) const {
+    template <int kEach>
+    __device__ __forceinline__ Nothing ask(const ProductArgs&, int64_t, int64_t) const {
+        return {};
+    }
+    template <int kEach>
+    __device__ __forceinline__ void row(const ProductArgs& args, const TileIndex& tile, int64_t m, int64_t n, Nothing, const f32x4 (&v)[kEach][1]) const {
         using T4 = T __attribute__((ext_vector_type(4)));
-        if (m >= args.m || n >= args.n) return;
-        if (partial) {
-            const int64_t padded = (args.n + 3) / 4 * 4;
-            *reinterpret_cast<f32x4*>(partial + (((int64_t)tile.split * args.batch + tile.batch) * args.m + m) * padded + n) = v;
-            return;
-        }
-        T* to = c[tile.batch] + m * ld + n;
-        if (vectors && n + 4 <= args.n) {
-            *reinterpret_cast<T4*>(to) = T4{from_float<T>(v[0]), from_float<T>(v[1]), from_float<T>(v[2]), from_float<T>(v[3])};
-        } else {
+        if (m >= args.m) return;
+        const int64_t padded = (args.n + 3) / 4 * 4;
+        float* split = partial ? partial + (((int64_t)tile.split * args.batch + tile.batch) * args.m + m) * padded + n : nullptr;
+        T* to = (tile.batch ? c[1] : c[0]) + m * ld + n;
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (n + r < args.n) to[r] = from_float<T>(v[r]);
+        for (int j = 0; j < kEach; ++j) {
+            const f32x4 x = v[j][0];
+            if (n + 16 * j >= args.n) break;
+            if (partial) {
+                *reinterpret_cast<f32x4*>(split + 16 * j) = x;
+            } else if (vectors && n + 16 * j + 4 <= args.n) {
+                *reinterpret_cast<T4*>(to + 16 * j) = T4{from_float<T>(x[0]), from_float<T>(x[1]), from_float<T>(x[2]), from_float<T>(x[3])};
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (n + 16 * j + r < args.n) to[16 * j + r] = from_float<T>(x[r]);
+            }
         }
     }
 };

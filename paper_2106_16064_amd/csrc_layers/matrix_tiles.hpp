@@ -324,25 +324,32 @@ struct TileProduct {
             }
     }
 
-    // hands the elements to out.store(args, tile, m, n, four neighbours along n), or out.store(..., four of each result) of a dual tile
+    // Hands the results to out.row(args, tile, m, n, more, v[j][...]), a row of fragments at a time: element m and, for fragment j, four
+    // elements from n + 16 j on; of a dual tile v[j][0] and v[j][1] are of the two results.  `more` is what out.ask(args, m, n) gave for
+    // them a row earlier.
     template <typename Out>
     __device__ __forceinline__ void store(const ProductArgs& args, const TileIndex& tile, const Out& out) {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int wave_m = wave / Shape::kWavesN, wave_n = wave % Shape::kWavesN;
-        constexpr int kEach = Shape::kDual ? Shape::kFragsN / 2 : Shape::kFragsN;
+        constexpr int kEach = Shape::kDual ? Shape::kFragsN / 2 : Shape::kFragsN, kResults = Shape::kDual ? 2 : 1;
+        const int64_t m = tile.m * Shape::kM + wave_m * Shape::kFragsM * 16 + lane % 16;
+        const int64_t n = tile.n * Shape::kColumns + wave_n * kEach * 16 + lane / 16 * 4;
+        auto more = out.template ask<kEach>(args, m, n);
 #pragma unroll
-        for (int i = 0; i < Shape::kFragsM; ++i)
+        for (int i = 0; i < Shape::kFragsM; ++i) {
+            const auto have = more;
+            if (i + 1 < Shape::kFragsM) more = out.template ask<kEach>(args, m + 16 * (i + 1), n);
+            f32x4 v[kEach][kResults];
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) {
-                const int64_t m = tile.m * Shape::kM + (wave_m * Shape::kFragsM + i) * 16 + lane % 16;
-                const int64_t n = tile.n * Shape::kColumns + (wave_n * kEach + j) * 16 + lane / 16 * 4;
-                if constexpr (Shape::kDual)
-                    out.store(args, tile, m, n, acc[j][i], acc[j + kEach][i]);
-                else
-                    out.store(args, tile, m, n, acc[j][i]);
-            }
+            for (int j = 0; j < kEach; ++j)
+#pragma unroll
+                for (int r = 0; r < kResults; ++r) v[j][r] = acc[j + r * kEach][i];
+            out.row(args, tile, m + 16 * i, n, have, v);
+        }
     }
 };
+
+struct Nothing {};
 
 // A workgroup per tile.
 template <typename E, typename Shape, bool kARows, bool kBRows, typename Out>
