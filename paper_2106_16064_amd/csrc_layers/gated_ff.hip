@@ -53,20 +53,25 @@ struct Cut {
 
 constexpr int64_t kCus = 256;
 
-// The largest tiles of which there is one for every CU: a tile of 256 x 256 reads half as much per product as one of 128 x 128.  Where
-// even the small ones are fewer and the depth allows it, the depth is split, to two workgroups a CU of at least 512 each.
-Cut cut(int64_t m, int64_t n, int64_t depth, int batch, bool dual, bool may_split) {
+// Which tiles.  256 x 256 read half as much per product as 128 x 128, but take a CU each, so that nothing runs while their results leave:
+// they pay where the sum is long (1024 at least, counting pairs and products of planes), there is one for every CU, and the edges
+// waste little.  (2^16 x 512 of depth 128 in float, 768 in all: 284 us, with 128 x 128 230 us; 8192 x 16384 of depth 4096: 1.24 ms
+// against 1.6.)  64 x 64 are for what has fewer than a tile of 128 for every CU and cannot be split along the depth, or is hardly half
+// as wide.  Where tiles are fewer than CUs the depth is split, to two workgroups a CU of at least 512 each.
+Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, bool dual, bool may_split) {
+    auto tiles = [&](int size) { return ceil_div(m, size) * ceil_div(n, dual ? size / 2 : size) * batch; };
+    const bool splits = may_split && depth >= 1024;
     Cut c{kSmall, 0, 0, 1, padded(std::max<int64_t>(depth, 1), kDepth)};
-    for (int size : {kLarge, kMiddle, kSmall}) {
-        c.size = size;
-        c.tiles_m = ceil_div(m, size);
-        c.tiles_n = ceil_div(n, dual ? size / 2 : size);
-        if (c.tiles_m * c.tiles_n * batch >= kCus) break;
-    }
-    const int64_t tiles = c.tiles_m * c.tiles_n * batch;
-    if (may_split && tiles < kCus && depth >= 1024) {
-        const int64_t splits = std::min<int64_t>(ceil_div(2 * kCus, tiles), depth / 512);
-        c.split_depth = padded(ceil_div(depth, splits), kDepth);
+    if (tiles(kLarge) >= kCus && depth * terms >= 1024 && 4 * tiles(kLarge) <= tiles(kMiddle) + tiles(kMiddle) / 8)
+        c.size = kLarge;
+    else if ((tiles(kMiddle) >= kCus || splits) && 2 * (4 * tiles(kMiddle)) <= 3 * tiles(kSmall))
+        c.size = kMiddle;
+    c.tiles_m = ceil_div(m, c.size);
+    c.tiles_n = ceil_div(n, dual ? c.size / 2 : c.size);
+    const int64_t count = tiles(c.size);
+    if (splits && count < kCus) {
+        const int64_t most = std::min<int64_t>(ceil_div(2 * kCus, count), depth / 512);
+        c.split_depth = padded(ceil_div(depth, most), kDepth);
         c.splits = (int)ceil_div(depth, c.split_depth);
     }
     return c;
@@ -134,16 +139,34 @@ bool in_place(const void* p, int64_t rows, int64_t cols, int64_t ld) {
     return sizeof(T) == 2 && cols % 8 == 0 && (rows == 1 || (ld % 8 == 0 && ld >= cols && ld <= kMostWidth)) && aligned(p, 16);
 }
 
-// The matrix as the products read it: in place where it can be (unless `copy`), else laid out in `piece`.
+// The matrices of a call as its products read them: in place where they can be, else laid out in a piece of memory, all in one launch
+// that has to come before the products'.
 template <typename T, typename E>
-Source source(const void* p, int64_t rows, int64_t cols, int64_t ld, void* piece, hipStream_t stream, bool copy = false) {
-    if (in_place<T>(p, rows, cols, ld) && !copy) return {static_cast<const uint16_t*>(p), rows, cols, rows == 1 ? cols : ld, 0};
-    const int64_t to_ld = padded(cols, 8), plane = rows * to_ld;
-    if (rows > 0)
-        lay_out_kernel<T, E><<<(unsigned)std::min<int64_t>(ceil_div(plane / 8, 256), 1 << 16), 256, 0, stream>>>(
-            rows, cols, static_cast<const T*>(p), ld, static_cast<E*>(piece), to_ld, plane);
-    return {static_cast<const uint16_t*>(piece), rows, to_ld, to_ld, sizeof(T) == 4 ? plane : 0};
-}
+class Operands {
+public:
+    Source add(const void* p, int64_t rows, int64_t cols, int64_t ld, void* piece, bool copy = false) {
+        if (in_place<T>(p, rows, cols, ld) && !copy) return {static_cast<const uint16_t*>(p), rows, cols, rows == 1 ? cols : ld, 0};
+        const int64_t to_ld = padded(cols, 8), chunks = rows * to_ld / 8;
+        if (rows > 0) {
+            const auto groups = (unsigned)std::min<int64_t>(ceil_div(chunks, 256), 1 << 14);
+            all_.each[all_.count++] = {static_cast<const T*>(p), rows, cols, ld, static_cast<E*>(piece), to_ld, groups};
+            groups_ += groups;
+        }
+        return laid_out(piece, rows, cols);
+    }
+    // what an earlier call has laid out there
+    static Source laid_out(const void* piece, int64_t rows, int64_t cols) {
+        const int64_t ld = padded(cols, 8);
+        return {static_cast<const uint16_t*>(piece), rows, ld, ld, sizeof(T) == 4 ? rows * ld : 0};
+    }
+    void launch(hipStream_t stream) const {
+        if (all_.count) lay_out_kernel<T, E><<<groups_, 256, 0, stream>>>(all_);
+    }
+
+private:
+    Layouts<T, E> all_{};
+    unsigned groups_ = 0;
+};
 
 template <typename E>
 Source source(const Planes<E>& planes, int64_t rows) {
@@ -156,36 +179,48 @@ Planes<E> hidden_planes(void* p, int64_t rows, int64_t hidden) {
     return {static_cast<E*>(p), ld, sizeof(T) == 4 ? rows * ld : 0};
 }
 
-// what the forward pass leaves: act(g) and u act'(g) in 32 bits, and h
+// What the forward pass leaves: act(g) and u act'(g) in 32 bits, h, and of float matrices the planes that it has laid out.
 struct Saved {
-    void *act, *mul, *h;
-    Saved(Pieces& pieces, int64_t rows, int64_t hidden, int type)
+    void *act, *mul, *h, *x = nullptr, *gate = nullptr, *up = nullptr, *down = nullptr;
+    Saved(Pieces& pieces, int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type)
         : act(pieces.take(rows * padded(hidden, 8) * 4)), mul(pieces.take(rows * padded(hidden, 8) * 4)),
-          h(pieces.take(laid_out_bytes(rows, hidden, type))) {}
+          h(pieces.take(laid_out_bytes(rows, hidden, type))) {
+        if (type != DGSP_F32) return;
+        x = pieces.take(laid_out_bytes(rows, width, type));
+        gate = pieces.take(laid_out_bytes(hidden, width, type));
+        up = pieces.take(laid_out_bytes(hidden, width, type));
+        down = pieces.take(laid_out_bytes(out_width, hidden, type));
+    }
 };
+
+int terms_of(int type) { return type == DGSP_F32 ? 6 : 1; }
 
 struct ForwardPieces {
     Cut up, down;
     void *x, *gate, *up_weight, *down_weight, *h, *partial;
-    ForwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type, bool saved)
-        : up(cut(rows, hidden, width, 1, true, false)), down(cut(rows, out_width, hidden, 1, false, true)),
+    ForwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type)
+        : up(cut(rows, hidden, width, terms_of(type), 1, true, false)), down(cut(rows, out_width, hidden, terms_of(type), 1, false, true)),
           x(pieces.take(laid_out_bytes(rows, width, type))), gate(pieces.take(laid_out_bytes(hidden, width, type))),
           up_weight(pieces.take(laid_out_bytes(hidden, width, type))), down_weight(pieces.take(laid_out_bytes(out_width, hidden, type))),
-          h(saved ? nullptr : pieces.take(laid_out_bytes(rows, hidden, type))), partial(pieces.take(partial_bytes(down, rows, out_width, 1))) {}
+          h(pieces.take(laid_out_bytes(rows, hidden, type))), partial(pieces.take(partial_bytes(down, rows, out_width, 1))) {}
 };
 
 struct BackwardPieces {
     Cut slope, dx, gates, down;
-    void *x, *gate, *up_weight, *down_weight, *dy, *dg, *du, *partial;
+    void *x = nullptr, *gate = nullptr, *up_weight = nullptr, *down_weight = nullptr, *dy, *dg, *du, *partial;
     BackwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type, int batch)
-        : slope(cut(rows, hidden, out_width, 1, false, false)), dx(cut(rows, width, hidden, 1, false, true)),
-          gates(cut(hidden, width, rows, batch, false, true)), down(cut(out_width, hidden, rows, 1, false, true)),
-          x(pieces.take(laid_out_bytes(rows, width, type))), gate(pieces.take(laid_out_bytes(hidden, width, type))),
-          up_weight(pieces.take(laid_out_bytes(hidden, width, type))), down_weight(pieces.take(laid_out_bytes(out_width, hidden, type))),
+        : slope(cut(rows, hidden, out_width, terms_of(type), 1, false, false)), dx(cut(rows, width, hidden, 2 * terms_of(type), 1, false, true)),
+          gates(cut(hidden, width, rows, terms_of(type), batch, false, true)), down(cut(out_width, hidden, rows, terms_of(type), 1, false, true)),
           dy(pieces.take(laid_out_bytes(rows, out_width, type))), dg(pieces.take(laid_out_bytes(rows, hidden, type))),
           du(pieces.take(laid_out_bytes(rows, hidden, type))),
           partial(pieces.take(std::max({partial_bytes(dx, rows, width, 1), partial_bytes(gates, hidden, width, batch),
-                                        partial_bytes(down, out_width, hidden, 1)}))) {}
+                                        partial_bytes(down, out_width, hidden, 1)}))) {
+        if (type == DGSP_F32) return;
+        x = pieces.take(laid_out_bytes(rows, width, type));
+        gate = pieces.take(laid_out_bytes(hidden, width, type));
+        up_weight = pieces.take(laid_out_bytes(hidden, width, type));
+        down_weight = pieces.take(laid_out_bytes(out_width, hidden, type));
+    }
 };
 
 template <typename F>
@@ -200,14 +235,14 @@ int with_elements(int type, F&& f) {
 extern "C" int64_t dgsp_gated_ff_saved_bytes(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type) {
     if (!gated_extents(rows, width, hidden, out_width, type) || narrow_fits(width, hidden, out_width, type)) return 0;
     Pieces pieces(nullptr);
-    Saved saved(pieces, rows, hidden, type);
+    Saved saved(pieces, rows, width, hidden, out_width, type);
     return pieces.used();
 }
 
 extern "C" int64_t dgsp_gated_ff_workspace_bytes(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type) {
     if (!gated_extents(rows, width, hidden, out_width, type) || narrow_fits(width, hidden, out_width, type)) return 0;
     Pieces pieces(nullptr);
-    ForwardPieces need(pieces, rows, width, hidden, out_width, type, false);
+    ForwardPieces need(pieces, rows, width, hidden, out_width, type);
     return pieces.used();
 }
 
@@ -232,8 +267,8 @@ extern "C" int dgsp_gated_ff(int64_t rows, int64_t width, int64_t hidden, int64_
     if (narrow_fits(width, hidden, out_width, type))
         return narrow_forward({rows, width, hidden, out_width, type, activation, x, ldx, w_gate, ldg, w_up, ldu, w_down, ldd, y, ldy}, stream);
     Pieces pieces(workspace), kept(saved);
-    const ForwardPieces at(pieces, rows, width, hidden, out_width, type, saved != nullptr);
-    const Saved keep(kept, rows, hidden, type);
+    const ForwardPieces at(pieces, rows, width, hidden, out_width, type);
+    const Saved keep(kept, rows, width, hidden, out_width, type);
     if (!launchable(at.up, 1) || !launchable(at.down, 1)) return DGSP_ERR_UNSUPPORTED;
     return with_elements(type, [&](auto t, auto e) {
         using T = decltype(t);
@@ -241,16 +276,18 @@ extern "C" int dgsp_gated_ff(int64_t rows, int64_t width, int64_t hidden, int64_
         const auto on = static_cast<hipStream_t>(stream);
         const int planes = planes_of(type);
         const Planes<E> h = hidden_planes<T, E>(saved ? keep.h : at.h, rows, hidden);
-        ProductArgs args = product_args(at.up, rows, hidden, width, planes, 1);
-        args.a[0] = source<T, E>(x, rows, width, ldx, at.x, on);
-        args.b[0] = source<T, E>(w_gate, hidden, width, ldg, at.gate, on);
-        args.b[1] = source<T, E>(w_up, hidden, width, ldu, at.up_weight, on);
-        launch<E, true, true, true>(at.up, args, GatedUpOut<E, sizeof(T) == 2>{h, saved ? static_cast<float*>(keep.act) : nullptr, saved ? static_cast<float*>(keep.mul) : nullptr,
+        const bool planes_kept = saved && type == DGSP_F32;
+        Operands<T, E> operands;
+        ProductArgs args = product_args(at.up, rows, hidden, width, planes, 1), down = product_args(at.down, rows, out_width, hidden, planes, 1);
+        args.a[0] = operands.add(x, rows, width, ldx, planes_kept ? keep.x : at.x);
+        args.b[0] = operands.add(w_gate, hidden, width, ldg, planes_kept ? keep.gate : at.gate);
+        args.b[1] = operands.add(w_up, hidden, width, ldu, planes_kept ? keep.up : at.up_weight);
+        down.a[0] = source(h, rows);
+        down.b[0] = operands.add(w_down, out_width, hidden, ldd, planes_kept ? keep.down : at.down_weight);
+        operands.launch(on);
+        launch<E, true, true, true>(at.up, args, GatedUpOut<E, sizeof(T) == 4>{h, saved ? static_cast<float*>(keep.act) : nullptr, saved ? static_cast<float*>(keep.mul) : nullptr,
                                                                activation}, on);
-        args = product_args(at.down, rows, out_width, hidden, planes, 1);
-        args.a[0] = source(h, rows);
-        args.b[0] = source<T, E>(w_down, out_width, hidden, ldd, at.down_weight, on);
-        product<T, E, true, true>(at.down, args, {{static_cast<T*>(y), nullptr}, ldy, false, nullptr}, at.partial, on);
+        product<T, E, true, true>(at.down, down, {{static_cast<T*>(y), nullptr}, ldy, false, nullptr}, at.partial, on);
         return launched();
     });
 }
@@ -273,7 +310,7 @@ extern "C" int dgsp_gated_ff_backward(int64_t rows, int64_t width, int64_t hidde
     const int batch = dw_gate && dw_up ? 2 : 1;
     Pieces pieces(workspace), kept(const_cast<void*>(saved));
     const BackwardPieces at(pieces, rows, width, hidden, out_width, type, batch);
-    const Saved keep(kept, rows, hidden, type);
+    const Saved keep(kept, rows, width, hidden, out_width, type);
     if (!launchable(at.slope, 1) || !launchable(at.dx, 1) || !launchable(at.gates, batch) || !launchable(at.down, 1))
         return DGSP_ERR_UNSUPPORTED;
     return with_elements(type, [&](auto t, auto e) {
@@ -281,14 +318,28 @@ extern "C" int dgsp_gated_ff_backward(int64_t rows, int64_t width, int64_t hidde
         using E = decltype(e);
         const auto on = static_cast<hipStream_t>(stream);
         const int planes = planes_of(type);
-        const bool gates = dx || dw_gate || dw_up;
-        const Source grad = source<T, E>(dy, rows, out_width, lddy, at.dy, on);
+        const bool gates = (dx || dw_gate || dw_up) && rows > 0;
+        Operands<T, E> operands;
+        // of float matrices the forward pass has left the planes; weights of a pair have to lie alike
+        auto operand = [&](const void* p, int64_t count, int64_t cols, int64_t ld, const void* planes_kept, void* piece, bool copy = false) {
+            return type == DGSP_F32 ? Operands<T, E>::laid_out(planes_kept, count, cols) : operands.add(p, count, cols, ld, piece, copy);
+        };
+        const bool alike = ldg == ldu && in_place<T>(w_gate, hidden, width, ldg) && in_place<T>(w_up, hidden, width, ldu);
+        const Source grad = operands.add(dy, rows, out_width, lddy, at.dy);
+        Source in{}, gate{}, up{}, down{};
+        if (dw_gate || dw_up) in = operand(x, rows, width, ldx, keep.x, at.x);
+        if (dx) {
+            gate = operand(w_gate, hidden, width, ldg, keep.gate, at.gate, !alike);
+            up = operand(w_up, hidden, width, ldu, keep.up, at.up_weight, !alike);
+        }
+        if (gates) down = operand(w_down, out_width, hidden, ldd, keep.down, at.down_weight);
+        operands.launch(on);
         const Planes<E> dg = hidden_planes<T, E>(at.dg, rows, hidden), du = hidden_planes<T, E>(at.du, rows, hidden);
         ProductArgs args;
-        if (gates && rows > 0) {
+        if (gates) {
             args = product_args(at.slope, rows, hidden, out_width, planes, 1);
             args.a[0] = grad;
-            args.b[0] = source<T, E>(w_down, out_width, hidden, ldd, at.down_weight, on);
+            args.b[0] = down;
             launch<E, false, true, false>(at.slope, args,
                                           GatedSlopeOut<E>{static_cast<const float*>(keep.act), static_cast<const float*>(keep.mul), dg, du}, on);
         }
@@ -297,16 +348,15 @@ extern "C" int dgsp_gated_ff_backward(int64_t rows, int64_t width, int64_t hidde
             args.pairs = 2;
             args.a[0] = source(dg, rows);
             args.a[1] = source(du, rows);
-            const bool alike = ldg == ldu && in_place<T>(w_gate, hidden, width, ldg) && in_place<T>(w_up, hidden, width, ldu);
-            args.b[0] = source<T, E>(w_gate, hidden, width, ldg, at.gate, on, !alike);
-            args.b[1] = source<T, E>(w_up, hidden, width, ldu, at.up_weight, on, !alike);
+            args.b[0] = gate;
+            args.b[1] = up;
             product<T, E, true, false>(at.dx, args, {{static_cast<T*>(dx), nullptr}, width, false, nullptr}, at.partial, on);
         }
         if (dw_gate || dw_up) {
             args = product_args(at.gates, hidden, width, rows, planes, batch);
             args.a[0] = source(dw_gate ? dg : du, rows);
             args.a[1] = source(du, rows);
-            args.b[0] = source<T, E>(x, rows, width, ldx, at.x, on);
+            args.b[0] = in;
             product<T, E, false, false>(at.gates, args, {{static_cast<T*>(dw_gate ? dw_gate : dw_up), static_cast<T*>(dw_up)}, width, false, nullptr},
                                         at.partial, on);
         }

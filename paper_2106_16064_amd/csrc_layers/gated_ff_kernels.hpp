@@ -2,38 +2,37 @@
 #pragma once
 
 #include "../../include/dgsp_layers.h"
+#include "chunks.hpp"
 #include "matrix_tiles.hpp"
 
 namespace dgsp {
 
-// act(g) and its derivative
-__device__ __forceinline__ void activate(int kind, float g, float& value, float& slope) {
-    if (kind == DGSP_ACT_RELU) {
-        value = g > 0.0f ? g : (g != g ? g : 0.0f);
-        slope = g > 0.0f ? 1.0f : 0.0f;
-    } else if (kind == DGSP_ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-g));
-        value = g * s;
-        slope = s * (1.0f + g * (1.0f - s));
-    } else {
-        const float c = 0.5f * (1.0f + erff(g * 0.70710678f));
-        value = g * c;
-        slope = c + g * expf(-0.5f * g * g) * 0.39894228f;
-    }
-}
-
-// The same for results of 16 bits, kCount numbers at once (one branch on the kind for all of them): exp2 and the reciprocal of the
-// hardware (one unit in the last place of float each; the argument of the exponential is off by g 2^-24), and erf to 1.5e-7 (Abramowitz,
-// Stegun, Handbook of Mathematical Functions, 7.1.26).  A third of the instructions.
-template <int kCount>
-__device__ __forceinline__ void activate_short(int kind, const float (&g)[kCount], float (&value)[kCount], float (&slope)[kCount]) {
+// act(g) and its derivative, kCount numbers at once (one branch on the kind for all of them): exp2 and the reciprocal of the hardware
+// (one unit in the last place of float each; the argument of the exponential is off by g 2^-24), and erf to 1.5e-7 (Abramowitz, Stegun,
+// Handbook of Mathematical Functions, 7.1.26), which is what 1 + erf(z) keeps of it in float anyway.  A third of the instructions of
+// the library's functions, which took longer than the products where the depth is small.  kFloat: results are float, and the rounding of
+// the sigmoid's argument is made up for.
+template <bool kFloat, int kCount>
+__device__ __forceinline__ void activate(int kind, const float (&g)[kCount], float (&value)[kCount], float (&slope)[kCount]) {
     if (kind == DGSP_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) activate(DGSP_ACT_RELU, g[i], value[i], slope[i]);
+        for (int i = 0; i < kCount; ++i) {
+            value[i] = g[i] > 0.0f ? g[i] : (g[i] != g[i] ? g[i] : 0.0f);
+            slope[i] = g[i] > 0.0f ? 1.0f : 0.0f;
+        }
     } else if (kind == DGSP_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g[i]));
+            float e;
+            if constexpr (kFloat) {
+                const float power = fminf(-1.44269504f * g[i], 126.0f);                     // below that the value is 0
+                const float rest = power < 126.0f ? fmaf(-1.44269504f, g[i], -power) - 1.925963e-8f * g[i] : 0.0f;
+                e = __builtin_amdgcn_exp2f(power);
+                e = fmaf(e, 0.69314718f * rest, e);
+            } else {
+                e = __builtin_amdgcn_exp2f(-1.44269504f * g[i]);
+            }
+            const float s = __builtin_amdgcn_rcpf(1.0f + e);
             value[i] = g[i] * s;
             slope[i] = s + value[i] * (1.0f - s);
         }
@@ -96,27 +95,54 @@ struct Planes {
 
 // ---------------------------------------------------------------- laying out
 
-// `from`, rows x cols, as planes whose rows are padded to a multiple of 8 with zeros
+// A matrix of T as planes of E whose rows are padded to a multiple of 8 with zeros.
 template <typename T, typename E>
-__global__ void lay_out_kernel(int64_t rows, int64_t cols, const T* from, int64_t ld, E* to, int64_t to_ld, int64_t plane) {
+struct Layout {
+    const T* from;
+    int64_t rows, cols, ld;
+    E* to;
+    int64_t to_ld;
+    unsigned groups;            // workgroups that work on it
+};
+
+constexpr int kMostLayouts = 5;
+
+template <typename T, typename E>
+struct Layouts {
+    Layout<T, E> each[kMostLayouts];
+    int count;
+};
+
+// all matrices of a call in one launch
+template <typename T, typename E>
+__global__ __launch_bounds__(256) void lay_out_kernel(Layouts<T, E> all) {
     using E8 = E __attribute__((ext_vector_type(8)));
-    const int64_t chunks = to_ld / 8, step = (int64_t)gridDim.x * blockDim.x;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < rows * chunks; i += step) {
-        const int64_t row = i / chunks, col = (i - row * chunks) * 8;
-        const T* at = from + row * ld + col;
-        E8 out[3];
+    unsigned group = blockIdx.x;
+    Layout<T, E> l = all.each[0];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const T v = col + j < cols ? at[j] : (T)0.0f;
-            if constexpr (sizeof(T) == 4) {
-                bf16_t parts[3];
-                split3(v, parts);
-                for (int q = 0; q < 3; ++q) out[q][j] = parts[q];
-            } else {
-                out[0][j] = v;
-            }
+    for (int i = 1; i < kMostLayouts; ++i)
+        if (i < all.count && group >= l.groups) {
+            group -= l.groups;
+            l = all.each[i];
         }
-        for (int q = 0; q < (sizeof(T) == 4 ? 3 : 1); ++q) *reinterpret_cast<E8*>(to + q * plane + row * to_ld + col) = out[q];
+    const int64_t chunks = l.to_ld / 8, step = (int64_t)l.groups * blockDim.x, plane = l.rows * l.to_ld;
+    for (int64_t i = (int64_t)group * blockDim.x + threadIdx.x; i < l.rows * chunks; i += step) {
+        const int64_t row = i / chunks, col = (i - row * chunks) * 8;
+        const RawChunk<T> raw = load_chunk(l.from + row * l.ld + col, l.cols - col);
+        E* to = l.to + row * l.to_ld + col;
+        if constexpr (sizeof(T) == 4) {
+            E8 out[3];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                bf16_t parts[3];
+                split3(raw.at(j), parts);
+                for (int q = 0; q < 3; ++q) out[q][j] = parts[q];
+            }
+#pragma unroll
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<E8*>(to + q * plane) = out[q];
+        } else {
+            *reinterpret_cast<u32x4*>(to) = raw.q[0];
+        }
     }
 }
 
@@ -124,8 +150,7 @@ __global__ void lay_out_kernel(int64_t rows, int64_t cols, const T* from, int64_
 
 // h = act(g) u, and for the backward pass act(g) and u act'(g), which it multiplies by dh.  These two are kept in 32 bits: rounded to
 // 16 they would double the squared error of the gates' gradients, and the 8 bytes an element cost 3 % of a large block's step.
-// kShort: of a 16-bit type.
-template <typename E, bool kShort>
+template <typename E, bool kFloat>
 struct GatedUpOut {
     Planes<E> h;
     float *act, *mul;           // null: not wanted
@@ -140,12 +165,7 @@ struct GatedUpOut {
         float g[4 * kEach], value[4 * kEach], slope[4 * kEach];
 #pragma unroll
         for (int i = 0; i < 4 * kEach; ++i) g[i] = v[i / 4][0][i % 4];
-        if constexpr (kShort) {
-            activate_short(activation, g, value, slope);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4 * kEach; ++i) activate(activation, g[i], value[i], slope[i]);
-        }
+        activate<kFloat>(activation, g, value, slope);
         const int64_t at = m * h.ld + n;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
@@ -237,16 +257,27 @@ struct ProductOut {
     }
 };
 
-// the sum of the splits, in order
+constexpr int kJoinAhead = 8;
+
+// the sum of the splits, in order; eight are asked for at a time
 template <typename T>
-__global__ void join_kernel(int64_t m, int64_t n, int batch, int splits, const float* partial, ProductOut<T> out) {
+__global__ __launch_bounds__(256) void join_kernel(int64_t m, int64_t n, int batch, int splits, const float* partial, ProductOut<T> out) {
     const int64_t quads = (n + 3) / 4, count = m * quads, step = (int64_t)gridDim.x * blockDim.x;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < count * batch; i += step) {
-        const int64_t b = i / count, row = (i - b * count) / quads, col = (i % quads) * 4;
+        const int64_t b = i / count, row = (i - b * count) / quads, col = (i - b * count - row * quads) * 4;
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(partial + 4 * (s * count * batch + i));
+        for (int s = 0; s < splits; s += kJoinAhead) {
+            f32x4 ahead[kJoinAhead];
+#pragma unroll
+            for (int j = 0; j < kJoinAhead; ++j)
+                ahead[j] = s + j < splits ? *reinterpret_cast<const f32x4*>(partial + 4 * ((s + j) * count * batch + i)) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < kJoinAhead; ++j) sum += ahead[j];
+        }
+        T* to = (b ? out.c[1] : out.c[0]) + row * out.ld + col;
+#pragma unroll
         for (int r = 0; r < 4; ++r)
-            if (col + r < n) out.c[b][row * out.ld + col + r] = from_float<T>(sum[r]);
+            if (col + r < n) to[r] = from_float<T>(sum[r]);
     }
 }
 

@@ -150,7 +150,7 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_forward_kernel(NarrowArgs<
                 float in[8], value[8], slope[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) in[i] = g[i / 4][i % 4];
-                activate_short(a.activation, in, value, slope);
+                activate<false>(a.activation, in, value, slope);
 #pragma unroll
                 for (int b = 0; b < 2; ++b) h[b][part] = pack<E>(f32x4{value[4 * b], value[4 * b + 1], value[4 * b + 2], value[4 * b + 3]} * u[b]);
             }
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_staged_kernel(Nar
                                      dy[s], dh);
                 }
                 float in[4] = {g[0], g[1], g[2], g[3]}, value[4], slope[4];
-                activate_short(a.activation, in, value, slope);
+                activate<false>(a.activation, in, value, slope);
                 f32x4 gs, us, hs;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
@@ -372,7 +372,7 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs
             float in[8], value[8], slope[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) in[i] = g[i / 4][i % 4];
-            activate_short(a.activation, in, value, slope);
+            activate<false>(a.activation, in, value, slope);
             s16x4 dg[2], du[2], h[2];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
