@@ -11,6 +11,7 @@ using namespace dgsp;
 
 constexpr int64_t kMostWidth = (1LL << 22) - 8;         // 256 rows of it span less than 2^31 bytes (matrix_tiles.hpp)
 constexpr int64_t kAlign = 256;
+constexpr int64_t kCus = 256;
 
 int64_t padded(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
 
@@ -19,9 +20,9 @@ bool gated_extents(int64_t rows, int64_t width, int64_t hidden, int64_t out_widt
            out_width >= 1 && out_width <= kMostWidth && known_type(type);
 }
 
-bool enough(const void* workspace, int64_t bytes, int64_t need) { return need == 0 || (workspace && aligned(workspace, 16) && bytes >= need); }
+bool known_activation(int activation) { return activation >= DGSP_ACT_SILU && activation <= DGSP_ACT_RELU; }
 
-int planes_of(int type) { return type == DGSP_F32 ? 3 : 1; }
+bool enough(const void* workspace, int64_t bytes, int64_t need) { return need == 0 || (workspace && aligned(workspace, 16) && bytes >= need); }
 
 // Hands out pieces of a buffer, or adds up what they need where there is none.
 class Pieces {
@@ -51,18 +52,16 @@ struct Cut {
     int64_t groups(int batch) const { return tiles_m * tiles_n * batch * splits; }
 };
 
-constexpr int64_t kCus = 256;
-
 // Which tiles.  256 x 256 read half as much per product as 128 x 128, but take a CU each, so that nothing runs while their results leave:
-// they pay where the sum is long (1024 at least, counting pairs and products of planes), there is one for every CU, and the edges
-// waste little.  (2^16 x 512 of depth 128 in float, 768 in all: 284 us, with 128 x 128 230 us; 8192 x 16384 of depth 4096: 1.24 ms
-// against 1.6.)  64 x 64 are for what has fewer than a tile of 128 for every CU and cannot be split along the depth, or is hardly half
-// as wide.  Where tiles are fewer than CUs the depth is split, to two workgroups a CU of at least 512 each.
-Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, bool dual, bool may_split) {
+// they pay where the sum is long (`terms` counts pairs of operands), there is one for every CU, and the edges waste little.  64 x 64 are
+// for what has fewer than a tile of 128 for every CU and cannot be split along the depth, or is hardly half as wide.  Where tiles are
+// fewer than CUs the depth is split, to two workgroups a CU of at least 512 each.  Float matrices have no tiles of 256: their three planes
+// of two operands do not fit the registers.
+Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, int type, bool dual, bool may_split) {
     auto tiles = [&](int size) { return ceil_div(m, size) * ceil_div(n, dual ? size / 2 : size) * batch; };
     const bool splits = may_split && depth >= 1024;
     Cut c{kSmall, 0, 0, 1, padded(std::max<int64_t>(depth, 1), kDepth)};
-    if (tiles(kLarge) >= kCus && depth * terms >= 1024 && 4 * tiles(kLarge) <= tiles(kMiddle) + tiles(kMiddle) / 8)
+    if (type != DGSP_F32 && tiles(kLarge) >= kCus && depth * terms >= 1024 && 4 * tiles(kLarge) <= tiles(kMiddle) + tiles(kMiddle) / 8)
         c.size = kLarge;
     else if ((tiles(kMiddle) >= kCus || splits) && 2 * (4 * tiles(kMiddle)) <= 3 * tiles(kSmall))
         c.size = kMiddle;
@@ -86,10 +85,10 @@ using Middle = TileShape<128, 128, 2, 2, kDual>;
 template <bool kDual>
 using Small = TileShape<64, 64, 2, 2, kDual>;
 
-ProductArgs product_args(const Cut& c, int64_t m, int64_t n, int64_t depth, int planes, int batch) {
-    ProductArgs args{};
+template <typename T>
+ProductArgs<T> product_args(const Cut& c, int64_t m, int64_t n, int64_t depth, int batch) {
+    ProductArgs<T> args{};
     args.pairs = 1;
-    args.planes = planes;
     args.m = m;
     args.n = n;
     args.depth = depth;
@@ -105,24 +104,30 @@ int64_t partial_bytes(const Cut& c, int64_t m, int64_t n, int batch) {
     return c.splits > 1 ? (int64_t)c.splits * batch * m * padded(n, 4) * 4 : 0;
 }
 
-template <typename E, bool kDual, bool kARows, bool kBRows, typename Out>
-void launch(const Cut& c, const ProductArgs& args, const Out& out, hipStream_t stream) {
+template <typename T, bool kDual, bool kARows, bool kBRows, typename Out>
+void launch(const Cut& c, const ProductArgs<T>& args, const Out& out, hipStream_t stream) {
     const auto groups = (unsigned)c.groups(args.batch);
-    if (c.size == kLarge)
-        tile_kernel<E, Large<kDual>, kARows, kBRows, Out><<<groups, Large<kDual>::kThreads, 0, stream>>>(args, out);
-    else if (c.size == kMiddle)
-        tile_kernel<E, Middle<kDual>, kARows, kBRows, Out><<<groups, Middle<kDual>::kThreads, 0, stream>>>(args, out);
-    else
-        tile_kernel<E, Small<kDual>, kARows, kBRows, Out><<<groups, Small<kDual>::kThreads, 0, stream>>>(args, out);
+    if constexpr (sizeof(T) == 4) {
+        if (c.size == kMiddle)
+            float_tile_kernel<Middle<kDual>, kARows, kBRows, Out><<<groups, Middle<kDual>::kThreads, 0, stream>>>(args, out);
+        else
+            float_tile_kernel<Small<kDual>, kARows, kBRows, Out><<<groups, Small<kDual>::kThreads, 0, stream>>>(args, out);
+    } else if (c.size == kLarge) {
+        tile_kernel<T, Large<kDual>, kARows, kBRows, Out><<<groups, Large<kDual>::kThreads, 0, stream>>>(args, out);
+    } else if (c.size == kMiddle) {
+        tile_kernel<T, Middle<kDual>, kARows, kBRows, Out><<<groups, Middle<kDual>::kThreads, 0, stream>>>(args, out);
+    } else {
+        tile_kernel<T, Small<kDual>, kARows, kBRows, Out><<<groups, Small<kDual>::kThreads, 0, stream>>>(args, out);
+    }
 }
 
 // c[0 ... batch - 1] = the product
-template <typename T, typename E, bool kARows, bool kBRows>
-void product(const Cut& c, const ProductArgs& args, ProductOut<T> out, void* partial, hipStream_t stream) {
+template <typename T, bool kARows, bool kBRows>
+void product(const Cut& c, const ProductArgs<T>& args, ProductOut<T> out, void* partial, hipStream_t stream) {
     if (args.m == 0) return;
     out.vectors = out.ld % 4 == 0 && aligned(out.c[0], 4 * sizeof(T)) && (args.batch < 2 || aligned(out.c[1], 4 * sizeof(T)));
     out.partial = c.splits > 1 ? static_cast<float*>(partial) : nullptr;
-    launch<E, false, kARows, kBRows>(c, args, out, stream);
+    launch<T, false, kARows, kBRows>(c, args, out, stream);
     if (c.splits > 1) {
         const int64_t quads = args.batch * args.m * ceil_div(args.n, 4);
         join_kernel<T><<<(unsigned)std::min<int64_t>(ceil_div(quads, 256), 4096), 256, 0, stream>>>(args.m, args.n, args.batch, c.splits, out.partial, out);
@@ -131,111 +136,87 @@ void product(const Cut& c, const ProductArgs& args, ProductOut<T> out, void* par
 
 // ---------------------------------------------------------------- operands
 
-int64_t laid_out_bytes(int64_t rows, int64_t cols, int type) { return rows * padded(cols, 8) * 2 * planes_of(type); }
+int64_t kept_bytes(int64_t rows, int64_t cols, int type) { return rows * padded(cols, 8) * element_bytes(type); }
 
-// Is the matrix of 16-bit elements, in whole 16-byte pieces?
+// what a matrix that does not lie as the products read it takes; float matrices are read as they lie
+int64_t laid_out_bytes(int64_t rows, int64_t cols, int type) { return type == DGSP_F32 ? 0 : kept_bytes(rows, cols, type); }
+
+// The matrices of a call as its products read them: float matrices as they are, those of 16-bit elements in place if they lie in whole
+// 16-byte pieces, else laid out in a piece of memory, all in one launch that has to come before the products'.
 template <typename T>
-bool in_place(const void* p, int64_t rows, int64_t cols, int64_t ld) {
-    return sizeof(T) == 2 && cols % 8 == 0 && (rows == 1 || (ld % 8 == 0 && ld >= cols && ld <= kMostWidth)) && aligned(p, 16);
-}
-
-// The matrices of a call as its products read them: in place where they can be, else laid out in a piece of memory, all in one launch
-// that has to come before the products'.
-template <typename T, typename E>
 class Operands {
 public:
-    Source add(const void* p, int64_t rows, int64_t cols, int64_t ld, void* piece, bool copy = false) {
-        if (in_place<T>(p, rows, cols, ld) && !copy) return {static_cast<const uint16_t*>(p), rows, cols, rows == 1 ? cols : ld, 0};
-        const int64_t to_ld = padded(cols, 8), chunks = rows * to_ld / 8;
+    static bool in_place(const void* p, int64_t rows, int64_t cols, int64_t ld) {
+        return sizeof(T) == 4 || (cols % 8 == 0 && (rows == 1 || (ld % 8 == 0 && ld >= cols && ld <= kMostWidth)) && aligned(p, 16));
+    }
+    Source<T> add(const void* p, int64_t rows, int64_t cols, int64_t ld, void* piece, bool copy = false) {
+        if (in_place(p, rows, cols, ld) && !copy) return {static_cast<const T*>(p), rows, cols, rows == 1 ? cols : ld};
+        const int64_t to_ld = padded(cols, 8);
         if (rows > 0) {
-            const auto groups = (unsigned)std::min<int64_t>(ceil_div(chunks, 256), 1 << 14);
-            all_.each[all_.count++] = {static_cast<const T*>(p), rows, cols, ld, static_cast<E*>(piece), to_ld, groups};
+            const auto groups = (unsigned)std::min<int64_t>(ceil_div(rows * to_ld / 8, 256), 1 << 14);
+            all_.each[all_.count++] = {static_cast<const T*>(p), rows, cols, ld, static_cast<T*>(piece), to_ld, groups};
             groups_ += groups;
         }
-        return laid_out(piece, rows, cols);
-    }
-    // what an earlier call has laid out there
-    static Source laid_out(const void* piece, int64_t rows, int64_t cols) {
-        const int64_t ld = padded(cols, 8);
-        return {static_cast<const uint16_t*>(piece), rows, ld, ld, sizeof(T) == 4 ? rows * ld : 0};
+        return {static_cast<const T*>(piece), rows, to_ld, to_ld};
     }
     void launch(hipStream_t stream) const {
-        if (all_.count) lay_out_kernel<T, E><<<groups_, 256, 0, stream>>>(all_);
+        if constexpr (sizeof(T) == 2)
+            if (all_.count) lay_out_kernel<T><<<groups_, 256, 0, stream>>>(all_);
     }
 
 private:
-    Layouts<T, E> all_{};
+    Layouts<T> all_{};
     unsigned groups_ = 0;
 };
 
-template <typename E>
-Source source(const Planes<E>& planes, int64_t rows) {
-    return {reinterpret_cast<const uint16_t*>(planes.p), rows, planes.ld, planes.ld, planes.plane};
+template <typename T>
+Source<T> source(const Kept<T>& kept, int64_t rows) {
+    return {kept.p, rows, kept.ld, kept.ld};
 }
 
-template <typename T, typename E>
-Planes<E> hidden_planes(void* p, int64_t rows, int64_t hidden) {
-    const int64_t ld = padded(hidden, 8);
-    return {static_cast<E*>(p), ld, sizeof(T) == 4 ? rows * ld : 0};
+template <typename T>
+Kept<T> kept(void* p, int64_t hidden) {
+    return {static_cast<T*>(p), padded(hidden, 8)};
 }
 
-// What the forward pass leaves: act(g) and u act'(g) in 32 bits, h, and of float matrices the planes that it has laid out.
+// what the forward pass leaves: act(g) and u act'(g) in 32 bits, and h
 struct Saved {
-    void *act, *mul, *h, *x = nullptr, *gate = nullptr, *up = nullptr, *down = nullptr;
-    Saved(Pieces& pieces, int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type)
-        : act(pieces.take(rows * padded(hidden, 8) * 4)), mul(pieces.take(rows * padded(hidden, 8) * 4)),
-          h(pieces.take(laid_out_bytes(rows, hidden, type))) {
-        if (type != DGSP_F32) return;
-        x = pieces.take(laid_out_bytes(rows, width, type));
-        gate = pieces.take(laid_out_bytes(hidden, width, type));
-        up = pieces.take(laid_out_bytes(hidden, width, type));
-        down = pieces.take(laid_out_bytes(out_width, hidden, type));
-    }
+    void *act, *mul, *h;
+    Saved(Pieces& pieces, int64_t rows, int64_t hidden, int type)
+        : act(pieces.take(kept_bytes(rows, hidden, DGSP_F32))), mul(pieces.take(kept_bytes(rows, hidden, DGSP_F32))),
+          h(pieces.take(kept_bytes(rows, hidden, type))) {}
 };
-
-int terms_of(int type) { return type == DGSP_F32 ? 6 : 1; }
 
 struct ForwardPieces {
     Cut up, down;
     void *x, *gate, *up_weight, *down_weight, *h, *partial;
     ForwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type)
-        : up(cut(rows, hidden, width, terms_of(type), 1, true, false)), down(cut(rows, out_width, hidden, terms_of(type), 1, false, true)),
+        : up(cut(rows, hidden, width, 1, 1, type, true, false)), down(cut(rows, out_width, hidden, 1, 1, type, false, true)),
           x(pieces.take(laid_out_bytes(rows, width, type))), gate(pieces.take(laid_out_bytes(hidden, width, type))),
           up_weight(pieces.take(laid_out_bytes(hidden, width, type))), down_weight(pieces.take(laid_out_bytes(out_width, hidden, type))),
-          h(pieces.take(laid_out_bytes(rows, hidden, type))), partial(pieces.take(partial_bytes(down, rows, out_width, 1))) {}
+          h(pieces.take(kept_bytes(rows, hidden, type))), partial(pieces.take(partial_bytes(down, rows, out_width, 1))) {}
 };
 
 struct BackwardPieces {
     Cut slope, dx, gates, down;
-    void *x = nullptr, *gate = nullptr, *up_weight = nullptr, *down_weight = nullptr, *dy, *dg, *du, *partial;
+    void *x, *gate, *up_weight, *down_weight, *dy, *dg, *du, *partial;
     BackwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type, int batch)
-        : slope(cut(rows, hidden, out_width, terms_of(type), 1, false, false)), dx(cut(rows, width, hidden, 2 * terms_of(type), 1, false, true)),
-          gates(cut(hidden, width, rows, terms_of(type), batch, false, true)), down(cut(out_width, hidden, rows, terms_of(type), 1, false, true)),
-          dy(pieces.take(laid_out_bytes(rows, out_width, type))), dg(pieces.take(laid_out_bytes(rows, hidden, type))),
-          du(pieces.take(laid_out_bytes(rows, hidden, type))),
+        : slope(cut(rows, hidden, out_width, 1, 1, type, false, false)), dx(cut(rows, width, hidden, 2, 1, type, false, true)),
+          gates(cut(hidden, width, rows, 1, batch, type, false, true)), down(cut(out_width, hidden, rows, 1, 1, type, false, true)),
+          x(pieces.take(laid_out_bytes(rows, width, type))), gate(pieces.take(laid_out_bytes(hidden, width, type))),
+          up_weight(pieces.take(laid_out_bytes(hidden, width, type))), down_weight(pieces.take(laid_out_bytes(out_width, hidden, type))),
+          dy(pieces.take(laid_out_bytes(rows, out_width, type))), dg(pieces.take(kept_bytes(rows, hidden, type))),
+          du(pieces.take(kept_bytes(rows, hidden, type))),
           partial(pieces.take(std::max({partial_bytes(dx, rows, width, 1), partial_bytes(gates, hidden, width, batch),
-                                        partial_bytes(down, out_width, hidden, 1)}))) {
-        if (type == DGSP_F32) return;
-        x = pieces.take(laid_out_bytes(rows, width, type));
-        gate = pieces.take(laid_out_bytes(hidden, width, type));
-        up_weight = pieces.take(laid_out_bytes(hidden, width, type));
-        down_weight = pieces.take(laid_out_bytes(out_width, hidden, type));
-    }
+                                        partial_bytes(down, out_width, hidden, 1)}))) {}
 };
-
-template <typename F>
-int with_elements(int type, F&& f) {
-    if (type == DGSP_F32) return f(float{}, bf16_t{});
-    if (type == DGSP_BF16) return f(bf16_t{}, bf16_t{});
-    return f(f16_t{}, f16_t{});
-}
 
 }  // namespace
 
 extern "C" int64_t dgsp_gated_ff_saved_bytes(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type) {
     if (!gated_extents(rows, width, hidden, out_width, type) || narrow_fits(width, hidden, out_width, type)) return 0;
     Pieces pieces(nullptr);
-    Saved saved(pieces, rows, width, hidden, out_width, type);
+    Saved saved(pieces, rows, hidden, type);
     return pieces.used();
 }
 
@@ -257,8 +238,7 @@ extern "C" int64_t dgsp_gated_ff_backward_workspace_bytes(int64_t rows, int64_t 
 extern "C" int dgsp_gated_ff(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type, int activation, const void* x,
                              int64_t ldx, const void* w_gate, int64_t ldg, const void* w_up, int64_t ldu, const void* w_down, int64_t ldd,
                              void* y, int64_t ldy, void* saved, void* workspace, int64_t workspace_bytes, void* stream) {
-    if (!gated_extents(rows, width, hidden, out_width, type) || activation < DGSP_ACT_SILU || activation > DGSP_ACT_RELU)
-        return DGSP_ERR_INVALID_ARG;
+    if (!gated_extents(rows, width, hidden, out_width, type) || !known_activation(activation)) return DGSP_ERR_INVALID_ARG;
     if (rows == 0) return DGSP_OK;
     if (!readable(x, rows, width, ldx) || !readable(w_gate, hidden, width, ldg) || !readable(w_up, hidden, width, ldu) ||
         !readable(w_down, out_width, hidden, ldd) || !writable(y, rows, out_width, ldy) || !aligned(saved, 16) ||
@@ -266,28 +246,25 @@ extern "C" int dgsp_gated_ff(int64_t rows, int64_t width, int64_t hidden, int64_
         return DGSP_ERR_INVALID_ARG;
     if (narrow_fits(width, hidden, out_width, type))
         return narrow_forward({rows, width, hidden, out_width, type, activation, x, ldx, w_gate, ldg, w_up, ldu, w_down, ldd, y, ldy}, stream);
-    Pieces pieces(workspace), kept(saved);
+    Pieces pieces(workspace), kept_pieces(saved);
     const ForwardPieces at(pieces, rows, width, hidden, out_width, type);
-    const Saved keep(kept, rows, width, hidden, out_width, type);
+    const Saved keep(kept_pieces, rows, hidden, type);
     if (!launchable(at.up, 1) || !launchable(at.down, 1)) return DGSP_ERR_UNSUPPORTED;
-    return with_elements(type, [&](auto t, auto e) {
-        using T = decltype(t);
-        using E = decltype(e);
+    return with_type(type, [&](auto element) {
+        using T = decltype(element);
         const auto on = static_cast<hipStream_t>(stream);
-        const int planes = planes_of(type);
-        const Planes<E> h = hidden_planes<T, E>(saved ? keep.h : at.h, rows, hidden);
-        const bool planes_kept = saved && type == DGSP_F32;
-        Operands<T, E> operands;
-        ProductArgs args = product_args(at.up, rows, hidden, width, planes, 1), down = product_args(at.down, rows, out_width, hidden, planes, 1);
-        args.a[0] = operands.add(x, rows, width, ldx, planes_kept ? keep.x : at.x);
-        args.b[0] = operands.add(w_gate, hidden, width, ldg, planes_kept ? keep.gate : at.gate);
-        args.b[1] = operands.add(w_up, hidden, width, ldu, planes_kept ? keep.up : at.up_weight);
+        const Kept<T> h = kept<T>(saved ? keep.h : at.h, hidden);
+        Operands<T> operands;
+        ProductArgs<T> up = product_args<T>(at.up, rows, hidden, width, 1), down = product_args<T>(at.down, rows, out_width, hidden, 1);
+        up.a[0] = operands.add(x, rows, width, ldx, at.x);
+        up.b[0] = operands.add(w_gate, hidden, width, ldg, at.gate);
+        up.b[1] = operands.add(w_up, hidden, width, ldu, at.up_weight);
         down.a[0] = source(h, rows);
-        down.b[0] = operands.add(w_down, out_width, hidden, ldd, planes_kept ? keep.down : at.down_weight);
+        down.b[0] = operands.add(w_down, out_width, hidden, ldd, at.down_weight);
         operands.launch(on);
-        launch<E, true, true, true>(at.up, args, GatedUpOut<E, sizeof(T) == 4>{h, saved ? static_cast<float*>(keep.act) : nullptr, saved ? static_cast<float*>(keep.mul) : nullptr,
-                                                               activation}, on);
-        product<T, E, true, true>(at.down, down, {{static_cast<T*>(y), nullptr}, ldy, false, nullptr}, at.partial, on);
+        launch<T, true, true, true>(at.up, up, GatedUpOut<T>{h, saved ? static_cast<float*>(keep.act) : nullptr,
+                                                             saved ? static_cast<float*>(keep.mul) : nullptr, activation}, on);
+        product<T, true, true>(at.down, down, {{static_cast<T*>(y), nullptr}, ldy, false, nullptr}, at.partial, on);
         return launched();
     });
 }
@@ -296,9 +273,8 @@ extern "C" int dgsp_gated_ff_backward(int64_t rows, int64_t width, int64_t hidde
                                       const void* x, int64_t ldx, const void* w_gate, int64_t ldg, const void* w_up, int64_t ldu,
                                       const void* w_down, int64_t ldd, const void* dy, int64_t lddy, const void* saved, void* dx,
                                       void* dw_gate, void* dw_up, void* dw_down, void* workspace, int64_t workspace_bytes, void* stream) {
-    if (!gated_extents(rows, width, hidden, out_width, type) || activation < DGSP_ACT_SILU || activation > DGSP_ACT_RELU)
-        return DGSP_ERR_INVALID_ARG;
-    if (!enough(workspace, workspace_bytes, dgsp_gated_ff_backward_workspace_bytes(rows, width, hidden, out_width, type)))
+    if (!gated_extents(rows, width, hidden, out_width, type) || !known_activation(activation) ||
+        !enough(workspace, workspace_bytes, dgsp_gated_ff_backward_workspace_bytes(rows, width, hidden, out_width, type)))
         return DGSP_ERR_INVALID_ARG;
     const bool narrow = narrow_fits(width, hidden, out_width, type);
     if (rows > 0 && (!readable(x, rows, width, ldx) || !readable(w_gate, hidden, width, ldg) || !readable(w_up, hidden, width, ldu) ||
@@ -308,64 +284,56 @@ extern "C" int dgsp_gated_ff_backward(int64_t rows, int64_t width, int64_t hidde
         return narrow_backward({rows, width, hidden, out_width, type, activation, x, ldx, w_gate, ldg, w_up, ldu, w_down, ldd, nullptr, 0, dy, lddy, dx,
                                 dw_gate, dw_up, dw_down, workspace}, stream);
     const int batch = dw_gate && dw_up ? 2 : 1;
-    Pieces pieces(workspace), kept(const_cast<void*>(saved));
+    Pieces pieces(workspace), kept_pieces(const_cast<void*>(saved));
     const BackwardPieces at(pieces, rows, width, hidden, out_width, type, batch);
-    const Saved keep(kept, rows, width, hidden, out_width, type);
+    const Saved keep(kept_pieces, rows, hidden, type);
     if (!launchable(at.slope, 1) || !launchable(at.dx, 1) || !launchable(at.gates, batch) || !launchable(at.down, 1))
         return DGSP_ERR_UNSUPPORTED;
-    return with_elements(type, [&](auto t, auto e) {
-        using T = decltype(t);
-        using E = decltype(e);
+    return with_type(type, [&](auto element) {
+        using T = decltype(element);
         const auto on = static_cast<hipStream_t>(stream);
-        const int planes = planes_of(type);
         const bool gates = (dx || dw_gate || dw_up) && rows > 0;
-        Operands<T, E> operands;
-        // of float matrices the forward pass has left the planes; weights of a pair have to lie alike
-        auto operand = [&](const void* p, int64_t count, int64_t cols, int64_t ld, const void* planes_kept, void* piece, bool copy = false) {
-            return type == DGSP_F32 ? Operands<T, E>::laid_out(planes_kept, count, cols) : operands.add(p, count, cols, ld, piece, copy);
-        };
-        const bool alike = ldg == ldu && in_place<T>(w_gate, hidden, width, ldg) && in_place<T>(w_up, hidden, width, ldu);
-        const Source grad = operands.add(dy, rows, out_width, lddy, at.dy);
-        Source in{}, gate{}, up{}, down{};
-        if (dw_gate || dw_up) in = operand(x, rows, width, ldx, keep.x, at.x);
-        if (dx) {
-            gate = operand(w_gate, hidden, width, ldg, keep.gate, at.gate, !alike);
-            up = operand(w_up, hidden, width, ldu, keep.up, at.up_weight, !alike);
+        Operands<T> operands;
+        Source<T> in{}, gate{}, up{}, down{};
+        const Source<T> grad = operands.add(dy, rows, out_width, lddy, at.dy);
+        if (dw_gate || dw_up) in = operands.add(x, rows, width, ldx, at.x);
+        if (dx) {                                       // a pair's operands lie alike
+            const bool alike = ldg == ldu && operands.in_place(w_gate, hidden, width, ldg) && operands.in_place(w_up, hidden, width, ldu);
+            gate = operands.add(w_gate, hidden, width, ldg, at.gate, sizeof(T) == 2 && !alike);
+            up = operands.add(w_up, hidden, width, ldu, at.up_weight, sizeof(T) == 2 && !alike);
         }
-        if (gates) down = operand(w_down, out_width, hidden, ldd, keep.down, at.down_weight);
+        if (gates) down = operands.add(w_down, out_width, hidden, ldd, at.down_weight);
         operands.launch(on);
-        const Planes<E> dg = hidden_planes<T, E>(at.dg, rows, hidden), du = hidden_planes<T, E>(at.du, rows, hidden);
-        ProductArgs args;
+        const Kept<T> dg = kept<T>(at.dg, hidden), du = kept<T>(at.du, hidden), h = kept<T>(keep.h, hidden);
         if (gates) {
-            args = product_args(at.slope, rows, hidden, out_width, planes, 1);
+            ProductArgs<T> args = product_args<T>(at.slope, rows, hidden, out_width, 1);
             args.a[0] = grad;
             args.b[0] = down;
-            launch<E, false, true, false>(at.slope, args,
-                                          GatedSlopeOut<E>{static_cast<const float*>(keep.act), static_cast<const float*>(keep.mul), dg, du}, on);
+            launch<T, false, true, false>(at.slope, args,
+                                          GatedSlopeOut<T>{static_cast<const float*>(keep.act), static_cast<const float*>(keep.mul), dg, du}, on);
         }
         if (dx) {
-            args = product_args(at.dx, rows, width, hidden, planes, 1);
+            ProductArgs<T> args = product_args<T>(at.dx, rows, width, hidden, 1);
             args.pairs = 2;
             args.a[0] = source(dg, rows);
             args.a[1] = source(du, rows);
             args.b[0] = gate;
             args.b[1] = up;
-            product<T, E, true, false>(at.dx, args, {{static_cast<T*>(dx), nullptr}, width, false, nullptr}, at.partial, on);
+            product<T, true, false>(at.dx, args, {{static_cast<T*>(dx), nullptr}, width, false, nullptr}, at.partial, on);
         }
         if (dw_gate || dw_up) {
-            args = product_args(at.gates, hidden, width, rows, planes, batch);
+            ProductArgs<T> args = product_args<T>(at.gates, hidden, width, rows, batch);
             args.a[0] = source(dw_gate ? dg : du, rows);
             args.a[1] = source(du, rows);
             args.b[0] = in;
-            product<T, E, false, false>(at.gates, args, {{static_cast<T*>(dw_gate ? dw_gate : dw_up), static_cast<T*>(dw_up)}, width, false, nullptr},
-                                        at.partial, on);
+            product<T, false, false>(at.gates, args, {{static_cast<T*>(dw_gate ? dw_gate : dw_up), static_cast<T*>(dw_up)}, width, false, nullptr},
+                                     at.partial, on);
         }
         if (dw_down) {
-            args = product_args(at.down, out_width, hidden, rows, planes, 1);
+            ProductArgs<T> args = product_args<T>(at.down, out_width, hidden, rows, 1);
             args.a[0] = grad;
-            const Planes<E> h = hidden_planes<T, E>(keep.h, rows, hidden);
             args.b[0] = source(h, rows);
-            product<T, E, false, false>(at.down, args, {{static_cast<T*>(dw_down), nullptr}, hidden, false, nullptr}, at.partial, on);
+            product<T, false, false>(at.down, args, {{static_cast<T*>(dw_down), nullptr}, hidden, false, nullptr}, at.partial, on);
         }
         return launched();
     });

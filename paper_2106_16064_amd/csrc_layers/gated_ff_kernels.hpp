@@ -3,6 +3,7 @@
 
 #include "../../include/dgsp_layers.h"
 #include "chunks.hpp"
+#include "float_tiles.hpp"
 #include "matrix_tiles.hpp"
 
 namespace dgsp {
@@ -49,100 +50,53 @@ __device__ __forceinline__ void activate(int kind, const float (&g)[kCount], flo
     }
 }
 
-// v as the sum of three bf16 numbers, each the rest rounded to nearest: what is left is below 2^-26 of v.  Where rounding would pass
-// the largest bf16 number the first one is cut off instead; what is not finite stays in the first one.
-__device__ __forceinline__ void split3(float v, bf16_t (&out)[3]) {
-    out[0] = (bf16_t)v;
-    float rest = v - (float)out[0];
-    if (!(fabsf((float)out[0]) < __builtin_inff())) {
-        if (fabsf(v) < __builtin_inff()) {
-            out[0] = __builtin_bit_cast(bf16_t, (uint16_t)(__builtin_bit_cast(uint32_t, v) >> 16));
-            rest = v - (float)out[0];
-        } else {
-            rest = 0.0f;
-        }
-    }
-    out[1] = (bf16_t)rest;
-    out[2] = (bf16_t)(rest - (float)out[1]);
-}
-
-// A matrix that later products read, in planes of E.  ld is a multiple of 8.
-template <typename E>
-struct Planes {
-    E* p;
-    int64_t ld, plane;          // plane 0: one plane
+// A matrix that the block keeps between its products; ld is a multiple of 8.
+template <typename T>
+struct Kept {
+    T* p;
+    int64_t ld;
     // four neighbours
     __device__ __forceinline__ void store(int64_t at, f32x4 v) const {
-        using E4 = E __attribute__((ext_vector_type(4)));
-        E* to = p + at;
-        if (plane) {
-            if constexpr (sizeof(E) == 2 && !__is_same(E, f16_t)) {
-                E4 out[3];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    bf16_t parts[3];
-                    split3(v[r], parts);
-                    for (int q = 0; q < 3; ++q) out[q][r] = parts[q];
-                }
-#pragma unroll
-                for (int q = 0; q < 3; ++q) *reinterpret_cast<E4*>(to + q * plane) = out[q];
-            }
-        } else {
-            *reinterpret_cast<E4*>(to) = E4{from_float<E>(v[0]), from_float<E>(v[1]), from_float<E>(v[2]), from_float<E>(v[3])};
-        }
+        using T4 = T __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<T4*>(p + at) = T4{from_float<T>(v[0]), from_float<T>(v[1]), from_float<T>(v[2]), from_float<T>(v[3])};
     }
 };
 
 // ---------------------------------------------------------------- laying out
 
-// A matrix of T as planes of E whose rows are padded to a multiple of 8 with zeros.
-template <typename T, typename E>
+// A matrix of 16-bit elements whose rows are padded to a multiple of 8 with zeros.
+template <typename T>
 struct Layout {
     const T* from;
     int64_t rows, cols, ld;
-    E* to;
+    T* to;
     int64_t to_ld;
     unsigned groups;            // workgroups that work on it
 };
 
 constexpr int kMostLayouts = 5;
 
-template <typename T, typename E>
+template <typename T>
 struct Layouts {
-    Layout<T, E> each[kMostLayouts];
+    Layout<T> each[kMostLayouts];
     int count;
 };
 
 // all matrices of a call in one launch
-template <typename T, typename E>
-__global__ __launch_bounds__(256) void lay_out_kernel(Layouts<T, E> all) {
-    using E8 = E __attribute__((ext_vector_type(8)));
+template <typename T>
+__global__ __launch_bounds__(256) void lay_out_kernel(Layouts<T> all) {
     unsigned group = blockIdx.x;
-    Layout<T, E> l = all.each[0];
+    Layout<T> l = all.each[0];
 #pragma unroll
     for (int i = 1; i < kMostLayouts; ++i)
         if (i < all.count && group >= l.groups) {
             group -= l.groups;
             l = all.each[i];
         }
-    const int64_t chunks = l.to_ld / 8, step = (int64_t)l.groups * blockDim.x, plane = l.rows * l.to_ld;
+    const int64_t chunks = l.to_ld / 8, step = (int64_t)l.groups * blockDim.x;
     for (int64_t i = (int64_t)group * blockDim.x + threadIdx.x; i < l.rows * chunks; i += step) {
         const int64_t row = i / chunks, col = (i - row * chunks) * 8;
-        const RawChunk<T> raw = load_chunk(l.from + row * l.ld + col, l.cols - col);
-        E* to = l.to + row * l.to_ld + col;
-        if constexpr (sizeof(T) == 4) {
-            E8 out[3];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                bf16_t parts[3];
-                split3(raw.at(j), parts);
-                for (int q = 0; q < 3; ++q) out[q][j] = parts[q];
-            }
-#pragma unroll
-            for (int q = 0; q < 3; ++q) *reinterpret_cast<E8*>(to + q * plane) = out[q];
-        } else {
-            *reinterpret_cast<u32x4*>(to) = raw.q[0];
-        }
+        *reinterpret_cast<u32x4*>(l.to + row * l.to_ld + col) = load_chunk(l.from + row * l.ld + col, l.cols - col).q[0];
     }
 }
 
@@ -150,22 +104,22 @@ __global__ __launch_bounds__(256) void lay_out_kernel(Layouts<T, E> all) {
 
 // h = act(g) u, and for the backward pass act(g) and u act'(g), which it multiplies by dh.  These two are kept in 32 bits: rounded to
 // 16 they would double the squared error of the gates' gradients, and the 8 bytes an element cost 3 % of a large block's step.
-template <typename E, bool kFloat>
+template <typename T>
 struct GatedUpOut {
-    Planes<E> h;
+    Kept<T> h;
     float *act, *mul;           // null: not wanted
     int activation;
     template <int kEach>
-    __device__ __forceinline__ Nothing ask(const ProductArgs&, int64_t, int64_t) const {
+    __device__ __forceinline__ Nothing ask(const ProductArgs<T>&, int64_t, int64_t) const {
         return {};
     }
     template <int kEach>
-    __device__ __forceinline__ void row(const ProductArgs& args, const TileIndex&, int64_t m, int64_t n, Nothing, const f32x4 (&v)[kEach][2]) const {
+    __device__ __forceinline__ void row(const ProductArgs<T>& args, const TileIndex&, int64_t m, int64_t n, Nothing, const f32x4 (&v)[kEach][2]) const {
         if (m >= args.m) return;
         float g[4 * kEach], value[4 * kEach], slope[4 * kEach];
 #pragma unroll
         for (int i = 0; i < 4 * kEach; ++i) g[i] = v[i / 4][0][i % 4];
-        activate<kFloat>(activation, g, value, slope);
+        activate<sizeof(T) == 4>(activation, g, value, slope);
         const int64_t at = m * h.ld + n;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
@@ -182,17 +136,17 @@ struct GatedUpOut {
 };
 
 // dg = dh u act'(g) and du = dh act(g), dh = dy w_down
-template <typename E>
+template <typename T>
 struct GatedSlopeOut {
     const float *act, *mul;
-    Planes<E> dg, du;
+    Kept<T> dg, du;
     template <int kEach>
-    struct Kept {
+    struct Factors {
         f32x4 act[kEach], mul[kEach];
     };
     template <int kEach>
-    __device__ __forceinline__ Kept<kEach> ask(const ProductArgs& args, int64_t m, int64_t n) const {
-        Kept<kEach> out;
+    __device__ __forceinline__ Factors<kEach> ask(const ProductArgs<T>& args, int64_t m, int64_t n) const {
+        Factors<kEach> out;
         const int64_t at = m * dg.ld + n;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
@@ -203,7 +157,7 @@ struct GatedSlopeOut {
         return out;
     }
     template <int kEach>
-    __device__ __forceinline__ void row(const ProductArgs& args, const TileIndex&, int64_t m, int64_t n, const Kept<kEach>& kept,
+    __device__ __forceinline__ void row(const ProductArgs<T>& args, const TileIndex&, int64_t m, int64_t n, const Factors<kEach>& kept,
                                         const f32x4 (&v)[kEach][1]) const {
         if (m >= args.m) return;
         const int64_t at = m * dg.ld + n;
@@ -230,11 +184,11 @@ struct ProductOut {
     bool vectors;               // four neighbours may be written at once
     float* partial;             // not null: split results, [split][batch][m][n padded to 4]
     template <int kEach>
-    __device__ __forceinline__ Nothing ask(const ProductArgs&, int64_t, int64_t) const {
+    __device__ __forceinline__ Nothing ask(const ProductArgs<T>&, int64_t, int64_t) const {
         return {};
     }
     template <int kEach>
-    __device__ __forceinline__ void row(const ProductArgs& args, const TileIndex& tile, int64_t m, int64_t n, Nothing, const f32x4 (&v)[kEach][1]) const {
+    __device__ __forceinline__ void row(const ProductArgs<T>& args, const TileIndex& tile, int64_t m, int64_t n, Nothing, const f32x4 (&v)[kEach][1]) const {
         using T4 = T __attribute__((ext_vector_type(4)));
         if (m >= args.m) return;
         const int64_t padded = (args.n + 3) / 4 * 4;

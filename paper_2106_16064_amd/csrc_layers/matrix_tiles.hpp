@@ -7,9 +7,6 @@
 //                 8 elements a lane, one 16-byte read.
 //   rows of m/n   an operand that is contiguous along m or n (transposed): rows of one k, pairs of chunks (16 elements) exchanged by k.
 //                 Fragments come from the transposing reads: 16 lanes read 4 k's of 16 elements and receive 4 k's of one element each.
-// A product of float matrices takes each as the sum of three bf16 planes, 8 bits of the significand in each, and adds the six products
-// of planes that are larger than 2^-24 of the whole, smallest first: six times the matrix instructions, but these are sixteen times as
-// fast as those of float (2.5 PFLOP/s to 0.157).
 #pragma once
 
 #include "element_types.hpp"
@@ -50,16 +47,18 @@ __device__ __forceinline__ void accumulate<f16_t>(s16x8 a, s16x8 b, f32x4& c) {
     asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
 }
 
-// A matrix of 16-bit elements in memory, or three planes of one.  Address, ld, cols and plane are multiples of 8 elements, ld >= cols,
-// and 256 rows span less than 2^31 bytes.
+// A matrix in memory.  Of 16-bit elements, address, ld and cols are multiples of 8 elements, ld >= cols, and 256 rows span less than 2^31
+// bytes.
+template <typename T>
 struct Source {
-    const uint16_t* p;
-    int64_t rows, cols, ld, plane;
+    const T* p;
+    int64_t rows, cols, ld;
 };
 
+template <typename T>
 struct ProductArgs {
-    Source a[2], b[2];          // the sum runs over `pairs` of them, of equal ld; or see TileShape::kDual, `batch`
-    int pairs, planes;          // planes: 1 or 3
+    Source<T> a[2], b[2];       // the sum runs over `pairs` of them, of equal ld; or see TileShape::kDual, `batch`
+    int pairs;
     int64_t m, n, depth;
     int64_t tiles_m, tiles_n;
     int batch;                  // 2: two products, of a[0] and of a[1], with b[0]
@@ -109,9 +108,10 @@ struct Loader {
         int depth_left;         // elements of a row, along k
     };
     // row i0 along m or n, k0; `row0`: the wave's first row of the tile
-    static __device__ __forceinline__ Cursor begin(const Source& s, int plane, int64_t i0, int64_t k0, int row0) {
+    template <typename T>
+    static __device__ __forceinline__ Cursor begin(const Source<T>& s, int64_t i0, int64_t k0, int row0) {
         const int64_t origin = kAlongK ? (i0 + row0) * s.ld + k0 : (k0 + row0) * s.ld + i0, end = (s.rows - 1) * s.ld + s.cols;
-        return {reinterpret_cast<const char*>(s.p + plane * s.plane + origin), (end - origin) * 2, (int)(s.cols - k0)};
+        return {reinterpret_cast<const char*>(s.p + origin), (end - origin) * 2, (int)(s.cols - k0)};
     }
     // a stage on its way to `lds`, where the wave's rows begin
     __device__ __forceinline__ void issue(Cursor& c, int64_t ld, char* lds) const {
@@ -171,7 +171,8 @@ struct TileIndex {
     int batch, split;
 };
 
-__device__ __forceinline__ TileIndex tile_of(const ProductArgs& args) {
+template <typename T>
+__device__ __forceinline__ TileIndex tile_of(const ProductArgs<T>& args) {
     const uint32_t count = gridDim.x, id = blockIdx.x;
     const uint32_t each = count / 8, more = count % 8, xcd = id % 8;
     uint32_t t = xcd * each + (xcd < more ? xcd : more) + id / 8;
@@ -196,7 +197,7 @@ struct TileProduct {
     using BLoader = Loader<Shape::kN, kBRows, Shape::kWaves>;
     f32x4 acc[Shape::kFragsN][Shape::kFragsM];
 
-    __device__ __forceinline__ void run(const ProductArgs& args, const TileIndex& tile) {
+    __device__ __forceinline__ void run(const ProductArgs<E>& args, const TileIndex& tile) {
         // apart, so that the compiler sees that reads of one do not wait for what is on its way to the other
         __shared__ __attribute__((aligned(1024))) char first[kABytes + kBBytes];
         __shared__ __attribute__((aligned(1024))) char second[kABytes + kBBytes];
@@ -224,31 +225,25 @@ struct TileProduct {
             for (int i = 0; i < Shape::kFragsM; ++i) acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
         const int steps = k_end > k_first ? (int)((k_end - k_first + kDepth - 1) / kDepth) : 0;
-        const int products = args.planes == 3 ? 6 : 1, total = steps * products * args.pairs;
+        const int total = steps * args.pairs;
         if (total == 0) return;
-        // products of planes (1,1) (0,2) (2,0) (0,1) (1,0) (0,0), two bits each
-        constexpr uint32_t kPlanesA = 1u | 0u << 2 | 2u << 4 | 0u << 6 | 1u << 8 | 0u << 10;
-        constexpr uint32_t kPlanesB = 1u | 2u << 2 | 0u << 4 | 1u << 6 | 0u << 8 | 0u << 10;
         const int64_t a_ld = args.a[args.batch > 1 ? tile.batch : 0].ld, b_ld = args.b[side].ld;
         a_loader.init(lane, wave * kARowsEach, a_ld);
         b_loader.init(lane, b_wave * kBRowsEach, b_ld);
 
-        // stages are loaded in order: along the depth, then the next product of planes, then the next pair
-        int pair = 0, product = 0;
+        // stages are loaded in order: along the depth, then the next pair
+        int pair = 0;
         int stages_left = steps;
         typename ALoader::Cursor a_at;
         typename BLoader::Cursor b_at;
         auto enter = [&] {
-            a_at = ALoader::begin(args.a[args.batch > 1 ? tile.batch : pair], args.planes == 3 ? (kPlanesA >> (2 * product)) & 3 : 0, i0, k_first, wave * kARowsEach);
-            b_at = BLoader::begin(args.b[Shape::kDual ? side : pair], args.planes == 3 ? (kPlanesB >> (2 * product)) & 3 : 0, j0, k_first, b_wave * kBRowsEach);
+            a_at = ALoader::begin(args.a[args.batch > 1 ? tile.batch : pair], i0, k_first, wave * kARowsEach);
+            b_at = BLoader::begin(args.b[Shape::kDual ? side : pair], j0, k_first, b_wave * kBRowsEach);
         };
         enter();
         auto load = [&](char* lds) {
             if (stages_left == 0) {
-                if (++product == products) {
-                    product = 0;
-                    ++pair;
-                }
+                ++pair;
                 stages_left = steps;
                 enter();
             }
@@ -323,42 +318,42 @@ struct TileProduct {
                 asm volatile("" : "+v"(acc[j][i]));
             }
     }
-
-    // Hands the results to out.row(args, tile, m, n, more, v[j][...]), a row of fragments at a time: element m and, for fragment j, four
-    // elements from n + 16 j on; of a dual tile v[j][0] and v[j][1] are of the two results.  `more` is what out.ask(args, m, n) gave for
-    // them a row earlier.
-    template <typename Out>
-    __device__ __forceinline__ void store(const ProductArgs& args, const TileIndex& tile, const Out& out) {
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int wave_m = wave / Shape::kWavesN, wave_n = wave % Shape::kWavesN;
-        constexpr int kEach = Shape::kDual ? Shape::kFragsN / 2 : Shape::kFragsN, kResults = Shape::kDual ? 2 : 1;
-        const int64_t m = tile.m * Shape::kM + wave_m * Shape::kFragsM * 16 + lane % 16;
-        const int64_t n = tile.n * Shape::kColumns + wave_n * kEach * 16 + lane / 16 * 4;
-        auto more = out.template ask<kEach>(args, m, n);
-#pragma unroll
-        for (int i = 0; i < Shape::kFragsM; ++i) {
-            const auto have = more;
-            if (i + 1 < Shape::kFragsM) more = out.template ask<kEach>(args, m + 16 * (i + 1), n);
-            f32x4 v[kEach][kResults];
-#pragma unroll
-            for (int j = 0; j < kEach; ++j)
-#pragma unroll
-                for (int r = 0; r < kResults; ++r) v[j][r] = acc[j + r * kEach][i];
-            out.row(args, tile, m + 16 * i, n, have, v);
-        }
-    }
 };
+
+// Hands the results of a tile to out.row(args, tile, m, n, more, v[j][...]), a row of fragments at a time: element m and, for fragment j,
+// four elements from n + 16 j on; of a dual tile v[j][0] and v[j][1] are of the two results.  `more` is what out.ask(args, m, n) gave for
+// them a row earlier.
+template <typename Shape, typename T, typename Out>
+__device__ __forceinline__ void store_tile(const f32x4 (&acc)[Shape::kFragsN][Shape::kFragsM], const ProductArgs<T>& args, const TileIndex& tile, const Out& out) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave_m = wave / Shape::kWavesN, wave_n = wave % Shape::kWavesN;
+    constexpr int kEach = Shape::kDual ? Shape::kFragsN / 2 : Shape::kFragsN, kResults = Shape::kDual ? 2 : 1;
+    const int64_t m = tile.m * Shape::kM + wave_m * Shape::kFragsM * 16 + lane % 16;
+    const int64_t n = tile.n * Shape::kColumns + wave_n * kEach * 16 + lane / 16 * 4;
+    auto more = out.template ask<kEach>(args, m, n);
+#pragma unroll
+    for (int i = 0; i < Shape::kFragsM; ++i) {
+        const auto have = more;
+        if (i + 1 < Shape::kFragsM) more = out.template ask<kEach>(args, m + 16 * (i + 1), n);
+        f32x4 v[kEach][kResults];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+#pragma unroll
+            for (int r = 0; r < kResults; ++r) v[j][r] = acc[j + r * kEach][i];
+        out.row(args, tile, m + 16 * i, n, have, v);
+    }
+}
 
 struct Nothing {};
 
 // A workgroup per tile.
 template <typename E, typename Shape, bool kARows, bool kBRows, typename Out>
-__global__ __launch_bounds__(Shape::kThreads, Shape::kWavesASimd) void tile_kernel(ProductArgs args, Out out) {
+__global__ __launch_bounds__(Shape::kThreads, Shape::kWavesASimd) void tile_kernel(ProductArgs<E> args, Out out) {
 #if defined(__HIP_DEVICE_COMPILE__)         // the host's half knows neither buffers nor matrix instructions
     const TileIndex tile = tile_of(args);
     TileProduct<E, Shape, kARows, kBRows> product;
     product.run(args, tile);
-    product.store(args, tile, out);
+    store_tile<Shape>(product.acc, args, tile, out);
 #endif
 }
 
