@@ -55,11 +55,11 @@ struct Cut {
 // Which tiles.  256 x 256 read half as much per product as 128 x 128, but take a CU each, so that nothing runs while their results leave:
 // they pay where the sum is long (`terms` counts pairs of operands), there is one for every CU, and the edges waste little.  64 x 64 are
 // for what has fewer than a tile of 128 for every CU and cannot be split along the depth, or is hardly half as wide.  Where tiles are
-// fewer than CUs the depth is split, to two workgroups a CU of at least 512 each.  Float matrices have no tiles of 256: their three planes
+// fewer than CUs the depth is split, to two workgroups a CU of at least 256 each.  Float matrices have no tiles of 256: their three planes
 // of two operands do not fit the registers.
 Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, int type, bool dual, bool may_split) {
     auto tiles = [&](int size) { return ceil_div(m, size) * ceil_div(n, dual ? size / 2 : size) * batch; };
-    const bool splits = may_split && depth >= 1024;
+    const bool splits = may_split && depth >= (type == DGSP_F32 ? 512 : 1024);
     Cut c{kSmall, 0, 0, 1, padded(std::max<int64_t>(depth, 1), kDepth)};
     if (type != DGSP_F32 && tiles(kLarge) >= kCus && depth * terms >= 1024 && 4 * tiles(kLarge) <= tiles(kMiddle) + tiles(kMiddle) / 8)
         c.size = kLarge;
@@ -69,7 +69,7 @@ Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, int type, boo
     c.tiles_n = ceil_div(n, dual ? c.size / 2 : c.size);
     const int64_t count = tiles(c.size);
     if (splits && count < kCus) {
-        const int64_t most = std::min<int64_t>(ceil_div(2 * kCus, count), depth / 512);
+        const int64_t most = std::min<int64_t>(ceil_div(2 * kCus, count), depth / 256);
         c.split_depth = padded(ceil_div(depth, most), kDepth);
         c.splits = (int)ceil_div(depth, c.split_depth);
     }
@@ -191,10 +191,11 @@ struct ForwardPieces {
     Cut up, down;
     void *x, *gate, *up_weight, *down_weight, *h, *partial;
     ForwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type)
-        : up(cut(rows, hidden, width, 1, 1, type, true, false)), down(cut(rows, out_width, hidden, 1, 1, type, false, true)),
+        : up(cut(rows, hidden, width, 1, 1, type, true, true)), down(cut(rows, out_width, hidden, 1, 1, type, false, true)),
           x(pieces.take(laid_out_bytes(rows, width, type))), gate(pieces.take(laid_out_bytes(hidden, width, type))),
           up_weight(pieces.take(laid_out_bytes(hidden, width, type))), down_weight(pieces.take(laid_out_bytes(out_width, hidden, type))),
-          h(pieces.take(kept_bytes(rows, hidden, type))), partial(pieces.take(partial_bytes(down, rows, out_width, 1))) {}
+          h(pieces.take(kept_bytes(rows, hidden, type))),
+          partial(pieces.take(std::max(partial_bytes(up, rows, padded(hidden, 8), 2), partial_bytes(down, rows, out_width, 1)))) {}
 };
 
 struct BackwardPieces {
@@ -262,8 +263,11 @@ extern "C" int dgsp_gated_ff(int64_t rows, int64_t width, int64_t hidden, int64_
         down.a[0] = source(h, rows);
         down.b[0] = operands.add(w_down, out_width, hidden, ldd, at.down_weight);
         operands.launch(on);
-        launch<T, true, true, true>(at.up, up, GatedUpOut<T>{h, saved ? static_cast<float*>(keep.act) : nullptr,
-                                                             saved ? static_cast<float*>(keep.mul) : nullptr, activation}, on);
+        const GatedUpOut<T> out{h, saved ? static_cast<float*>(keep.act) : nullptr, saved ? static_cast<float*>(keep.mul) : nullptr, activation,
+                                at.up.splits > 1 ? static_cast<float*>(at.partial) : nullptr};
+        launch<T, true, true, true>(at.up, up, out, on);
+        if (out.partial)
+            gated_join_kernel<T><<<(unsigned)std::min<int64_t>(ceil_div(rows * h.ld / 4, 256), 4096), 256, 0, on>>>(rows, at.up.splits, out);
         product<T, true, true>(at.down, down, {{static_cast<T*>(y), nullptr}, ldy, false, nullptr}, at.partial, on);
         return launched();
     });

@@ -1,7 +1,7 @@
 // C(m, n) = sum over k of A(m, k) B(n, k) for matrices of 16-bit elements: tiles of C in registers, tiles of A and B in LDS.
 //
 // A stage is 64 deep.  Its tiles go from memory to LDS without passing through registers, 1 KB per wave and instruction, into one of
-// two buffers while the other one is multiplied; a barrier per stage hands the buffers over.  Each lane chooses which 16 bytes of
+// two buffers (three of small tiles) while another one is multiplied; a barrier per stage hands the buffers over.  Each lane chooses which 16 bytes of
 // memory its 16 bytes of LDS receive, and the choice spreads what the fragments' reads touch over all banks:
 //   rows of k     an operand that is contiguous along k: 128 bytes a row, 16-byte chunk c of row r at chunk c ^ (r % 8).  Fragments are
 //                 8 elements a lane, one 16-byte read.
@@ -73,7 +73,10 @@ struct TileShape {
     // the first half of a tile's kN rows is of b[0], the second of b[1], for the same kN / 2 columns of two results
     static constexpr bool kDual = kDual_;
     static constexpr int kColumns = kDual ? kN / 2 : kN;
-    static constexpr int kWavesASimd = kM == 64 ? 4 : 2;
+    static constexpr int kWavesASimd = kM == 64 ? 3 : 2;
+    // Small tiles are of products that read more than they multiply, by few workgroups: one token at width 4096 reads weights at 4.2 TB/s
+    // with a stage on its way and at 4.9 with two.
+    static constexpr int kBuffers = kM == 64 ? 3 : 2;
 };
 
 // Moves a stage of one operand to LDS: kRows elements along m or n.
@@ -201,6 +204,7 @@ struct TileProduct {
         // apart, so that the compiler sees that reads of one do not wait for what is on its way to the other
         __shared__ __attribute__((aligned(1024))) char first[kABytes + kBBytes];
         __shared__ __attribute__((aligned(1024))) char second[kABytes + kBBytes];
+        __shared__ __attribute__((aligned(1024))) char third[Shape::kBuffers > 2 ? kABytes + kBBytes : 16];
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int wave_m = wave / Shape::kWavesN, wave_n = wave % Shape::kWavesN;
 
@@ -258,9 +262,15 @@ struct TileProduct {
                 f[j] = b_reader.read(lds + kABytes + j / kEach * (kBBytes / 2), s, j % kEach);     // the second half's rows lie kN / 2 rows on
             }
         };
-        // what this wave has asked for has arrived, and all waves are here
-        auto arrive = [&] {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // what this wave has asked for has arrived, but for the latest `later` stages, and all waves are here
+        constexpr int kOfAStage = ALoader::kInstructions + BLoader::kInstructions;
+        auto arrive = [&](int later) {
+            if (later <= 0)
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            else if (Shape::kBuffers == 2 || later == 1)
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kOfAStage) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * kOfAStage) : "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
@@ -274,12 +284,13 @@ struct TileProduct {
             for (int j = 0; j < Shape::kFragsN; ++j) accumulate<E>(b[j], a[i], acc[j][i]);
         };
         load(first);
-        arrive();
         if (total > 1) load(second);
+        if (Shape::kBuffers > 2 && total > 2) load(third);
+        arrive(min(total, Shape::kBuffers) - 1);
         read_b(first, 0, b_low);
 #pragma unroll
         for (int i = 0; i < Shape::kFragsM; ++i) a[i] = a_reader.read(first, 0, i);
-        auto stage = [&](char* here, char* other, bool more) {
+        auto stage = [&](char* here, char* other, int number) {
             read_b(here, 1, b_high);
 #pragma unroll
             for (int i = 0; i < Shape::kFragsM; ++i) {
@@ -290,8 +301,8 @@ struct TileProduct {
 #pragma unroll
             for (int i = 0; i < kEarly; ++i) multiply_row(i, b_high);
             __builtin_amdgcn_sched_barrier(0);
-            arrive();
-            if (more) load(here);
+            arrive(min(total - 2 - number, Shape::kBuffers - 2));
+            if (number + Shape::kBuffers < total) load(here);
             read_b(other, 0, b_low);
 #pragma unroll
             for (int i = 0; i < kEarly; ++i) a[i] = a_reader.read(other, 0, i);
@@ -304,11 +315,14 @@ struct TileProduct {
             }
         };
         int step = 0;
-        for (; step + 2 <= total; step += 2) {
-            stage(first, second, step + 2 < total);
-            stage(second, first, step + 3 < total);
+        for (; step + Shape::kBuffers <= total; step += Shape::kBuffers) {
+            stage(first, second, step);
+            stage(second, Shape::kBuffers > 2 ? third : first, step + 1);
+            if constexpr (Shape::kBuffers > 2) stage(third, first, step + 2);
         }
-        if (step < total) stage(first, second, false);
+        if (step < total) stage(first, second, step++);
+        if constexpr (Shape::kBuffers > 2)
+            if (step < total) stage(second, third, step);
         // other instructions may read a result 11 cycles after its matrix instruction has begun; the compiler does not see these
 #pragma unroll
         for (int i = 0; i < Shape::kFragsM; ++i)
