@@ -55,8 +55,9 @@ struct Cut {
 // Which tiles.  256 x 256 read half as much per product as 128 x 128, but take a CU each, so that nothing runs while their results leave:
 // they pay where the sum is long (`terms` counts pairs of operands), there is one for every CU, and the edges waste little.  64 x 64 are
 // for what has fewer than a tile of 128 for every CU and cannot be split along the depth, or is hardly half as wide.  Where tiles are
-// fewer than CUs the depth is split, to two workgroups a CU of at least 256 each.  Float matrices have no tiles of 256: their three planes
-// of two operands do not fit the registers.
+// fewer than CUs the depth is split, to as many workgroups as are resident together (two of 128, three of 64 a CU; one token, 4096 x
+// 16384: 97, 88, 81 and 88 us with one to four a CU), down to 256 each, of float matrices 128.  Float matrices have no tiles of 256:
+// their three planes of two operands do not fit the registers.
 Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, int type, bool dual, bool may_split) {
     auto tiles = [&](int size) { return ceil_div(m, size) * ceil_div(n, dual ? size / 2 : size) * batch; };
     const bool splits = may_split && depth >= (type == DGSP_F32 ? 512 : 1024);
@@ -69,7 +70,7 @@ Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, int type, boo
     c.tiles_n = ceil_div(n, dual ? c.size / 2 : c.size);
     const int64_t count = tiles(c.size);
     if (splits && count < kCus) {
-        const int64_t most = std::min<int64_t>(ceil_div(2 * kCus, count), depth / 256);
+        const int64_t most = std::min<int64_t>(ceil_div((c.size == kMiddle ? 2 : 3) * kCus, count), depth / (type == DGSP_F32 ? 128 : 256));
         c.split_depth = padded(ceil_div(depth, most), kDepth);
         c.splits = (int)ceil_div(depth, c.split_depth);
     }

@@ -74,8 +74,8 @@ struct TileShape {
     static constexpr bool kDual = kDual_;
     static constexpr int kColumns = kDual ? kN / 2 : kN;
     static constexpr int kWavesASimd = kM == 64 ? 3 : 2;
-    // Small tiles are of products that read more than they multiply, by few workgroups: one token at width 4096 reads weights at 4.2 TB/s
-    // with a stage on its way and at 4.9 with two.
+    // Small tiles are of products that read more than they multiply, by few workgroups: for one token at width 4096 the projections'
+    // weights come at 4.2 TB/s with one stage on its way and at 5.3 with two.
     static constexpr int kBuffers = kM == 64 ? 3 : 2;
 };
 
