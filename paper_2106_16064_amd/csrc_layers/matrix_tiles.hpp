@@ -9,7 +9,7 @@
 //                 Fragments come from the transposing reads: 16 lanes read 4 k's of 16 elements and receive 4 k's of one element each.
 #pragma once
 
-#include "element_types.hpp"
+#include "chunks.hpp"
 
 namespace dgsp {
 
@@ -35,16 +35,18 @@ __device__ __forceinline__ f32x4 multiply<f16_t>(s16x8 a, s16x8 b, f32x4 c) {
 }
 
 // c += a b in place.  The builtin leaves the compiler free to put each result into other registers than c's; with the accumulators
-// filling half of the registers, two thirds of them moved around and others were spilled.
+// filling half of the registers, two thirds of them moved around and others were spilled.  A matrix instruction may read
+// a register two cycles after another vector instruction has written it; the compiler does not know that this is one and puts nothing
+// between them.  The wait is over before the matrix unit is free again.
 template <typename E>
 __device__ __forceinline__ void accumulate(s16x8 a, s16x8 b, f32x4& c);
 template <>
 __device__ __forceinline__ void accumulate<bf16_t>(s16x8 a, s16x8 b, f32x4& c) {
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
+    asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
 }
 template <>
 __device__ __forceinline__ void accumulate<f16_t>(s16x8 a, s16x8 b, f32x4& c) {
-    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
+    asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
 }
 
 // A matrix in memory.  Of 16-bit elements, address, ld and cols are multiples of 8 elements, ld >= cols, and 256 rows span less than 2^31
@@ -116,8 +118,10 @@ struct Loader {
         const int64_t origin = kAlongK ? (i0 + row0) * s.ld + k0 : (k0 + row0) * s.ld + i0, end = (s.rows - 1) * s.ld + s.cols;
         return {reinterpret_cast<const char*>(s.p + origin), (end - origin) * 2, (int)(s.cols - k0)};
     }
-    // a stage on its way to `lds`, where the wave's rows begin
-    __device__ __forceinline__ void issue(Cursor& c, int64_t ld, char* lds) const {
+    // A stage on its way to byte `lds` of LDS, where the wave's rows begin.  The instruction is written out because the compiler waits for
+    // one of its own before any read of LDS that it cannot tell from where it goes; the waits are arrive()'s.  It has no result in
+    // registers.
+    __device__ __forceinline__ void issue(Cursor& c, int64_t ld, uint32_t lds) const {
         const bool beyond = kAlongK && chunk * 8 >= c.depth_left;           // the next row lies there
         const char* at = c.at;
         int64_t left = c.left;
@@ -126,9 +130,11 @@ struct Loader {
             // in halves, as there are no 64-bit comparisons of scalars
             const int high = (int)(left >> 32);
             const uint32_t low = (uint32_t)left, some = high > 0 ? 0x7fffffffu : low < 0x7fffffffu ? low : 0x7fffffffu;
-            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, high < 0 ? 0u : some, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + j * kWaveBytes), 16,
-                                                     beyond ? kNowhere : offset[kPatternBit < 0 ? 0 : j >> kPatternBit & 1], 0, 0, 0);
+            const uint64_t address = reinterpret_cast<uint64_t>(at);
+            const u32x4 buffer = {(uint32_t)address, (uint32_t)(address >> 32) & 0xffffu, high < 0 ? 0u : some, 0x00020000u};
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + j * kWaveBytes),
+                         "v"(beyond ? kNowhere : offset[kPatternBit < 0 ? 0 : j >> kPatternBit & 1]), "s"(buffer)
+                         : "memory");
             at += kRowsEach * 2 * ld;
             left -= kRowsEach * 2 * ld;
         }
@@ -201,10 +207,9 @@ struct TileProduct {
     f32x4 acc[Shape::kFragsN][Shape::kFragsM];
 
     __device__ __forceinline__ void run(const ProductArgs<E>& args, const TileIndex& tile) {
-        // apart, so that the compiler sees that reads of one do not wait for what is on its way to the other
-        __shared__ __attribute__((aligned(1024))) char first[kABytes + kBBytes];
-        __shared__ __attribute__((aligned(1024))) char second[kABytes + kBBytes];
-        __shared__ __attribute__((aligned(1024))) char third[Shape::kBuffers > 2 ? kABytes + kBBytes : 16];
+        constexpr uint32_t kStage = kABytes + kBBytes, kRing = Shape::kBuffers * kStage;
+        __shared__ __attribute__((aligned(1024))) char lds[kRing];
+        const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int wave_m = wave / Shape::kWavesN, wave_n = wave % Shape::kWavesN;
 
@@ -216,7 +221,7 @@ struct TileProduct {
         ALoader a_loader;
         BLoader b_loader;
         constexpr int kARowsEach = ALoader::kInstructions * ALoader::kRowsEach, kBRowsEach = BLoader::kInstructions * BLoader::kRowsEach;
-        const uint32_t a_lds = wave * ALoader::kInstructions * kWaveBytes, b_lds = kABytes + wave * BLoader::kInstructions * kWaveBytes;
+        const uint32_t a_lds = lds_at + wave * ALoader::kInstructions * kWaveBytes, b_lds = lds_at + kABytes + wave * BLoader::kInstructions * kWaveBytes;
 
         Reader<Shape::kM, kARows, Shape::kFragsM> a_reader;
         Reader<Shape::kN, kBRows, Shape::kFragsN / (Shape::kDual ? 2 : 1)> b_reader;
@@ -245,21 +250,22 @@ struct TileProduct {
             b_at = BLoader::begin(args.b[Shape::kDual ? side : pair], j0, k_first, b_wave * kBRowsEach);
         };
         enter();
-        auto load = [&](char* lds) {
+        auto load = [&](uint32_t buffer) {
             if (stages_left == 0) {
                 ++pair;
                 stages_left = steps;
                 enter();
             }
             --stages_left;
-            a_loader.issue(a_at, a_ld, lds + a_lds);
-            b_loader.issue(b_at, b_ld, lds + b_lds);
+            a_loader.issue(a_at, a_ld, a_lds + buffer);
+            b_loader.issue(b_at, b_ld, b_lds + buffer);
         };
-        auto read_b = [&](const char* lds, int s, s16x8 (&f)[Shape::kFragsN]) {
+        auto read_a = [&](uint32_t buffer, int s, int i) { return a_reader.read(lds + buffer, s, i); };
+        auto read_b = [&](uint32_t buffer, int s, s16x8 (&f)[Shape::kFragsN]) {
 #pragma unroll
             for (int j = 0; j < Shape::kFragsN; ++j) {
                 constexpr int kEach = Shape::kDual ? Shape::kFragsN / 2 : Shape::kFragsN;
-                f[j] = b_reader.read(lds + kABytes + j / kEach * (kBBytes / 2), s, j % kEach);     // the second half's rows lie kN / 2 rows on
+                f[j] = b_reader.read(lds + buffer + kABytes + j / kEach * (kBBytes / 2), s, j % kEach);     // the second half's rows lie kN / 2 rows on
             }
         };
         // what this wave has asked for has arrived, but for the latest `later` stages, and all waves are here
@@ -283,46 +289,45 @@ struct TileProduct {
 #pragma unroll
             for (int j = 0; j < Shape::kFragsN; ++j) accumulate<E>(b[j], a[i], acc[j][i]);
         };
-        load(first);
-        if (total > 1) load(second);
-        if (Shape::kBuffers > 2 && total > 2) load(third);
+        for (int i = 0; i < min(total, Shape::kBuffers); ++i) load(i * kStage);
         arrive(min(total, Shape::kBuffers) - 1);
-        read_b(first, 0, b_low);
+        read_b(0, 0, b_low);
 #pragma unroll
-        for (int i = 0; i < Shape::kFragsM; ++i) a[i] = a_reader.read(first, 0, i);
-        auto stage = [&](char* here, char* other, int number) {
-            read_b(here, 1, b_high);
+        for (int i = 0; i < Shape::kFragsM; ++i) a[i] = read_a(0, 0, i);
+        // the first half, and as much of the second as its last fragments take to arrive
+        auto first_half = [&](uint32_t buffer) {
+            read_b(buffer, 1, b_high);
 #pragma unroll
             for (int i = 0; i < Shape::kFragsM; ++i) {
                 multiply_row(i, b_low);
-                a[i] = a_reader.read(here, 1, i);
+                a[i] = read_a(buffer, 1, i);
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int i = 0; i < kEarly; ++i) multiply_row(i, b_high);
             __builtin_amdgcn_sched_barrier(0);
-            arrive(min(total - 2 - number, Shape::kBuffers - 2));
-            if (number + Shape::kBuffers < total) load(here);
-            read_b(other, 0, b_low);
+        };
+        uint32_t here = 0;
+        first_half(here);
+        for (int step = 0; step + 1 < total; ++step) {          // begins where no read is on its way that has to be waited for
+            const uint32_t next = here + kStage == kRing ? 0 : here + kStage;
+            arrive(min(total - 2 - step, Shape::kBuffers - 2));
+            if (step + Shape::kBuffers < total) load(here);
+            read_b(next, 0, b_low);
 #pragma unroll
-            for (int i = 0; i < kEarly; ++i) a[i] = a_reader.read(other, 0, i);
+            for (int i = 0; i < kEarly; ++i) a[i] = read_a(next, 0, i);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = kEarly; i < Shape::kFragsM; ++i) {
                 multiply_row(i, b_high);
-                a[i] = a_reader.read(other, 0, i);
+                a[i] = read_a(next, 0, i);
                 __builtin_amdgcn_sched_barrier(0);
             }
-        };
-        int step = 0;
-        for (; step + Shape::kBuffers <= total; step += Shape::kBuffers) {
-            stage(first, second, step);
-            stage(second, Shape::kBuffers > 2 ? third : first, step + 1);
-            if constexpr (Shape::kBuffers > 2) stage(third, first, step + 2);
+            here = next;
+            first_half(here);
         }
-        if (step < total) stage(first, second, step++);
-        if constexpr (Shape::kBuffers > 2)
-            if (step < total) stage(second, third, step);
+#pragma unroll
+        for (int i = kEarly; i < Shape::kFragsM; ++i) multiply_row(i, b_high);
         // other instructions may read a result 11 cycles after its matrix instruction has begun; the compiler does not see these
 #pragma unroll
         for (int i = 0; i < Shape::kFragsM; ++i)
