@@ -32,43 +32,86 @@ __device__ __forceinline__ void split3(float v, bf16_t (&out)[3]) {
     out[2] = (bf16_t)(rest - (float)out[1]);
 }
 
-// A stage of one operand: kRows elements along m or n, kStage along k.
+// Eight of them.  Two at a time, 6 instructions each; where that made an infinity, or met one or a NaN, the last rest is NaN, and they are split one by
+// one (with each tested by itself the splitting took twice as long as the products).
+__device__ __forceinline__ void split_chunk(const RawChunk<float>& v, u32x4 (&out)[3]) {
+    using F2 = float __attribute__((ext_vector_type(2)));
+    using E2 = bf16_t __attribute__((ext_vector_type(2)));
+    float rests = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float low = v.at(2 * j), high = v.at(2 * j + 1);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            const uint32_t part = __builtin_bit_cast(uint32_t, __builtin_convertvector((F2{low, high}), E2));
+            out[q][j] = part;
+            if (q == 2) break;
+            low -= __builtin_bit_cast(float, part << 16);
+            high -= __builtin_bit_cast(float, part & 0xffff0000u);
+        }
+        rests += low + high;
+    }
+    if (__builtin_amdgcn_ballot_w64(rests != rests) == 0) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        bf16_t parts[3];
+        split3(v.at(j), parts);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            const uint32_t part = __builtin_bit_cast(uint16_t, parts[q]);
+            out[q][j / 2] = j % 2 ? (out[q][j / 2] & 0xffffu) | part << 16 : part;
+        }
+    }
+}
+
+// A stage of one operand: kRows elements along m or n, kStage along k.  Where all of it is inside the matrix a load is an address of the
+// whole stage's plus an offset of the thread's, which stays; else every chunk is looked at.
 template <int kRows, int kStage, bool kAlongK, int kThreads>
 struct FloatLoader {
     static constexpr int kChunks = kAlongK ? kStage / 8 : kRows / 8;            // of 8 elements in a row of a plane
+    static constexpr int kRowsEach = kThreads / kChunks;                        // that the threads take at a time
     static constexpr int kEach = kRows * kStage / 8 / kThreads;                 // chunks a thread
     static constexpr int kPlane = kRows * kStage * 2;                           // bytes
+    static constexpr int64_t kMostLd = (1LL << 22) - 8;                         // 128 rows span less than 2^31 bytes
     RawChunk<float> kept[kEach];
+    uint32_t offset[kEach];
 
     // with what the number of a row's chunk along k is exchanged
     static __device__ __forceinline__ int turn(int row) { return kStage == 64 ? row & 7 : row >> 1 & 3; }
     static __device__ __forceinline__ int exchange(int k) { return ((k & 3) + 4 * ((k >> 3) & 3)) & (kRows / 16 - 1); }
 
-    // `row0` and the rest as of the half of a dual tile that these rows are of
+    __device__ __forceinline__ void init(int e, int64_t ld, int first_row) {
+        const int row = threadIdx.x / kChunks + e * kRowsEach - first_row, chunk = threadIdx.x % kChunks;
+        offset[e] = ((uint32_t)row * (uint32_t)ld + chunk * 8) * 4;
+    }
+    // `count` of the tile's elements along m or n from i0 on, and the stage from k0 on
+    static __device__ __forceinline__ bool whole(const Source<float>& s, int64_t i0, int64_t k0, int count) {
+        return s.ld <= kMostLd && (kAlongK ? i0 : k0) + (kAlongK ? count : kStage) <= s.rows && (kAlongK ? k0 : i0) + (kAlongK ? kStage : count) <= s.cols;
+    }
+    static __device__ __forceinline__ const float* begin(const Source<float>& s, int64_t i0, int64_t k0) {
+        return s.p + (kAlongK ? i0 * s.ld + k0 : k0 * s.ld + i0);
+    }
+    __device__ __forceinline__ void ask_whole(int e, const float* from) {
+        const auto* p = reinterpret_cast<const ChunkInMemory<float>*>(reinterpret_cast<const char*>(from) + offset[e]);
+#pragma unroll
+        for (int i = 0; i < RawChunk<float>::kQuads; ++i) kept[e].q[i] = p->q[i];
+    }
     __device__ __forceinline__ void ask(int e, const Source<float>& s, int64_t i0, int64_t k0, int first_row) {
-        const int c = threadIdx.x + e * kThreads, row = c / kChunks - (kAlongK ? first_row : 0), chunk = c % kChunks;
+        const int row = threadIdx.x / kChunks + e * kRowsEach - first_row, chunk = threadIdx.x % kChunks;
         const int64_t at = (kAlongK ? i0 : k0) + row, col = (kAlongK ? k0 : i0) + chunk * 8;
         const bool inside = at < s.rows && col < s.cols;
         kept[e] = load_chunk(s.p + (inside ? at * s.ld + col : 0), inside ? s.cols - col : 0);
     }
-    // which row of the tile chunk `e` of this thread is of
-    static __device__ __forceinline__ int row_of(int e) { return (threadIdx.x + e * kThreads) / kChunks; }
 
     __device__ __forceinline__ void leave(char* lds) const {
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             const int c = threadIdx.x + e * kThreads, row = c / kChunks, chunk = c % kChunks;
             const int to = kAlongK ? chunk ^ turn(row) : (((chunk >> 1) ^ exchange(row)) << 1) + (chunk & 1);
-            using E8 = bf16_t __attribute__((ext_vector_type(8)));
-            E8 out[3];
+            u32x4 out[3];
+            split_chunk(kept[e], out);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                bf16_t parts[3];
-                split3(kept[e].at(j), parts);
-                for (int q = 0; q < 3; ++q) out[q][j] = parts[q];
-            }
-#pragma unroll
-            for (int q = 0; q < 3; ++q) *reinterpret_cast<E8*>(lds + q * kPlane + row * kChunks * 16 + to * 16) = out[q];
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x4*>(lds + q * kPlane + row * kChunks * 16 + to * 16) = out[q];
         }
     }
 };
@@ -127,21 +170,43 @@ __global__ __launch_bounds__(Shape::kThreads, 2) void float_tile_kernel(ProductA
 #pragma unroll
         for (int i = 0; i < Shape::kFragsM; ++i) acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    auto ask = [&](int pair, int64_t k) {
-        const Source<float>& a = args.a[args.batch > 1 ? tile.batch : pair];
-#pragma unroll
-        for (int e = 0; e < ALoader::kEach; ++e) a_loader.ask(e, a, i0, k, 0);
-#pragma unroll
-        for (int e = 0; e < BLoader::kEach; ++e) {
-            // the first half of a dual tile's rows is of b[0], the second of b[1]
-            const int half = Shape::kDual && BLoader::row_of(e) >= Shape::kN / 2;
-            b_loader.ask(e, args.b[Shape::kDual ? half : pair], j0, k, half * (Shape::kN / 2));
-        }
-    };
+    // the first half of a dual tile's rows is of b[0], the second of b[1]
+    constexpr int kSides = Shape::kDual ? 2 : 1, kSideRows = Shape::kN / kSides;
+    static_assert(kSideRows % BLoader::kRowsEach == 0 || !Shape::kDual);
+    constexpr int kEachSide = Shape::kDual ? kSideRows / BLoader::kRowsEach : BLoader::kEach;
+    Source<float> a_now, b_now[kSides];
     int pair = 0;
     int64_t k = k_first;
+    auto enter = [&] {
+        a_now = args.a[args.batch > 1 ? tile.batch : pair];
+#pragma unroll
+        for (int e = 0; e < ALoader::kEach; ++e) a_loader.init(e, a_now.ld, 0);
+#pragma unroll
+        for (int side = 0; side < kSides; ++side) b_now[side] = args.b[Shape::kDual ? side : pair];
+#pragma unroll
+        for (int e = 0; e < BLoader::kEach; ++e) b_loader.init(e, b_now[e / kEachSide].ld, e / kEachSide * kSideRows);
+    };
+    auto ask = [&] {
+        bool whole = ALoader::whole(a_now, i0, k, Shape::kM);
+#pragma unroll
+        for (int side = 0; side < kSides; ++side) whole = whole && BLoader::whole(b_now[side], j0, k, kSideRows);
+        if (whole) {
+#pragma unroll
+            for (int e = 0; e < ALoader::kEach; ++e) a_loader.ask_whole(e, ALoader::begin(a_now, i0, k));
+#pragma unroll
+            for (int e = 0; e < BLoader::kEach; ++e) b_loader.ask_whole(e, BLoader::begin(b_now[e / kEachSide], j0, k));
+        } else {
+#pragma unroll
+            for (int e = 0; e < ALoader::kEach; ++e) a_loader.ask(e, a_now, i0, k, 0);
+#pragma unroll
+            for (int e = 0; e < BLoader::kEach; ++e) b_loader.ask(e, b_now[e / kEachSide], j0, k, e / kEachSide * kSideRows);
+        }
+    };
     bool more = k < k_end;
-    if (more) ask(pair, k);
+    if (more) {
+        enter();
+        ask();
+    }
     while (more) {
         __syncthreads();                                        // the last stage has been read
         a_loader.leave(a_lds);
@@ -150,10 +215,10 @@ __global__ __launch_bounds__(Shape::kThreads, 2) void float_tile_kernel(ProductA
         k += kStage;
         if (k >= k_end) {
             k = k_first;
-            ++pair;
+            more = ++pair < args.pairs;
+            if (more) enter();
         }
-        more = pair < args.pairs;
-        if (more) ask(pair, k);
+        if (more) ask();
 #pragma unroll
         for (int s = 0; s < kStage / 32; ++s) {
             s16x8 b[3][Shape::kFragsN];
