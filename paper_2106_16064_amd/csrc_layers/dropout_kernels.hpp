@@ -17,45 +17,29 @@ struct Divisor {
     __device__ __forceinline__ uint32_t quotient(uint32_t a) const { return (uint32_t)(((uint64_t)a * magic >> 32) + a) >> shift; }
 };
 
-template <typename T, int kEach>
+template <typename T>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(int64_t rows, int64_t width, Divisor chunks, DropMask mask, const T* x, int64_t ldx,
                                                                const T* residual, int64_t ldr, T* y, int64_t ldy) {
     const uint64_t offset = mask.device_offset ? *mask.device_offset : mask.offset;
     const int64_t total = rows * (int64_t)chunks.by;
-    for (int64_t first = (int64_t)blockIdx.x * (kDropThreads * kEach); first < total; first += (int64_t)gridDim.x * (kDropThreads * kEach)) {
+    for (int64_t first = (int64_t)blockIdx.x * kDropThreads; first < total; first += (int64_t)gridDim.x * kDropThreads) {
         const int64_t row0 = first / chunks.by;
-        const uint32_t in_row = (uint32_t)(first - row0 * chunks.by);
-        RawChunk<T> a[kEach], b[kEach];
-        int64_t row[kEach];
-        uint32_t chunk[kEach];
-        bool inside[kEach];
+        const uint32_t at = (uint32_t)(first - row0 * chunks.by) + threadIdx.x, down = chunks.quotient(at), chunk = at - down * chunks.by;
+        const int64_t row = row0 + down, col = (int64_t)chunk * kChunk, here = width - col;
+        if (row >= rows) continue;
+        const RawChunk<T> in = load_chunk(x + row * ldx + col, here);
+        RawChunk<T> other;
+        if (residual) other = load_chunk(residual + row * ldr + col, here);
+        float v[kChunk];
+        widen(in, v);
+        if (mask.dropped) drop(mask, offset, row, chunk, v);
+        if (residual) {
+            float r[kChunk];
+            widen(other, r);
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const uint32_t at = in_row + e * kDropThreads + threadIdx.x, down = chunks.quotient(at);
-            row[e] = row0 + down;
-            chunk[e] = at - down * chunks.by;
-            inside[e] = row[e] < rows;
-            const int64_t col = (int64_t)chunk[e] * kChunk;
-            if (inside[e]) {
-                a[e] = load_chunk(x + row[e] * ldx + col, width - col);
-                if (residual) b[e] = load_chunk(residual + row[e] * ldr + col, width - col);
-            }
+            for (int j = 0; j < kChunk; ++j) v[j] += r[j];
         }
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            if (!inside[e]) continue;
-            const int64_t col = (int64_t)chunk[e] * kChunk;
-            float v[kChunk];
-            widen(a[e], v);
-            if (mask.dropped) drop(mask, offset, row[e], chunk[e], v);
-            if (residual) {
-                float r[kChunk];
-                widen(b[e], r);
-#pragma unroll
-                for (int j = 0; j < kChunk; ++j) v[j] += r[j];
-            }
-            store_chunk(y + row[e] * ldy + col, width - col, v);
-        }
+        store_chunk(y + row * ldy + col, here, v);
     }
 }
 

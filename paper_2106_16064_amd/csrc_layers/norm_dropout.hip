@@ -83,18 +83,13 @@ extern "C" int dgsp_dropout(int64_t rows, int64_t width, int type, const dgsp_dr
     if (!readable(x, rows, width, ldx) || (residual && !readable(residual, rows, width, ldr)) || !writable(y, rows, width, ldy))
         return DGSP_ERR_INVALID_ARG;
     const int64_t chunks = ceil_div(width, kChunk), total = rows * chunks;
-    // four chunks a lane keep more loads in flight, where there is work for every lane of the machine
-    const int each = total >= kCus * 2048 * 4 ? 4 : 1;
-    const unsigned groups = (unsigned)std::min<int64_t>(ceil_div(total, kDropThreads * each), 1 << 23);
+    const unsigned groups = (unsigned)std::min<int64_t>(ceil_div(total, kDropThreads), 1 << 23);
     return with_type(type, [&](auto element) {
         using T = decltype(element);
         const auto *in = static_cast<const T*>(x), *add = static_cast<const T*>(residual);
         const auto on = static_cast<hipStream_t>(stream);
         const Divisor divisor((uint32_t)chunks);
-        if (each == 4)
-            dropout_kernel<T, 4><<<groups, kDropThreads, 0, on>>>(rows, width, divisor, mask, in, ldx, add, ldr, static_cast<T*>(y), ldy);
-        else
-            dropout_kernel<T, 1><<<groups, kDropThreads, 0, on>>>(rows, width, divisor, mask, in, ldx, add, ldr, static_cast<T*>(y), ldy);
+        dropout_kernel<T><<<groups, kDropThreads, 0, on>>>(rows, width, divisor, mask, in, ldx, add, ldr, static_cast<T*>(y), ldy);
         return launched();
     });
 }
