@@ -21,7 +21,7 @@ struct Padded {
         p = most <= 32 ? 32 : most <= 64 ? 64 : 128;
         h = hidden <= 64 ? 64 : hidden <= 128 ? 128 : 256;
         fits = most <= 128 && hidden <= 256 && p * h <= 64 * 256;
-        waves = p * h == 64 * 256 || (p < 128 && h == 64) ? 4 : 8;
+        waves = (p == 64 && h == 256) || h == 64 ? 4 : 8;
         groups_a_cu = p < 128 && h == 64 ? 2 : 1;
     }
     int64_t groups(int64_t rows) const { return std::max<int64_t>(1, std::min(ceil_div(rows, 16 * waves), kCus * groups_a_cu)); }
@@ -131,9 +131,9 @@ int backward(const NarrowCall& call, hipStream_t stream) {
         else if (at.p == 64)
             launch_backward_staged<E, 64, 256, 4>(args, groups, stream);
         else if (at.h == 64)
-            launch_backward_staged<E, 128, 64, 8>(args, groups, stream);
+            launch_backward<E, 128, 4>(args, groups, stream);
         else
-            launch_backward_staged<E, 128, 128, 4>(args, groups, stream);
+            launch_backward<E, 128, 8>(args, groups, stream);
     }
     if (weights)
         narrow_join_kernel<E><<<(unsigned)(at.gradients() / kNarrowColumns), kNarrowColumns * kNarrowSlices, 0, stream>>>(

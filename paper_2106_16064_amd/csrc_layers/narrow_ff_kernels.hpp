@@ -306,6 +306,7 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs
     constexpr int kH = 16 * kWaves, kRows = 16 * kWaves, kSteps = kP / 32, kOut = kP / 16, kParts = kH / 32;
     constexpr int kLd = kP + 8, kLdT = kRows + 8;
     constexpr int kShare = kWaves / kOut > 0 ? kWaves / kOut : 1;          // waves that share 16 columns of dx
+    constexpr int kTurns = kOut / kWaves > 0 ? kOut / kWaves : 1;          // blocks of 16 columns that a wave takes
     using Shape = NarrowShape<E, kP, kH, kWaves>;
     __shared__ __attribute__((aligned(16))) uint16_t x_rows[kRows * kLd], dy_rows[kRows * kLd], dg_columns[kH * kLdT], du_columns[kH * kLdT];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane / 16, own = lane % 16;
@@ -316,8 +317,8 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs
         return row < rows && col < cols ? __builtin_bit_cast(short, w[row * ld + col]) : (short)0;
     };
     // weights: of this wave's hidden values along width and out_width, and of its columns of dx along hidden
-    s16x8 gate[kSteps], up[kSteps], down[kSteps], gate_columns[kParts], up_columns[kParts];
-    const int64_t hid = 16 * wave + own, col = 16 * (wave / kShare) + own;
+    s16x8 gate[kSteps], up[kSteps], down[kSteps], gate_columns[kTurns][kParts], up_columns[kTurns][kParts];
+    const int64_t hid = 16 * wave + own;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
 #pragma unroll
@@ -328,13 +329,15 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs
             down[s][j] = element(a.w_down, a.ldd, k, a.out_width, hid, a.hidden);
         }
 #pragma unroll
-    for (int t = 0; t < kParts; ++t)
+    for (int c = 0; c < kTurns; ++c)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int64_t k = 32 * t + 8 * q + j;
-            gate_columns[t][j] = element(a.w_gate, a.ldg, k, a.hidden, col, a.width);
-            up_columns[t][j] = element(a.w_up, a.ldu, k, a.hidden, col, a.width);
-        }
+        for (int t = 0; t < kParts; ++t)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int64_t k = 32 * t + 8 * q + j, col = 16 * (wave / kShare + c * kWaves) + own;
+                gate_columns[c][t][j] = element(a.w_gate, a.ldg, k, a.hidden, col, a.width);
+                up_columns[c][t][j] = element(a.w_up, a.ldu, k, a.hidden, col, a.width);
+            }
 
     f32x4 dw[3][kOut] = {};
     s16x8 next_x[kSteps], next_dy[kSteps];
@@ -401,15 +404,22 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs
         if (a.dx && wave / kShare < kOut) {
 #pragma unroll
             for (int r0 = wave % kShare * 16; r0 < kRows; r0 += kShare * 16) {
-                f32x4 dx = {};
+                f32x4 dx[kTurns] = {};
 #pragma unroll
                 for (int t = 0; t < kParts; ++t) {
                     const int at = (32 * t + 8 * q) * kLdT + r0;
-                    dx = multiply<E>(gate_columns[t], join(read_column(dg_columns + at, kLdT, lane), read_column(dg_columns + at + 4 * kLdT, kLdT, lane)), dx);
-                    dx = multiply<E>(up_columns[t], join(read_column(du_columns + at, kLdT, lane), read_column(du_columns + at + 4 * kLdT, kLdT, lane)), dx);
+                    const s16x8 dg = join(read_column(dg_columns + at, kLdT, lane), read_column(dg_columns + at + 4 * kLdT, kLdT, lane));
+                    const s16x8 du = join(read_column(du_columns + at, kLdT, lane), read_column(du_columns + at + 4 * kLdT, kLdT, lane));
+#pragma unroll
+                    for (int c = 0; c < kTurns; ++c) {
+                        dx[c] = multiply<E>(gate_columns[c][t], dg, dx[c]);
+                        dx[c] = multiply<E>(up_columns[c][t], du, dx[c]);
+                    }
                 }
                 const int64_t row = tile + r0 + own;
-                if (row < a.rows) store4<E, kFull>(a.dx + row * a.width, 16 * (wave / kShare) + 4 * q, a.width, dx);
+                if (row < a.rows)
+#pragma unroll
+                    for (int c = 0; c < kTurns; ++c) store4<E, kFull>(a.dx + row * a.width, 16 * (wave / kShare + c * kWaves) + 4 * q, a.width, dx[c]);
             }
         }
     }
