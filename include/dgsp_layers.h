@@ -95,8 +95,12 @@ int64_t dgsp_layer_norm_backward_workspace_bytes(int64_t rows, int64_t width);
  *   x        rows x width;   w_gate, w_up  hidden x width;   w_down  out_width x hidden;   y  rows x out_width
  *   saved    dgsp_gated_ff_saved_bytes(...) bytes, 16-byte aligned, for the backward pass; NULL: not wanted
  *   workspace  dgsp_gated_ff_workspace_bytes(...) bytes, 16-byte aligned
- * Of 16-bit types h, and what is saved, is rounded to `type`, as the matrix instructions take their operands.
- * rows is below 2^31 - 4096, the three widths are at least 1 and below 2^28.
+ * Either size may be 0; the pointer is not looked at then.  (Blocks whose weights fit a CU's LDS make g, u and h again.)
+ * Of 16-bit types h is rounded to `type`, as the matrix instructions take their operands; act(g) and u act'(g) are saved in
+ * 32 bits.  Products of float matrices are sums of products of three bfloat16 parts of each number, as exact as 32-bit
+ * arithmetic; an infinity or NaN in an operand makes infinity or NaN of the results that it belongs to, which of the two is
+ * not said.
+ * rows is below 2^31 - 4096, the three widths are at least 1 and below 2^22 - 7.
  */
 int dgsp_gated_ff(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type, int activation, const void *x,
                   int64_t ldx, const void *w_gate, int64_t ldg, const void *w_up, int64_t ldu, const void *w_down, int64_t ldd,

@@ -54,10 +54,16 @@ struct Cut {
 
 // Which tiles.  256 x 256 read half as much per product as 128 x 128, but take a CU each, so that nothing runs while their results leave:
 // they pay where the sum is long (`terms` counts pairs of operands), there is one for every CU, and the edges waste little.  64 x 64 are
-// for what has fewer than a tile of 128 for every CU and cannot be split along the depth, or is hardly half as wide.  Where tiles are
-// fewer than CUs the depth is split, to as many workgroups as are resident together (two of 128, three of 64 a CU; one token, 4096 x
-// 16384: 97, 88, 81 and 88 us with one to four a CU), down to 256 each, of float matrices 128.  Float matrices have no tiles of 256:
-// their three planes of two operands do not fit the registers.
+// for what has fewer than a tile of 128 for every CU and cannot be split along the depth, or is hardly half as wide.  Forward and backward
+// pass, bfloat16, us, by this rule, without 256 and with 64 alone:
+//     8192 rows, 4096 -> 16384 -> 4096      8900   11000   19300
+//     65536 rows, 256 -> 1024 -> 256         739     749     942
+//     2048 rows, 1024 -> 4096 -> 1024        221     224     286
+//     256 rows, 4096 -> 16384 -> 4096        572     573     821
+// and 256 alone in float, 65536 rows, 128 -> 512 -> 128, made the slopes 284 us where 128 took 231: float has no tiles of 256 (with 64
+// alone it takes 776 us, by this rule 638).  Where tiles are fewer than CUs the depth is split, to as many workgroups as are resident
+// together (two of 128, three of 64 a CU; one token, 4096 -> 16384: 97, 88, 81 and 88 us with one to four a CU), down to 256 each, of
+// float matrices 128.
 Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, int type, bool dual, bool may_split) {
     auto tiles = [&](int size) { return ceil_div(m, size) * ceil_div(n, dual ? size / 2 : size) * batch; };
     const bool splits = may_split && depth >= (type == DGSP_F32 ? 512 : 1024);
