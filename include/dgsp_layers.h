@@ -75,7 +75,10 @@ int dgsp_layer_norm(int64_t rows, int64_t width, int type, int param_type, const
  * Its gradient.  With hat = (s - mean) / sqrt(var + eps) and dhat = dy * weight:
  *     dsum = (dhat - mean(dhat) - hat mean(dhat hat)) / sqrt(var + eps) + ds
  *     dweight = sum over the rows of dy hat,   dbias = sum over the rows of dy
- *   s, stats   what the forward pass normalised (x, or the rounded sum it wrote) and its statistics
+ *   s          what the forward pass normalised: x, or the sum it wrote, which is rounded
+ *   residual   if not NULL, s is the forward pass's x and the sum is made again from both, which costs the reading of one
+ *              more matrix; with 16-bit types the rounded one would double the squared error of dweight
+ *   stats      the forward pass's statistics
  *   ds         gradient of the result `sum`, NULL: none
  *   dropout    that of the forward pass, NULL: none
  *   dsum       gradient of s: that of x without a residual, that of the residual with one
@@ -84,7 +87,8 @@ int dgsp_layer_norm(int64_t rows, int64_t width, int type, int param_type, const
  *   workspace  dgsp_layer_norm_backward_workspace_bytes(rows, width) bytes, 16-byte aligned
  */
 int dgsp_layer_norm_backward(int64_t rows, int64_t width, int type, int param_type, const void *s, int64_t lds,
-                             const float *stats, const void *weight, const void *dy, int64_t lddy, const void *ds, int64_t ldds,
+                             const void *residual, int64_t ldr, const float *stats, const void *weight, const void *dy,
+                             int64_t lddy, const void *ds, int64_t ldds,
                              const dgsp_dropout_t *dropout, void *dsum, void *dx, void *dweight, void *dbias, void *workspace,
                              int64_t workspace_bytes, void *stream);
 int64_t dgsp_layer_norm_backward_workspace_bytes(int64_t rows, int64_t width);

@@ -94,10 +94,13 @@ __device__ __forceinline__ void load_params(const void* p, bool wide, int64_t co
     }
 }
 
-__device__ __forceinline__ void drop(const DropMask& mask, uint64_t offset, int64_t row, int64_t chunk, float (&v)[kChunk]) {
-    const uint32_t keep = keep_bits(mask, offset, (uint32_t)row, (uint32_t)chunk);
+__device__ __forceinline__ void keep(uint32_t bits, float scale, float (&v)[kChunk]) {
 #pragma unroll
-    for (int j = 0; j < kChunk; ++j) v[j] = (keep >> j & 1) ? v[j] * mask.scale : 0.0f;
+    for (int j = 0; j < kChunk; ++j) v[j] = bits >> j & 1 ? v[j] * scale : 0.0f;
+}
+
+__device__ __forceinline__ void drop(const DropMask& mask, uint64_t offset, int64_t row, int64_t chunk, float (&v)[kChunk]) {
+    keep(keep_bits(mask, offset, (uint32_t)row, (uint32_t)chunk), mask.scale, v);
 }
 
 }  // namespace dgsp

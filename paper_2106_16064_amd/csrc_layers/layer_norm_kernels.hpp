@@ -5,7 +5,7 @@
 // registers of a full CU.  Memory bounds it (a large copy: 4.96 TB/s):
 //     float, 2^20 rows of 32:               forward 54 us, 5.0 TB/s; gradient 80 us, 5.0 TB/s, and 4 us for the parameters' sums
 //     bfloat16, 8192 rows of 8192:          forward 70 us, 3.8 TB/s; gradient 77 us, 5.2 TB/s, and 5 us: two barriers a row, 16 waves
-//     bfloat16, 32768 rows of 1024, residual and dropout:  forward 55 us, 4.9 TB/s; gradient 60 us, 5.6 TB/s (with ds and dx)
+//     bfloat16, 32768 rows of 1024, residual and dropout:  forward 53 us, 5.1 TB/s; gradient 85 us, 4.7 TB/s (with ds and dx)
 #pragma once
 
 #include "chunks.hpp"
@@ -155,8 +155,8 @@ template <typename T>
 struct NormBackwardArgs {
     int64_t rows, width;
     int lanes;
-    const T *s, *dy, *ds;
-    int64_t lds, lddy, ldds;
+    const T *s, *residual, *dy, *ds;        // with a residual `s` is x
+    int64_t lds, ldr, lddy, ldds;
     const float* stats;
     const void* weight;
     bool wide;
@@ -165,6 +165,9 @@ struct NormBackwardArgs {
     float* partial;         // [workgroup][dweight, dbias][width]; null: not wanted
 };
 
+// Where s is given as the residual and x it is made again: rounded to 16 bits it would add as much to the error of dweight as the rounding
+// of the result does.  A third more is read (bfloat16, 32768 rows of 1024: 85 us against 61).
+//
 // A lane adds up dy hat and dy of its columns over the rows it meets; a workgroup's lanes with the same columns meet in LDS, and the
 // workgroups' sums in memory, in the order of the workgroups (layer_norm_params_kernel).
 template <typename T, bool kWhole, bool kAdd>
@@ -173,14 +176,16 @@ __global__ __launch_bounds__(kWhole ? 1024 : 256) void layer_norm_backward_kerne
     const uint64_t offset = kAdd && a.mask.device_offset ? *a.mask.device_offset : a.mask.offset;
     const int64_t col = (int64_t)team.lane * kChunk, here = a.width - col;
     float w[kChunk], dw[kChunk], db[kChunk];
-    RawChunk<T> s, g, more;
+    RawChunk<T> s, r, g, more;
     float next_mean = 0.0f, next_rstd = 0.0f;
     auto ask = [&](int64_t row) {
         if (row >= a.rows || here <= 0) return;
         s = load_chunk(a.s + row * a.lds + col, here);
         g = load_chunk(a.dy + row * a.lddy + col, here);
-        if constexpr (kAdd)
+        if constexpr (kAdd) {
+            if (a.residual) r = load_chunk(a.residual + row * a.ldr + col, here);
             if (a.ds) more = load_chunk(a.ds + row * a.ldds + col, here);
+        }
         next_mean = a.stats[2 * row];
         next_rstd = a.stats[2 * row + 1];
     };
@@ -195,12 +200,21 @@ __global__ __launch_bounds__(kWhole ? 1024 : 256) void layer_norm_backward_kerne
         const float mean = next_mean, rstd = next_rstd;
         const bool inside = row < a.rows && here > 0;
         float hat[kChunk], dhat[kChunk], add[kChunk], sums[2] = {0.0f, 0.0f};
+        uint32_t kept = 0;
         if (inside) {
             float d[kChunk];
             widen(s, hat);
             widen(g, d);
-            if constexpr (kAdd)
+            if constexpr (kAdd) {
+                if (a.mask.dropped) kept = keep_bits(a.mask, offset, (uint32_t)row, (uint32_t)team.lane);
+                if (a.residual) {
+                    if (a.mask.dropped) keep(kept, a.mask.scale, hat);
+                    widen(r, add);
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j) hat[j] += add[j];
+                }
                 if (a.ds) widen(more, add);
+            }
 #pragma unroll
             for (int j = 0; j < kChunk; ++j) {
                 hat[j] = j < here ? (hat[j] - mean) * rstd : 0.0f;
@@ -227,7 +241,7 @@ __global__ __launch_bounds__(kWhole ? 1024 : 256) void layer_norm_backward_kerne
         store_chunk(a.dsum + to, here, out);
         if constexpr (kAdd) {
             if (a.dx) {
-                if (a.mask.dropped) drop(a.mask, offset, row, team.lane, out);
+                if (a.mask.dropped) keep(kept, a.mask.scale, out);
                 store_chunk(a.dx + to, here, out);
             }
         }
@@ -353,6 +367,11 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(NormBack
             const int64_t col = c * kChunk, here = a.width - col;
             float w[kChunk];
             widen(load_chunk(a.s + row * a.lds + col, here), hat);
+            if (a.residual) {
+                if (a.mask.dropped) drop(a.mask, offset, row, c, hat);
+                widen(load_chunk(a.residual + row * a.ldr + col, here), dhat);
+                for (int j = 0; j < kChunk; ++j) hat[j] += dhat[j];
+            }
             widen(load_chunk(a.dy + row * a.lddy + col, here), dhat);
             load_params<T>(a.weight, a.wide, col, here, 1.0f, w);
             for (int j = 0; j < kChunk; ++j) {
@@ -395,10 +414,16 @@ template <typename T>
 __global__ __launch_bounds__(256) void layer_norm_long_params_kernel(NormBackwardArgs<T> a) {
     const int64_t col = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (col >= a.width) return;
+    const uint64_t offset = a.mask.device_offset ? *a.mask.device_offset : a.mask.offset;
     float dw = 0.0f, db = 0.0f;
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const float d = to_float(a.dy[row * a.lddy + col]);
-        dw += d * ((to_float(a.s[row * a.lds + col]) - a.stats[2 * row]) * a.stats[2 * row + 1]);
+        float s = to_float(a.s[row * a.lds + col]);
+        if (a.residual) {
+            if (a.mask.dropped) s = keep_bits(a.mask, offset, (uint32_t)row, (uint32_t)(col / kChunk)) >> (col % kChunk) & 1 ? s * a.mask.scale : 0.0f;
+            s += to_float(a.residual[row * a.ldr + col]);
+        }
+        dw += d * ((s - a.stats[2 * row]) * a.stats[2 * row + 1]);
         db += d;
     }
     a.partial[2 * (int64_t)blockIdx.y * a.width + col] = dw;

@@ -131,7 +131,7 @@ extern "C" int64_t dgsp_layer_norm_backward_workspace_bytes(int64_t rows, int64_
 }
 
 extern "C" int dgsp_layer_norm_backward(int64_t rows, int64_t width, int type, int param_type, const void* s, int64_t lds,
-                                        const float* stats, const void* weight, const void* dy, int64_t lddy, const void* ds,
+                                        const void* residual, int64_t ldr, const float* stats, const void* weight, const void* dy, int64_t lddy, const void* ds,
                                         int64_t ldds, const dgsp_dropout_t* dropout, void* dsum, void* dx, void* dweight, void* dbias,
                                         void* workspace, int64_t workspace_bytes, void* stream) {
     DropMask mask;
@@ -139,7 +139,7 @@ extern "C" int dgsp_layer_norm_backward(int64_t rows, int64_t width, int type, i
         (param_type != type && param_type != DGSP_F32) || !make_mask(dropout, mask))
         return DGSP_ERR_INVALID_ARG;
     const bool params = dweight || dbias;
-    if (rows > 0 && (!readable(s, rows, width, lds) || !readable(dy, rows, width, lddy) || !stats || !dsum ||
+    if (rows > 0 && (!readable(s, rows, width, lds) || (residual && !readable(residual, rows, width, ldr)) || !readable(dy, rows, width, lddy) || !stats || !dsum ||
                      (ds && !readable(ds, rows, width, ldds)) || (dropout == nullptr) != (dx == nullptr)))
         return DGSP_ERR_INVALID_ARG;
     if (params && (!workspace || !aligned(workspace, 16) || workspace_bytes < dgsp_layer_norm_backward_workspace_bytes(rows, width)))
@@ -150,14 +150,14 @@ extern "C" int dgsp_layer_norm_backward(int64_t rows, int64_t width, int type, i
         const auto on = static_cast<hipStream_t>(stream);
         const bool wide = param_type != type;
         const int64_t groups = backward_groups(hold, rows);
-        const NormBackwardArgs<T> args{rows, width, hold.lanes, static_cast<const T*>(s), static_cast<const T*>(dy), static_cast<const T*>(ds),
-                                       lds,  lddy,  ldds,       stats, weight, wide, mask, static_cast<T*>(dsum), static_cast<T*>(dx),
+        const NormBackwardArgs<T> args{rows, width, hold.lanes, static_cast<const T*>(s), static_cast<const T*>(residual), static_cast<const T*>(dy), static_cast<const T*>(ds),
+                                       lds,  ldr,   lddy,  ldds,       stats, weight, wide, mask, static_cast<T*>(dsum), static_cast<T*>(dx),
                                        params ? static_cast<float*>(workspace) : nullptr};
         if (rows > 0 && !hold.fits) {
             layer_norm_backward_long_kernel<T><<<(unsigned)std::min<int64_t>(rows, kCus * 2), 1024, 0, on>>>(args);
             if (params) layer_norm_long_params_kernel<T><<<dim3((unsigned)ceil_div(width, 256), (unsigned)groups), 256, 0, on>>>(args);
         } else if (rows > 0) {
-            if (ds || dx)
+            if (ds || dx || residual)
                 launch_backward<T, true>(hold, args, groups, on);
             else
                 launch_backward<T, false>(hold, args, groups, on);

@@ -211,15 +211,24 @@ struct NormGradient {
     at::Tensor sum, x, weight, bias;
 };
 
-// `weight` and `bias` undefined: the norm has none; `ds` undefined: none.  The gradient of x is its own tensor only under dropout.
-NormGradient run_norm_backward(const at::Tensor& s, const at::Tensor& stats, const at::Tensor& weight, const at::Tensor& dy,
+// Is the sum made again from x and the residual in the backward pass, where the one that was written is rounded?
+bool again(const at::Tensor& x, const at::Tensor& residual) { return residual.defined() && x.scalar_type() != at::kFloat; }
+
+// `residual` defined: s is x.  `weight` and `bias` undefined: the norm has none; `ds` undefined: none.  The gradient of x is its own tensor
+// only under dropout.
+NormGradient run_norm_backward(const at::Tensor& s, const at::Tensor& residual, const at::Tensor& stats, const at::Tensor& weight, const at::Tensor& dy,
                                const at::Tensor& ds, bool dropped, const Drop& drop, const at::Tensor& offset, bool want_weight,
                                bool want_bias, at::ScalarType params) {
     const int type = type_of(s, "s");
     const Rows in = rows_of(s, "s"), grad = rows_of(dy, "dy");
     check_like(dy, s, "dy");
     if (dy.sizes() != s.sizes()) refuse("dy must have the shape of s");
-    Rows more;
+    Rows more, add;
+    if (residual.defined()) {
+        check_like(residual, s, "residual");
+        if (residual.sizes() != s.sizes()) refuse("residual must have the shape of s");
+        add = rows_of(residual, "residual");
+    }
     if (ds.defined()) {
         check_like(ds, s, "ds");
         if (ds.sizes() != s.sizes()) refuse("ds must have the shape of s");
@@ -241,7 +250,7 @@ NormGradient run_norm_backward(const at::Tensor& s, const at::Tensor& stats, con
     }
     const dgsp_dropout_t d = drop.on(offset);
     check(dgsp_layer_norm_backward(in.rows, width, type, params == at::kFloat ? DGSP_F32 : type, ptr(in.t), in.ld,
-                                   static_cast<const float*>(ptr(stats)), at_or_null(w), ptr(grad.t), grad.ld, at_or_null(more.t), more.ld,
+                                   at_or_null(add.t), add.ld, static_cast<const float*>(ptr(stats)), at_or_null(w), ptr(grad.t), grad.ld, at_or_null(more.t), more.ld,
                                    dropped ? &d : nullptr, ptr(out.sum), at_or_null(out.x), at_or_null(out.weight), at_or_null(out.bias),
                                    at_or_null(workspace), bytes, stream()),
           "dgsp_layer_norm_backward");
@@ -340,13 +349,14 @@ struct DropoutBackward : public LayerNode {
 
 struct NormBackward : public LayerNode {
     Drop drop;
-    SavedVariable s, weight, offset;
+    SavedVariable s, added, weight, offset;        // s: the sum, or x if the sum is made again from it and `added`
     at::Tensor stats;
-    bool residual, has_weight, has_bias;
+    bool residual, sum_again, has_weight, has_bias;
     at::ScalarType params;
     std::string name() const override { return residual ? "AddLayerNormBackward" : "LayerNormBackward"; }
     void release_variables() override {
         s.reset_data();
+        added.reset_data();
         weight.reset_data();
         offset.reset_data();
         stats.reset();
@@ -364,8 +374,8 @@ struct NormBackward : public LayerNode {
             out[3] = more;
             return out;
         }
-        const at::Tensor sum = s.unpack(residual ? shared_from_this() : nullptr);
-        NormGradient g = run_norm_backward(sum, stats, has_weight ? weight.unpack() : at::Tensor(), grads[0], more, dropped, drop, where,
+        const at::Tensor sum = s.unpack(residual && !sum_again ? shared_from_this() : nullptr);
+        NormGradient g = run_norm_backward(sum, sum_again ? added.unpack() : at::Tensor(), stats, has_weight ? weight.unpack() : at::Tensor(), grads[0], more, dropped, drop, where,
                                            has_weight && task_should_compute_output(1), has_bias && task_should_compute_output(2), params);
         out[0] = dropped ? g.x : g.sum;
         out[1] = g.weight;
@@ -495,6 +505,7 @@ PyObject* norm(const at::Tensor& x, const at::Tensor& residual, const at::Tensor
         auto node = new_node<NormBackward>();
         node->drop = drop;
         node->residual = residual.defined();
+        node->sum_again = again(x, residual);
         node->has_weight = weight.defined();
         node->has_bias = bias.defined();
         node->params = weight.defined() ? weight.scalar_type() : bias.defined() ? bias.scalar_type() : x.scalar_type();
@@ -505,7 +516,12 @@ PyObject* norm(const at::Tensor& x, const at::Tensor& residual, const at::Tensor
             node->set_next_edges(torch::autograd::collect_next_edges(x, weight, bias, residual));
             torch::autograd::set_history(out.y, node);
             torch::autograd::set_history(out.sum, node);
-            node->s = SavedVariable(out.sum, true);
+            if (node->sum_again) {
+                node->s = SavedVariable(x, false);
+                node->added = SavedVariable(residual, false);
+            } else {
+                node->s = SavedVariable(out.sum, true);
+            }
         } else {
             node->set_next_edges(torch::autograd::collect_next_edges(x, weight, bias));
             torch::autograd::set_history(out.y, node);
@@ -574,16 +590,16 @@ PyObject* layer_norm_forward(PyObject* const* a, Py_ssize_t n) {
     return wrap_all({out.y, out.sum, out.stats});
 }
 
-// (s, stats, weight, bias, dy, ds, dropped, p, seed, offset) -> (dsum, dx, dweight, dbias)
+// (s, residual, stats, weight, bias, dy, ds, dropped, p, seed, offset) -> (dsum, dx, dweight, dbias)
 PyObject* layer_norm_backward(PyObject* const* a, Py_ssize_t n) {
-    want(n, 10);
+    want(n, 11);
     const at::Tensor& s = as_tensor(a[0], "s");
     at::NoGradGuard no_grad;
-    const at::Tensor weight = optional_tensor(a[2], "weight"), bias = optional_tensor(a[3], "bias");
-    const Drop drop = as_drop(a + 7, s);
+    const at::Tensor weight = optional_tensor(a[3], "weight"), bias = optional_tensor(a[4], "bias");
+    const Drop drop = as_drop(a + 8, s);
     const at::ScalarType params = weight.defined() ? weight.scalar_type() : bias.defined() ? bias.scalar_type() : s.scalar_type();
-    const NormGradient g = run_norm_backward(s, as_tensor(a[1], "stats"), weight, as_tensor(a[4], "dy"), optional_tensor(a[5], "ds"),
-                                             as_int(a[6]) != 0, drop, drop.offset, weight.defined(), bias.defined(), params);
+    const NormGradient g = run_norm_backward(s, optional_tensor(a[1], "residual"), as_tensor(a[2], "stats"), weight, as_tensor(a[5], "dy"),
+                                             optional_tensor(a[6], "ds"), as_int(a[7]) != 0, drop, drop.offset, weight.defined(), bias.defined(), params);
     return wrap_all({g.sum, g.x, g.weight, g.bias});
 }
 

@@ -57,7 +57,7 @@ def lib():
         i64, vp, ci, cf, drop = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.POINTER(Dropout)
         L.dgsp_dropout.argtypes = [i64, i64, ci, drop, vp, i64, vp, i64, vp, i64, vp]
         L.dgsp_layer_norm.argtypes = [i64, i64, ci, ci, vp, i64, vp, i64, drop, vp, vp, cf, vp, i64, vp, i64, vp, vp]
-        L.dgsp_layer_norm_backward.argtypes = [i64, i64, ci, ci, vp, i64, vp, vp, vp, i64, vp, i64, drop, vp, vp, vp, vp, vp, i64, vp]
+        L.dgsp_layer_norm_backward.argtypes = [i64, i64, ci, ci, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, drop, vp, vp, vp, vp, vp, i64, vp]
         matrices = [vp, i64] * 4
         L.dgsp_gated_ff.argtypes = [i64] * 4 + [ci, ci] + matrices + [vp, i64, vp, vp, i64, vp]
         L.dgsp_gated_ff_backward.argtypes = [i64] * 4 + [ci, ci] + matrices + [vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]
@@ -98,7 +98,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
 
 def add_layer_norm(x, residual, weight=None, bias=None, eps=1e-5, p=0.0, seed=0, offset=0):
     """``s = residual + dropout(x)`` and the layer norm of ``s``, in one pass; returns ``(y, s)``.  ``s`` is rounded to the type
-    of ``x``, ``y`` is made from the sum before that."""
+    of ``x``, ``y`` is made from the sum before that; of 16-bit types the backward pass makes it again and keeps ``x`` and
+    ``residual`` for that."""
     out = (_native or native()).add_layer_norm(x, residual, weight, bias, eps, p, seed, offset)
     return _functions().norm.apply(x, residual, weight, bias, eps, p, seed, offset) if out is None else out
 
@@ -135,15 +136,16 @@ def _functions():
             y, s, stats = native().layer_norm_forward(x, residual, weight, bias, eps, p, seed, offset)
             ctx.drop = (p, seed, offset)
             ctx.residual = residual is not None
-            ctx.save_for_backward(s if ctx.residual else x, stats, weight, bias)
+            again = ctx.residual and x.dtype != torch.float32          # the sum is made again where the one written is rounded
+            ctx.save_for_backward(s if ctx.residual and not again else x, residual if again else None, stats, weight, bias)
             return (y, s) if ctx.residual else (y,)
 
         @staticmethod
         @torch.autograd.function.once_differentiable
         def backward(ctx, dy, ds=None):
-            s, stats, weight, bias = ctx.saved_tensors
+            s, added, stats, weight, bias = ctx.saved_tensors
             dropped = ctx.residual and ctx.drop[0] > 0
-            dsum, dx, dweight, dbias = native().layer_norm_backward(s, stats, weight, bias, dy, ds, int(dropped), *ctx.drop)
+            dsum, dx, dweight, dbias = native().layer_norm_backward(s, added, stats, weight, bias, dy, ds, int(dropped), *ctx.drop)
             return dx if dropped else dsum, dsum if ctx.residual else None, dweight, dbias, None, None, None, None
 
     class Dropped(torch.autograd.Function):
