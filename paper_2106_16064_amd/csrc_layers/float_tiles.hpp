@@ -192,17 +192,20 @@ __global__ __launch_bounds__(Shape::kThreads, 2) void float_tile_kernel(ProductA
         for (int e = 0; e < BLoader::kEach; ++e) b_loader.init(e, b_now[e / kEachSide].ld, e / kEachSide * kSideRows);
     };
     auto ask = [&] {
-        bool whole = ALoader::whole(a_now, i0, k, Shape::kM);
+        if (ALoader::whole(a_now, i0, k, Shape::kM)) {
+#pragma unroll
+            for (int e = 0; e < ALoader::kEach; ++e) a_loader.ask_whole(e, ALoader::begin(a_now, i0, k));
+        } else {
+#pragma unroll
+            for (int e = 0; e < ALoader::kEach; ++e) a_loader.ask(e, a_now, i0, k, 0);
+        }
+        bool whole = true;
 #pragma unroll
         for (int side = 0; side < kSides; ++side) whole = whole && BLoader::whole(b_now[side], j0, k, kSideRows);
         if (whole) {
 #pragma unroll
-            for (int e = 0; e < ALoader::kEach; ++e) a_loader.ask_whole(e, ALoader::begin(a_now, i0, k));
-#pragma unroll
             for (int e = 0; e < BLoader::kEach; ++e) b_loader.ask_whole(e, BLoader::begin(b_now[e / kEachSide], j0, k));
         } else {
-#pragma unroll
-            for (int e = 0; e < ALoader::kEach; ++e) a_loader.ask(e, a_now, i0, k, 0);
 #pragma unroll
             for (int e = 0; e < BLoader::kEach; ++e) b_loader.ask(e, b_now[e / kEachSide], j0, k, e / kEachSide * kSideRows);
         }
