@@ -108,10 +108,12 @@ struct FloatLoader {
         kept[e] = load_chunk(s.p + (inside ? at * s.ld + col : 0), inside ? s.cols - col : 0);
     }
 
-    __device__ __forceinline__ void leave(char* lds) const {
+    // `rows` of an operand along k are there: what comes of others is not stored, and they are left out
+    __device__ __forceinline__ void leave(char* lds, int rows) const {
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             const int c = threadIdx.x + e * kThreads, row = c / kChunks, chunk = c % kChunks;
+            if (kAlongK && row >= rows) continue;
             const int to = kAlongK ? chunk ^ turn(row) : (((chunk >> 1) ^ exchange(row)) << 1) + (chunk & 1);
             u32x4 out[3];
             split_chunk(kept[e], out);
@@ -169,6 +171,9 @@ __global__ __launch_bounds__(Shape::kThreads, 2) void float_tile_kernel(ProductA
     FloatReader<Shape::kN, kStage, kBRows> b_reader;
     a_reader.init(lane, wave_m * Shape::kFragsM * 16);
     b_reader.init(lane, wave_n * kEachN * 16);
+    // small tiles may have few rows, and do nothing for fragments that have none
+    constexpr bool kFew = Shape::kM == 64;
+    const int rows = kFew ? (int)min(args.m - i0, (int64_t)Shape::kM) : Shape::kM, here_m = rows - wave_m * Shape::kFragsM * 16;
     f32x4 acc[Shape::kFragsN][Shape::kFragsM];
 #pragma unroll
     for (int j = 0; j < Shape::kFragsN; ++j)
@@ -188,6 +193,7 @@ __global__ __launch_bounds__(Shape::kThreads, 2) void float_tile_kernel(ProductA
         for (int e = 0; e < ALoader::kEach; ++e) a_loader.init(e, a_now.ld, 0);
 #pragma unroll
         for (int side = 0; side < kSides; ++side) b_now[side] = args.b[Shape::kDual ? side : pair];
+        if constexpr (Shape::kDual) b_now[1] = {b_now[1].p, b_now[0].rows, b_now[0].cols, b_now[1].ld};     // of equal extents
 #pragma unroll
         for (int e = 0; e < BLoader::kEach; ++e) b_loader.init(e, b_now[e / kEachSide].ld, e / kEachSide * kSideRows);
     };
@@ -217,8 +223,8 @@ __global__ __launch_bounds__(Shape::kThreads, 2) void float_tile_kernel(ProductA
     }
     while (more) {
         __syncthreads();                                        // the last stage has been read
-        a_loader.leave(a_lds);
-        b_loader.leave(b_lds);
+        a_loader.leave(a_lds, rows);
+        b_loader.leave(b_lds, Shape::kN);
         __syncthreads();
         k += kStage;
         if (k >= k_end) {
@@ -229,6 +235,7 @@ __global__ __launch_bounds__(Shape::kThreads, 2) void float_tile_kernel(ProductA
         if (more) ask();
 #pragma unroll
         for (int s = 0; s < kStage / 32; ++s) {
+            if (kFew && here_m <= 0) break;
             s16x8 b[3][Shape::kFragsN];
 #pragma unroll
             for (int j = 0; j < Shape::kFragsN; ++j)
@@ -237,6 +244,7 @@ __global__ __launch_bounds__(Shape::kThreads, 2) void float_tile_kernel(ProductA
                     b[q][j] = b_reader.read(b_lds + q * BLoader::kPlane + j / kEachN * (BLoader::kPlane / 2), s, j % kEachN);
 #pragma unroll
             for (int i = 0; i < Shape::kFragsM; ++i) {
+                if (kFew && i * 16 >= here_m) break;
                 s16x8 a[3];
 #pragma unroll
                 for (int q = 0; q < 3; ++q) a[q] = a_reader.read(a_lds + q * ALoader::kPlane, s, i);
