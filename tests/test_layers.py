@@ -655,3 +655,23 @@ def test_refusals_of_the_c_entry_points():
     assert gated(ws=None) == bad and gated(size=need - 1) == bad and gated(ws=space.data_ptr() + 4) == bad and gated(rows=-1) == bad
     assert gated(saved=space.data_ptr() + 4) == bad and gated(width=1 << 28) == bad
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("rows,width,p", [(60, 24, 0.0), (60, 24, 0.25), (9, 1001, 0.1), (3, 8200, 0.3)])
+def test_gradient_of_the_weight_is_of_the_sum_before_it_is_rounded(rows, width, p, dtype):
+    """With parameters in float nothing of 16 bits is left in it.  (s - mean) / spread is off by at most 2 (n + 8) e (|s| + mean |s|) /
+    spread: s, the mean and the spread are sums of n terms at most; the sum over the rows adds (rows + 4) e of its magnitudes."""
+    show("weight of add_layer_norm", rows, width, p, dtype)
+    seed, offset = 11, 5
+    x, r, dy, ds = (normal((rows, width), dtype, 120 + i, 1.0, 0.2) for i in range(4))
+    w, b = normal((width,), torch.float32, 124, 0.1, 1.0), normal((width,), torch.float32, 125)
+    on = [t.cuda().requires_grad_(True) for t in (x, r, w, b)]
+    y, s = layers.add_layer_norm(*on, eps=EPS, p=p, seed=seed, offset=offset)
+    torch.autograd.backward([y, s], [dy.cuda(), ds.cuda()])
+    want = r.double() + ref.dropped(x.double(), p, seed, offset)
+    _, dw, _ = ref.norm_gradient(want, w.double(), dy.double(), EPS)
+    mean = want.mean(1, keepdim=True)
+    rstd = 1 / torch.sqrt(((want - mean) ** 2).mean(1, keepdim=True) + EPS)
+    size = (dy.double().abs() * (want.abs() + want.abs().mean(1, keepdim=True)) * rstd).sum(0)
+    assert_within(on[2].grad, dw, (2 * (width + 8) + rows + 4) * EPS32 * size, "dweight")
