@@ -75,7 +75,7 @@ Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, int type, boo
     c.tiles_m = ceil_div(m, c.size);
     c.tiles_n = ceil_div(n, dual ? c.size / 2 : c.size);
     const int64_t count = tiles(c.size);
-    if (splits && count < kCus) {
+    if (splits && count > 0 && count < kCus) {               // no tiles: a batch without rows
         const int64_t most = std::min<int64_t>(ceil_div((c.size == kMiddle ? 2 : 3) * kCus, count), depth / (type == DGSP_F32 ? 128 : 256));
         c.split_depth = padded(ceil_div(depth, most), kDepth);
         c.splits = (int)ceil_div(depth, c.split_depth);

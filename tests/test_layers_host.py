@@ -2,6 +2,7 @@
 import os
 import re
 import subprocess
+import sys
 
 import pytest
 
@@ -88,3 +89,16 @@ def test_tensors_on_the_host_are_refused():
             call()
     with pytest.raises(dg.DgspError, match="silu, gelu, relu"):
         layers.gated_ff(x, x, x, x, activation=3)
+
+
+def test_sizes_of_a_block_without_rows():
+    """Deep enough for products to be split along the depth, where nothing is left to split.  In a process of its own: a division by
+    zero ends it."""
+    script = ("from paper_2106_16064_amd import layers\n"
+              "L = layers.lib()\n"
+              "for t in (layers.F32, layers.BF16, layers.F16):\n"
+              "    for block in ((4096, 64, 64), (64, 1024, 64), (40, 4096, 64), (512, 1024, 512), (64, 64, 4096), (4096, 16384, 4096), (1, 1, 1)):\n"
+              "        for size in (L.dgsp_gated_ff_saved_bytes, L.dgsp_gated_ff_workspace_bytes, L.dgsp_gated_ff_backward_workspace_bytes):\n"
+              "            assert 0 <= size(0, *block, t) <= size(1, *block, t), (block, t)\n")
+    run = subprocess.run([sys.executable, "-c", script], cwd=ROOT, capture_output=True, text=True)
+    assert run.returncode == 0, (run.returncode, run.stderr)
