@@ -72,7 +72,7 @@ NarrowArgs<E> arguments(const NarrowCall& c) {
     a.out_width = c.out_width;
     a.activation = c.activation;
     a.x = static_cast<const E*>(c.x);
-    a.ldx = c.ldx;
+    a.ldx = c.rows == 1 ? c.width : c.ldx;             // of one row it may be anything, and the kernels' buffers end where it says
     a.w_gate = static_cast<const E*>(c.w_gate);
     a.ldg = c.ldg;
     a.w_up = static_cast<const E*>(c.w_up);
@@ -82,7 +82,7 @@ NarrowArgs<E> arguments(const NarrowCall& c) {
     a.y = static_cast<E*>(c.y);
     a.ldy = c.ldy;
     a.dy = static_cast<const E*>(c.dy);
-    a.lddy = c.lddy;
+    a.lddy = c.rows == 1 ? c.out_width : c.lddy;
     a.dx = static_cast<E*>(c.dx);
     return a;
 }

@@ -30,3 +30,42 @@ def test_a_deep_block_of_no_rows(width, hidden, out, dtype):
     dx, *dw = torch.autograd.grad(y, [x, *w], torch.empty_like(y))
     assert dx.shape == x.shape
     assert all(g.shape == t.shape and g.dtype == dtype and not g.any() for g, t in zip(dw, w))
+
+
+# ---------------------------------------------------------------- the C interface: one row
+
+CODES = {torch.float32: layers.F32, torch.bfloat16: layers.BF16, torch.float16: layers.F16}
+
+
+def c_block(x, w, dy, ldx, lddy):
+    """Result and gradients through the C entry points, with the distances of rows given."""
+    L, code = layers.lib(), CODES[x.dtype]
+    (rows, width), (hidden, _), (out, _) = x.shape, w[0].shape, w[2].shape
+    extents = (rows, width, hidden, out, code)
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def space(size):
+        return torch.empty(max(size(*extents), 16), dtype=torch.uint8, device="cuda")
+
+    saved, work, back = space(L.dgsp_gated_ff_saved_bytes), space(L.dgsp_gated_ff_workspace_bytes), space(L.dgsp_gated_ff_backward_workspace_bytes)
+    y = torch.empty((rows, out), dtype=x.dtype, device="cuda")
+    grads = [torch.empty_like(t) for t in (x, *w)]
+    matrices = [x.data_ptr(), ldx, w[0].data_ptr(), width, w[1].data_ptr(), width, w[2].data_ptr(), hidden]
+    assert L.dgsp_gated_ff(*extents, layers.SILU, *matrices, y.data_ptr(), out, saved.data_ptr(), work.data_ptr(), work.numel(), stream) == 0
+    assert L.dgsp_gated_ff_backward(*extents, layers.SILU, *matrices, dy.data_ptr(), lddy, saved.data_ptr(), *(g.data_ptr() for g in grads),
+                                    back.data_ptr(), back.numel(), stream) == 0
+    return [y, *grads]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("width,hidden", [(32, 64), (32, 128), (32, 256), (64, 64), (64, 128), (64, 256), (128, 64), (128, 128), (40, 64), (256, 512)])
+def test_one_row_of_a_block_has_no_distance_to_the_next(width, hidden, dtype):
+    """Whatever the caller gives for it, the results are the same."""
+    show("one row", width, hidden, dtype)
+    torch.manual_seed(0)
+    x, dy = (torch.randn((1, width), device="cuda").to(dtype) for _ in range(2))
+    w = [(torch.randn(shape, device="cuda") * shape[1] ** -0.5).to(dtype) for shape in ((hidden, width), (hidden, width), (width, hidden))]
+    want = c_block(x, w, dy, width, width)
+    for ldx, lddy in ((8, 8), (8, width), (width, 8), (16, 24), (0, 0), (1, 1), (-8, -8), (1 << 40, 1 << 40)):
+        got = c_block(x, w, dy, ldx, lddy)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), (ldx, lddy)
