@@ -24,16 +24,15 @@ __device__ __forceinline__ void activate(int kind, const float (&g)[kCount], flo
     } else if (kind == DGSP_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            float e;
+            float s;
             if constexpr (kFloat) {
-                const float power = fminf(-1.44269504f * g[i], 126.0f);                     // below that the value is 0
-                const float rest = power < 126.0f ? fmaf(-1.44269504f, g[i], -power) - 1.925963e-8f * g[i] : 0.0f;
-                e = __builtin_amdgcn_exp2f(power);
-                e = fmaf(e, 0.69314718f * rest, e);
+                const float power = -1.44269504f * g[i], inside = fminf(power, 126.0f);
+                const float rest = fabsf(power) < 126.0f ? fmaf(-1.44269504f, g[i], -power) - 1.925963e-8f * g[i] : 0.0f;
+                const float e = __builtin_amdgcn_exp2f(inside);
+                s = power < 126.0f ? __builtin_amdgcn_rcpf(1.0f + fmaf(e, 0.69314718f * rest, e)) : 0.0f;       // 2^-126 and less: not times a large g
             } else {
-                e = __builtin_amdgcn_exp2f(-1.44269504f * g[i]);
+                s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g[i]));
             }
-            const float s = __builtin_amdgcn_rcpf(1.0f + e);
             value[i] = g[i] * s;
             slope[i] = s + value[i] * (1.0f - s);
         }

@@ -69,3 +69,36 @@ def test_one_row_of_a_block_has_no_distance_to_the_next(width, hidden, dtype):
     for ldx, lddy in ((8, 8), (8, width), (width, 8), (16, 24), (0, 0), (1, 1), (-8, -8), (1 << 40, 1 << 40)):
         got = c_block(x, w, dy, ldx, lddy)
         assert all(torch.equal(a, b) for a, b in zip(got, want)), (ldx, lddy)
+
+
+# ---------------------------------------------------------------- gates at the ends of the range
+
+UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("hidden", [1, 300])
+@pytest.mark.parametrize("activation", ["silu", "gelu", "relu"])
+def test_gates_far_from_zero(activation, hidden, dtype):
+    """One hidden value with g = x0 + x1, u = x2 = 1 and y = act(g), so that dx0 is act'(g).  From 88 on act(g) is g or 0 and its derivative
+    1 or 0, to less than 89 2^-126 (silu of -88); h and y are rounded once each, and so are dg and dx.  The sum of the two largest is beyond
+    the range of the sums, and its value too."""
+    show("far gates", activation, hidden, dtype)
+    ends = [88.0, 89.0, 104.0, 300.0, 1e3, 6e4] + ([1e10, 1e20, 1e30, 2.2e38, 2.5e38, 3e38] if dtype != torch.float16 else [])
+    g = torch.tensor([s * v for v in ends for s in (1.0, -1.0)]).to(dtype)
+    x = torch.zeros((len(g) + 1, 3), dtype=dtype)
+    x[:-1, 0], x[:, 2] = g, 1.0
+    x[-1, :2] = torch.finfo(dtype).max if dtype != torch.float16 else 3e4
+    w_gate, w_up, w_down = torch.zeros((hidden, 3)), torch.zeros((hidden, 3)), torch.zeros((1, hidden))
+    w_gate[0, :2], w_up[0, 2], w_down[0, 0] = 1.0, 1.0, 1.0
+    leaf, *w = (t.cuda().to(dtype).requires_grad_(True) for t in (x, w_gate, w_up, w_down))
+    y = layers.gated_ff(leaf, *w, activation=activation)
+    slope, = torch.autograd.grad(y[:-1], leaf, torch.ones_like(y[:-1]))
+    y, slope, want = y.detach()[:, 0].double().cpu(), slope[:-1, 0].double().cpu(), g.double().clamp(min=0.0)
+    tiny = 89 * 2.0 ** -126 if dtype != torch.float16 else 2.0 ** -25
+    assert ((y[:-1] - want).abs() <= 2 * UNIT[dtype] * want + tiny).all(), (g, y)
+    assert ((slope - (want > 0).double()).abs() <= 4 * UNIT[dtype]).all(), (g, slope)
+    if dtype == torch.float32:
+        assert not torch.isfinite(y[-1])                     # an infinity among products of parts: it or NaN, which is not said
+    else:
+        assert y[-1] == (float("inf") if dtype == torch.bfloat16 else 6e4)
