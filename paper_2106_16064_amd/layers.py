@@ -130,35 +130,45 @@ def _functions():
 
     import torch
 
+    def keep(drop, *tensors):
+        """What ``save_for_backward`` gets, with dropout's offset last if it is a tensor, and the arguments of dropout without it."""
+        p, seed, offset = drop
+        return ((*tensors, offset), (p, seed, None)) if isinstance(offset, torch.Tensor) else ((*tensors, None), drop)
+
+    def given(drop, offset):
+        return drop if offset is None else (*drop[:2], offset)
+
     class Norm(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, residual, weight, bias, eps, p, seed, offset):
             y, s, stats = native().layer_norm_forward(x, residual, weight, bias, eps, p, seed, offset)
-            ctx.drop = (p, seed, offset)
             ctx.residual = residual is not None
             again = ctx.residual and x.dtype != torch.float32          # the sum is made again where the one written is rounded
-            ctx.save_for_backward(s if ctx.residual and not again else x, residual if again else None, stats, weight, bias)
+            saved, ctx.drop = keep((p, seed, offset), s if ctx.residual and not again else x, residual if again else None, stats, weight, bias)
+            ctx.save_for_backward(*saved)
             return (y, s) if ctx.residual else (y,)
 
         @staticmethod
         @torch.autograd.function.once_differentiable
         def backward(ctx, dy, ds=None):
-            s, added, stats, weight, bias = ctx.saved_tensors
+            s, added, stats, weight, bias, offset = ctx.saved_tensors
             dropped = ctx.residual and ctx.drop[0] > 0
-            dsum, dx, dweight, dbias = native().layer_norm_backward(s, added, stats, weight, bias, dy, ds, int(dropped), *ctx.drop)
+            drop = given(ctx.drop, offset)
+            dsum, dx, dweight, dbias = native().layer_norm_backward(s, added, stats, weight, bias, dy, ds, int(dropped), *drop)
             return dx if dropped else dsum, dsum if ctx.residual else None, dweight, dbias, None, None, None, None
 
     class Dropped(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, p, seed, offset, residual):
-            ctx.drop = (p, seed, offset)
             ctx.residual = residual is not None
+            saved, ctx.drop = keep((p, seed, offset))
+            ctx.save_for_backward(*saved)
             return native().dropout_forward(x, p, seed, offset, residual)
 
         @staticmethod
         @torch.autograd.function.once_differentiable
         def backward(ctx, dy):
-            return native().dropout_forward(dy, *ctx.drop, None), None, None, None, dy if ctx.residual else None
+            return native().dropout_forward(dy, *given(ctx.drop, *ctx.saved_tensors), None), None, None, None, dy if ctx.residual else None
 
     class Gated(torch.autograd.Function):
         @staticmethod

@@ -102,3 +102,29 @@ def test_gates_far_from_zero(activation, hidden, dtype):
         assert not torch.isfinite(y[-1])                     # an infinity among products of parts: it or NaN, which is not said
     else:
         assert y[-1] == (float("inf") if dtype == torch.bfloat16 else 6e4)
+
+
+# ---------------------------------------------------------------- what the backward pass finds changed
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("which", ["add_layer_norm", "dropout"])
+def test_an_offset_changed_before_the_backward_pass_is_noticed(which, dtype):
+    """Another offset is another mask; on the way of the graph nodes and on that of autograd's own Functions.  Unchanged, both give what a
+    number gives."""
+    show("changed offset", which, dtype)
+    torch.manual_seed(0)
+    x, r, g = (torch.randn((20, 24), device="cuda").to(dtype) for _ in range(3))
+    functions = layers._functions()
+    calls = {"add_layer_norm": (lambda a, b, o: layers.add_layer_norm(a, b, p=0.5, seed=1, offset=o)[0],
+                                lambda a, b, o: functions.norm.apply(a, b, None, None, 1e-5, 0.5, 1, o)[0]),
+             "dropout": (lambda a, b, o: layers.dropout(a, 0.5, 1, o, residual=b), lambda a, b, o: functions.dropout.apply(a, 0.5, 1, o, b))}
+    for call in calls[which]:
+        leaves = [t.clone().requires_grad_(True) for t in (x, r)]
+        want = torch.autograd.grad(call(*leaves, 3), leaves, g)
+        offset = torch.full((1,), 3, dtype=torch.int64, device="cuda")
+        got = torch.autograd.grad(call(*leaves, offset), leaves, g)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        y = call(*leaves, offset)
+        offset.add_(1)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            torch.autograd.grad(y, leaves, g)
