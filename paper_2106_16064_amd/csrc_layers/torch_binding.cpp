@@ -211,6 +211,11 @@ struct NormGradient {
     at::Tensor sum, x, weight, bias;
 };
 
+// What a forward pass left, as hooks of saved tensors may give it back.
+void check_left(const at::Tensor& t, at::ScalarType type, int64_t count, const at::Tensor& like, const char* name) {
+    if (!is_array(t, type) || t.numel() != count || t.device() != like.device()) refuse(std::string(name) + " must be what the forward pass left");
+}
+
 // Is the sum made again from x and the residual in the backward pass, where the one that was written is rounded?
 bool again(const at::Tensor& x, const at::Tensor& residual) { return residual.defined() && x.scalar_type() != at::kFloat; }
 
@@ -234,6 +239,9 @@ NormGradient run_norm_backward(const at::Tensor& s, const at::Tensor& residual, 
         if (ds.sizes() != s.sizes()) refuse("ds must have the shape of s");
         more = rows_of(ds, "ds");
     }
+    if (weight.defined() && weight.scalar_type() != params) refuse("weight must have the type it had");
+    check_params(s, weight, {});
+    check_left(stats, at::kFloat, 2 * in.rows, s, "stats");
     const at::Tensor w = weight.defined() ? weight.contiguous() : weight;
     const c10::DeviceGuard guard(s.device());
     NormGradient out;
@@ -309,6 +317,7 @@ std::vector<at::Tensor> run_gated_backward(const Gated& g, const at::Tensor& x, 
     check_like(dy, x, "dy");
     const Rows grad = rows_of(dy, "dy");
     if (grad.rows != rows || grad.width != out_width) refuse("dy must have the shape of y");
+    check_left(saved, at::kByte, dgsp_gated_ff_saved_bytes(rows, width, hidden, out_width, g.type), x, "saved");
     std::vector<at::Tensor> out(4);
     if (wanted[0]) out[0] = empty_on(x.sizes(), x.scalar_type(), x);
     for (int i = 1; i < 4; ++i)
@@ -324,7 +333,22 @@ std::vector<at::Tensor> run_gated_backward(const Gated& g, const at::Tensor& x, 
 
 // ---------------------------------------------------------------- graph nodes
 
-// What the nodes share: they are not differentiable themselves, as their kernels are not, and say so.
+// Dropout's arguments as a node keeps them.
+struct SavedDrop {
+    Drop drop;                          // without the tensor
+    SavedVariable offset;
+    bool on_gpu = false;
+    void save(const Drop& d) {
+        drop = d;
+        drop.offset.reset();
+        on_gpu = d.offset.defined();
+        if (on_gpu) offset = SavedVariable(d.offset, false);
+    }
+    at::Tensor unpack_offset() const { return on_gpu ? offset.unpack() : at::Tensor(); }
+};
+
+// What the nodes share: they are not differentiable themselves, as their kernels are not, and say so.  All tensors that they keep are
+// SavedVariables: hooks may move them elsewhere, and changes in between are noticed.
 struct LayerNode : public torch::autograd::Node {
     void once_only() const {
         TORCH_CHECK(!at::GradMode::is_enabled(), name(), ": gradients of gradients are not supported (create_graph=True)");
@@ -332,25 +356,23 @@ struct LayerNode : public torch::autograd::Node {
 };
 
 struct DropoutBackward : public LayerNode {
-    Drop drop;
-    SavedVariable offset;
+    SavedDrop saved;
     bool residual;
     std::string name() const override { return "DropoutBackward"; }
-    void release_variables() override { offset.reset_data(); }
+    void release_variables() override { saved.offset.reset_data(); }
     variable_list apply(variable_list&& grads) override {
         once_only();
         variable_list out(residual ? 2 : 1);
         if (!grads[0].defined()) return out;
-        if (task_should_compute_output(0)) out[0] = run_dropout(grads[0], drop, drop.offset.defined() ? offset.unpack() : at::Tensor(), {});
+        if (task_should_compute_output(0)) out[0] = run_dropout(grads[0], saved.drop, saved.unpack_offset(), {});
         if (residual) out[1] = grads[0];
         return out;
     }
 };
 
 struct NormBackward : public LayerNode {
-    Drop drop;
-    SavedVariable s, added, weight, offset;        // s: the sum, or x if the sum is made again from it and `added`
-    at::Tensor stats;
+    SavedDrop saved;
+    SavedVariable s, added, weight, stats;         // s: the sum, or x if the sum is made again from it and `added`
     bool residual, sum_again, has_weight, has_bias;
     at::ScalarType params;
     std::string name() const override { return residual ? "AddLayerNormBackward" : "LayerNormBackward"; }
@@ -358,15 +380,16 @@ struct NormBackward : public LayerNode {
         s.reset_data();
         added.reset_data();
         weight.reset_data();
-        offset.reset_data();
-        stats.reset();
+        stats.reset_data();
+        saved.offset.reset_data();
     }
     // edges: x, weight, bias, and the residual
     variable_list apply(variable_list&& grads) override {
         once_only();
         variable_list out(residual ? 4 : 3);
         const at::Tensor more = residual ? grads[1] : at::Tensor();
-        const at::Tensor where = drop.offset.defined() ? offset.unpack() : at::Tensor();
+        const Drop& drop = saved.drop;
+        const at::Tensor where = saved.unpack_offset();
         const bool dropped = residual && drop.host.p > 0.0;
         if (!grads[0].defined()) {
             if (!more.defined()) return out;
@@ -375,7 +398,7 @@ struct NormBackward : public LayerNode {
             return out;
         }
         const at::Tensor sum = s.unpack(residual && !sum_again ? shared_from_this() : nullptr);
-        NormGradient g = run_norm_backward(sum, sum_again ? added.unpack() : at::Tensor(), stats, has_weight ? weight.unpack() : at::Tensor(), grads[0], more, dropped, drop, where,
+        NormGradient g = run_norm_backward(sum, sum_again ? added.unpack() : at::Tensor(), stats.unpack(), has_weight ? weight.unpack() : at::Tensor(), grads[0], more, dropped, drop, where,
                                            has_weight && task_should_compute_output(1), has_bias && task_should_compute_output(2), params);
         out[0] = dropped ? g.x : g.sum;
         out[1] = g.weight;
@@ -386,13 +409,11 @@ struct NormBackward : public LayerNode {
 };
 
 struct GatedBackward : public LayerNode {
-    SavedVariable x, w_gate, w_up, w_down;
-    at::Tensor saved;
+    SavedVariable x, w_gate, w_up, w_down, saved;
     int activation;
     std::string name() const override { return "GatedFeedForwardBackward"; }
     void release_variables() override {
-        for (SavedVariable* v : {&x, &w_gate, &w_up, &w_down}) v->reset_data();
-        saved.reset();
+        for (SavedVariable* v : {&x, &w_gate, &w_up, &w_down, &saved}) v->reset_data();
     }
     variable_list apply(variable_list&& grads) override {
         once_only();
@@ -401,7 +422,7 @@ struct GatedBackward : public LayerNode {
         const Gated g = gated_arguments(in, w_gate.unpack(), w_up.unpack(), w_down.unpack(), activation);
         const bool wanted[4] = {task_should_compute_output(0), task_should_compute_output(1), task_should_compute_output(2),
                                 task_should_compute_output(3)};
-        return run_gated_backward(g, in, grads[0], saved, wanted);
+        return run_gated_backward(g, in, grads[0], saved.unpack(), wanted);
     }
 };
 
@@ -485,8 +506,7 @@ PyObject* dropout(PyObject* const* a, Py_ssize_t n) {
     if (wants_grad({x, residual})) {
         auto node = new_node<DropoutBackward>();
         node->residual = residual.defined();
-        node->drop = drop;
-        if (drop.offset.defined()) node->offset = SavedVariable(drop.offset, false);
+        node->saved.save(drop);
         node->set_next_edges(residual.defined() ? torch::autograd::collect_next_edges(x, residual) : torch::autograd::collect_next_edges(x));
         torch::autograd::set_history(y, node);
     }
@@ -503,14 +523,13 @@ PyObject* norm(const at::Tensor& x, const at::Tensor& residual, const at::Tensor
     }
     if (graph) {
         auto node = new_node<NormBackward>();
-        node->drop = drop;
+        node->saved.save(drop);
         node->residual = residual.defined();
         node->sum_again = again(x, residual);
         node->has_weight = weight.defined();
         node->has_bias = bias.defined();
         node->params = weight.defined() ? weight.scalar_type() : bias.defined() ? bias.scalar_type() : x.scalar_type();
-        node->stats = out.stats;
-        if (drop.offset.defined()) node->offset = SavedVariable(drop.offset, false);
+        node->stats = SavedVariable(out.stats, false);
         if (weight.defined()) node->weight = SavedVariable(weight, false);
         if (residual.defined()) {
             node->set_next_edges(torch::autograd::collect_next_edges(x, weight, bias, residual));
@@ -566,7 +585,7 @@ PyObject* gated_ff(PyObject* const* a, Py_ssize_t n) {
     if (graph) {
         auto node = new_node<GatedBackward>();
         node->activation = activation;
-        node->saved = out.second;
+        node->saved = SavedVariable(out.second, false);
         node->x = SavedVariable(x, false);
         node->w_gate = SavedVariable(w_gate, false);
         node->w_up = SavedVariable(w_up, false);

@@ -128,3 +128,88 @@ def test_an_offset_changed_before_the_backward_pass_is_noticed(which, dtype):
         offset.add_(1)
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             torch.autograd.grad(y, leaves, g)
+
+
+# ---------------------------------------------------------------- what the graph keeps
+
+def layer_calls(dtype):
+    """Name, call and its inputs: blocks on the general and on the narrow way."""
+    torch.manual_seed(0)
+
+    def tensors(*shapes):
+        return [torch.randn(shape, device="cuda").to(dtype) for shape in shapes]
+
+    return {
+        "layer_norm": (layers.layer_norm, tensors((30, 40), (40,), (40,))),
+        "add_layer_norm": (lambda *t: layers.add_layer_norm(*t, p=0.25, seed=1), tensors((30, 40), (30, 40), (40,), (40,))),
+        "dropout": (lambda *t: layers.dropout(t[0], 0.25, 1, residual=t[1]), tensors((30, 40), (30, 40))),
+        "narrow block": (layers.gated_ff, tensors((30, 40), (24, 40), (24, 40), (16, 24))),
+        "block": (layers.gated_ff, tensors((30, 40), (300, 40), (300, 40), (16, 300))),
+    }
+
+
+def results(call, inputs):
+    leaves = [t.clone().requires_grad_(True) for t in inputs]
+    out = call(*leaves)
+    out = out if isinstance(out, tuple) else (out,)
+    return out, leaves
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("name", ["layer_norm", "add_layer_norm", "dropout", "narrow block", "block"])
+def test_all_that_a_node_keeps_goes_through_the_hooks_of_saved_tensors(name, dtype):
+    """A program may move it to the host until the backward pass or make it again then: once the results are gone, nothing of the call is
+    left on the GPU, and the gradients are the same."""
+    show("saved tensors", name, dtype)
+    call, inputs = layer_calls(dtype)[name]
+    out, leaves = results(call, inputs)
+    grads = [torch.randn_like(t) for t in out]
+    want = torch.autograd.grad(out, leaves, grads)
+
+    with torch.autograd.graph.save_on_cpu():
+        out, leaves = results(call, inputs)
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, leaves, grads), want))
+
+    from torch.utils.checkpoint import checkpoint
+    leaves = [t.clone().requires_grad_(True) for t in inputs]
+    out = checkpoint(call, *leaves, use_reentrant=False)
+    out = out if isinstance(out, tuple) else (out,)
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, leaves, grads), want))
+    del out, leaves, want
+
+    leaves = [t.clone().requires_grad_(True) for t in inputs]
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    with torch.autograd.graph.save_on_cpu():
+        out = call(*leaves)
+    nodes = {t.grad_fn for t in (out if isinstance(out, tuple) else (out,))}
+    assert len(nodes) == 1
+    del out
+    assert torch.cuda.memory_allocated() == before
+    del nodes
+
+
+@pytest.mark.parametrize("name", ["layer_norm", "add_layer_norm", "block"])
+def test_hooks_that_give_something_else_back_are_refused(name):
+    """Of another size, another type or on the host: before anything runs."""
+    show("hooks that give something else", name)
+    call, inputs = layer_calls(torch.bfloat16)[name]
+    shapes = {tuple(t.shape) for t in inputs}
+    for wrong in (lambda t: t[:-1], lambda t: t.cpu(), lambda t: t.to(torch.int16), lambda t: torch.cat((t, t))[::2]):
+        leaves = [t.clone().requires_grad_(True) for t in inputs]
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t if tuple(t.shape) in shapes else wrong(t)):
+            out = call(*leaves)
+        out = out if isinstance(out, tuple) else (out,)
+        with pytest.raises(RuntimeError, match="what the forward pass left"):
+            torch.autograd.grad(out, leaves, [torch.ones_like(t) for t in out])
+
+
+def test_hooks_that_give_another_weight_back_are_refused():
+    show("hooks that give another weight")
+    call, inputs = layer_calls(torch.bfloat16)["layer_norm"]
+    for wrong in (lambda t: t[:-1], lambda t: t.float(), lambda t: t.half(), lambda t: t.cpu()):
+        leaves = [t.clone().requires_grad_(True) for t in inputs]
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: wrong(t) if t.shape == (40,) else t):
+            y = call(*leaves)
+        with pytest.raises(RuntimeError, match="weight must"):
+            torch.autograd.grad(y, leaves, torch.ones_like(y))
