@@ -140,7 +140,7 @@ struct Loader {
             const u32x4 buffer = {(uint32_t)address, (uint32_t)(address >> 32) & 0xffffu, high < 0 ? 0u : some, 0x00020000u};
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + j * kWaveBytes),
                          "v"(beyond ? kNowhere : offset[kPatternBit < 0 ? 0 : j >> kPatternBit & 1]), "s"(buffer)
-                         : "memory");
+                         : "memory", "m0");
             at += kRowsEach * 2 * ld;
             left -= kRowsEach * 2 * ld;
         }

@@ -103,3 +103,18 @@ def test_matrix_results_and_operands_have_their_wait_states(objects):
     for name, lines in tiles.items():
         assert sum(line.startswith("v_mfma") for line in lines) >= 16, name
         assert early_uses(lines) == [], name
+
+
+def test_assembly_names_what_it_writes():
+    """The compiler keeps values of its own in m0, the scalar flags and the like, and sees of an assembly statement what it names."""
+    found = 0
+    for source in sorted(os.listdir(os.path.join(ROOT, "paper_2106_16064_amd", "csrc_layers"))):
+        text = open(os.path.join(ROOT, "paper_2106_16064_amd", "csrc_layers", source)).read()
+        for statement in re.findall(r"\basm volatile\((.*?)\);", text, re.S):
+            code, *operands = re.split(r'(?<!\\)"\s*:', statement, maxsplit=1)
+            named = operands[0] if operands else ""
+            for register in ("m0", "vcc", "exec", "scc"):
+                if re.search(rf"\b(?:s|v)_\w+ {register}\b", code):
+                    found += 1
+                    assert f'"{register}"' in named, (source, statement)
+    assert found >= 1
