@@ -279,6 +279,7 @@ __global__ __launch_bounds__(kWhole ? 1024 : 256) void layer_norm_backward_kerne
 }
 
 constexpr int kParamColumns = 32, kParamSlices = 32, kParamAhead = 8;
+constexpr int64_t kParamGroups = 1 << 20;       // at most: a launch has fewer than 2^32 threads, and drops what is beyond without an error
 
 // dweight and dbias from the workgroups' sums.  Few columns and many sums: what takes time is waiting for memory, so a lane asks for
 // eight sums at a time (one at a time: 17 to 38 us where this takes 4 to 8).
@@ -287,23 +288,27 @@ __global__ __launch_bounds__(kParamColumns* kParamSlices) void layer_norm_params
                                                                                          void* dbias, bool wide) {
     __shared__ float part[kParamSlices][kParamColumns];
     const int column = threadIdx.x % kParamColumns, slice = threadIdx.x / kParamColumns;
-    const int64_t at = (int64_t)blockIdx.x * kParamColumns + column;
-    float v = 0.0f;
-    if (at < 2 * width)
-        for (int64_t g = slice; g < groups; g += kParamSlices * kParamAhead) {
-            float ahead[kParamAhead];
+    for (int64_t first = (int64_t)blockIdx.x * kParamColumns; first < 2 * width; first += (int64_t)gridDim.x * kParamColumns) {
+        const int64_t at = first + column;
+        float v = 0.0f;
+        if (at < 2 * width)
+            for (int64_t g = slice; g < groups; g += kParamSlices * kParamAhead) {
+                float ahead[kParamAhead];
 #pragma unroll
-            for (int i = 0; i < kParamAhead; ++i) ahead[i] = g + i * kParamSlices < groups ? partial[(g + i * kParamSlices) * 2 * width + at] : 0.0f;
+                for (int i = 0; i < kParamAhead; ++i) ahead[i] = g + i * kParamSlices < groups ? partial[(g + i * kParamSlices) * 2 * width + at] : 0.0f;
 #pragma unroll
-            for (int i = 0; i < kParamAhead; ++i) v += ahead[i];
+                for (int i = 0; i < kParamAhead; ++i) v += ahead[i];
+            }
+        part[slice][column] = v;
+        __syncthreads();
+        if (slice == 0 && at < 2 * width) {
+#pragma unroll
+            for (int i = 1; i < kParamSlices; ++i) v += part[i][column];
+            void* to = at < width ? dweight : dbias;
+            if (to) store_param<T>(to, at < width ? at : at - width, wide, v);
         }
-    part[slice][column] = v;
-    __syncthreads();
-    if (slice || at >= 2 * width) return;
-#pragma unroll
-    for (int i = 1; i < kParamSlices; ++i) v += part[i][column];
-    void* to = at < width ? dweight : dbias;
-    if (to) store_param<T>(to, at < width ? at : at - width, wide, v);
+        __syncthreads();
+    }
 }
 
 // ---------------------------------------------------------------- rows beyond what registers hold

@@ -163,7 +163,7 @@ extern "C" int dgsp_layer_norm_backward(int64_t rows, int64_t width, int type, i
                 launch_backward<T, false>(hold, args, groups, on);
         }
         if (params)
-            layer_norm_params_kernel<T><<<(unsigned)ceil_div(2 * width, kParamColumns), kParamColumns * kParamSlices, 0, on>>>(
+            layer_norm_params_kernel<T><<<(unsigned)std::min(ceil_div(2 * width, kParamColumns), kParamGroups), kParamColumns * kParamSlices, 0, on>>>(
                 width, rows > 0 ? groups : 0, args.partial, dweight, dbias, wide);
         return launched();
     });

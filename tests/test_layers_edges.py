@@ -213,3 +213,27 @@ def test_hooks_that_give_another_weight_back_are_refused():
             y = call(*leaves)
         with pytest.raises(RuntimeError, match="weight must"):
             torch.autograd.grad(y, leaves, torch.ones_like(y))
+
+
+# ---------------------------------------------------------------- very wide rows
+
+def test_parameter_gradients_of_very_wide_rows():
+    """2^26 and some columns, where a workgroup for every 32 of them is more than a launch may have.  Rows of as many 1 as -1 have the mean 0
+    and the spread 1 exactly, so that hat is x / sqrt(1 + eps) to 4 units of the last place, and bfloat16 sums of two are rounded once."""
+    show("very wide rows")
+    width = (1 << 26) + 16
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.ones((2, width), device="cuda", dtype=torch.bfloat16)
+    x[0, 1::2] = -1.0
+    x[1, :width // 2] = -1.0
+    w, b = (torch.randn(width, device="cuda", generator=gen).to(torch.bfloat16).requires_grad_(True) for _ in range(2))
+    dy = torch.randn((2, width), device="cuda", generator=gen).to(torch.bfloat16)
+    y = layers.layer_norm(x, w, b)
+    dw, db = torch.autograd.grad(y, [w, b], dy)
+    u, e = 2.0 ** -8, 2.0 ** -24
+    hat = x.double() / (1 + 1e-5) ** 0.5
+    assert ((y.detach().double() - hat * w.detach().double() - b.detach().double()).abs()
+            <= (u + 8 * e) * (w.detach().double().abs() + b.detach().double().abs())).all()
+    assert torch.equal(db, (dy[0].float() + dy[1].float()).to(torch.bfloat16))
+    terms = dy.double() * hat
+    assert ((dw.double() - terms.sum(0)).abs() <= u * terms.sum(0).abs() + 8 * e * terms.abs().sum(0)).all()
