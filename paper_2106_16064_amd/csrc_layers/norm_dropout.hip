@@ -126,7 +126,7 @@ extern "C" int dgsp_layer_norm(int64_t rows, int64_t width, int type, int param_
 }
 
 extern "C" int64_t dgsp_layer_norm_backward_workspace_bytes(int64_t rows, int64_t width) {
-    if (rows < 0 || width < 1) return 0;
+    if (rows < 0 || width < 1 || rows > kMostRows || width > kMostRows) return 0;
     return 2 * backward_groups(Hold(width), rows) * width * 4;
 }
 

@@ -102,3 +102,14 @@ def test_sizes_of_a_block_without_rows():
               "            assert 0 <= size(0, *block, t) <= size(1, *block, t), (block, t)\n")
     run = subprocess.run([sys.executable, "-c", script], cwd=ROOT, capture_output=True, text=True)
     assert run.returncode == 0, (run.returncode, run.stderr)
+
+
+def test_sizes_of_extents_that_are_refused_are_zero():
+    L = layers.lib()
+    most = (1 << 31) - 1 - 4096
+    assert L.dgsp_layer_norm_backward_workspace_bytes(most, 64) > 0 and L.dgsp_layer_norm_backward_workspace_bytes(1, most) > 0
+    for rows, width in ((-1, 8), (8, 0), (8, -1), (most + 1, 64), (1, most + 1), (1 << 62, 8), (8, 1 << 62), (8, (1 << 63) - 1)):
+        assert L.dgsp_layer_norm_backward_workspace_bytes(rows, width) == 0, (rows, width)
+    for size in (L.dgsp_gated_ff_saved_bytes, L.dgsp_gated_ff_workspace_bytes, L.dgsp_gated_ff_backward_workspace_bytes):
+        for extents in ((most + 1, 8, 8, 8), (-1, 8, 8, 8), (8, 1 << 22, 8, 8), (8, 8, 1 << 62, 8), (8, 8, 8, 0)):
+            assert size(*extents, layers.F32) == 0, extents
