@@ -45,13 +45,20 @@ void check_like(const at::Tensor& t, const at::Tensor& x, const char* name) {
     if (t.device() != x.device()) refuse(std::string(name) + " must be on the device of x");
 }
 
+// With its sign in memory: views may be marked as negative in place of being written.
+at::Tensor signed_in_memory(const at::Tensor& t) { return t.is_neg() ? t.resolve_neg() : t; }
+
+// a norm's parameter as the library reads it; undefined: there is none
+at::Tensor packed(const at::Tensor& t) { return t.defined() ? signed_in_memory(t).contiguous() : t; }
+
 // The rows of a tensor whose last axis is the width.  What lies otherwise than row after row at one distance is copied.
 struct Rows {
     at::Tensor t;
     int64_t rows, width, ld;
 };
 
-Rows rows_of(const at::Tensor& given, const char* name) {
+Rows rows_of(const at::Tensor& any, const char* name) {
+    const at::Tensor given = signed_in_memory(any);
     if (given.dim() < 1) refuse(std::string(name) + " must have at least one axis");
     const int64_t width = given.size(-1), last = given.dim() - 1;
     int64_t rows = 1;
@@ -186,7 +193,7 @@ Norm run_norm(const at::Tensor& x, const at::Tensor& residual, const at::Tensor&
     if (!(eps >= 0.0f)) refuse("eps must not be negative");
     Rows add;
     Norm out;
-    const at::Tensor w = weight.defined() ? weight.contiguous() : weight, b = bias.defined() ? bias.contiguous() : bias;
+    const at::Tensor w = packed(weight), b = packed(bias);
     const c10::DeviceGuard guard(x.device());
     if (residual.defined()) {
         check_like(residual, x, "residual");
@@ -242,7 +249,7 @@ NormGradient run_norm_backward(const at::Tensor& s, const at::Tensor& residual, 
     if (weight.defined() && weight.scalar_type() != params) refuse("weight must have the type it had");
     check_params(s, weight, {});
     check_left(stats, at::kFloat, 2 * in.rows, s, "stats");
-    const at::Tensor w = weight.defined() ? weight.contiguous() : weight;
+    const at::Tensor w = packed(weight);
     const c10::DeviceGuard guard(s.device());
     NormGradient out;
     out.sum = empty_on(s.sizes(), s.scalar_type(), s);

@@ -237,3 +237,22 @@ def test_parameter_gradients_of_very_wide_rows():
     assert torch.equal(db, (dy[0].float() + dy[1].float()).to(torch.bfloat16))
     terms = dy.double() * hat
     assert ((dw.double() - terms.sum(0)).abs() <= u * terms.sum(0).abs() + 8 * e * terms.abs().sum(0)).all()
+
+
+# ---------------------------------------------------------------- views that count as negative
+
+def test_views_whose_sign_is_not_in_memory():
+    """torch marks some views as negative, such as the imaginary part of a conjugate, in place of writing them."""
+    show("negative views")
+    for dtype in TYPES:
+        for name, (call, inputs) in layer_calls(dtype).items():
+            grads = [torch.randn_like(t) for t in (lambda o: o if isinstance(o, tuple) else (o,))(call(*inputs))]
+            found = []
+            for view in (lambda t: torch._neg_view(-t), lambda t: t):
+                leaves = [view(t).requires_grad_(True) for t in inputs]
+                out = call(*leaves)
+                out = out if isinstance(out, tuple) else (out,)
+                found.append([*out, *torch.autograd.grad(out, leaves, [view(g) for g in grads])])
+            assert all(torch.equal(a, b) for a, b in zip(*found)), (name, dtype)
+    z = torch.randn((30, 1), device="cuda", dtype=torch.complex64)
+    assert torch.equal(layers.dropout(z.conj().imag, 0.5, 1), layers.dropout(-z.imag, 0.5, 1))
