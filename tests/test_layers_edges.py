@@ -256,3 +256,17 @@ def test_views_whose_sign_is_not_in_memory():
             assert all(torch.equal(a, b) for a, b in zip(*found)), (name, dtype)
     z = torch.randn((30, 1), device="cuda", dtype=torch.complex64)
     assert torch.equal(layers.dropout(z.conj().imag, 0.5, 1), layers.dropout(-z.imag, 0.5, 1))
+
+
+# ---------------------------------------------------------------- more rows than workgroups
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,width", [(70001, 8), (40003, 33), (33001, 64), (5001, 500), (4101, 600), (2501, 1001), (1700, 2050), (600, 8192), (530, 8200)])
+def test_norms_of_more_rows_than_workgroups(rows, width, dtype):
+    """Each goes on to further rows, asked for while the ones before are worked on; rows in a team's lanes, in a workgroup and read again."""
+    import test_layers as t
+    show("many rows", rows, width, dtype)
+    x, r, dy, ds = (t.normal((rows, width), dtype, 200 + i, 1.3, 0.4) for i in range(4))
+    w, b = t.normal((width,), dtype, 204, 0.2, 1.0), t.normal((width,), dtype, 205)
+    t.check_norm(x, w, b, dy)
+    t.check_add_norm(x, r, w, b, dy, ds, 0.25)

@@ -188,3 +188,23 @@ def test_the_bounds_tell_what_is_rounded(block, dtype):
         for of_factors in (True, False):
             wrong[of_factors] |= set(beyond(model(t, of_factors, not of_factors), want))
     assert {"dw_gate", "dw_up"} <= wrong[True] and {"dw_gate", "dw_up"} <= wrong[False]
+
+
+# width, hidden, out of every padded shape of the kernels that hold the weights, filling it and not
+NARROW = [(32, 64, 32), (30, 50, 7), (32, 128, 32), (20, 100, 31), (32, 256, 32), (9, 200, 24), (64, 64, 64), (33, 64, 40), (64, 128, 64), (60, 72, 50),
+          (64, 256, 64), (40, 130, 64), (128, 64, 128), (72, 33, 100), (128, 128, 128), (127, 128, 65)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("block", NARROW, ids=str)
+def test_narrow_blocks_of_many_rows(block, dtype):
+    """So many that workgroups go on to a second and a third tile, the last of which is not full."""
+    print("[case] narrow", block, dtype, flush=True)
+    t = operands(2 * 256 * 128 + 2 * 128 + 37, *block, dtype, "cuda")
+    with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CUDA]) as prof:
+        passes(t, "silu")
+        torch.cuda.synchronize()
+    names = " ".join(e.key for e in prof.key_averages())
+    assert "narrow_forward_kernel" in names and "narrow_backward" in names and "tile_kernel" not in names
+    check(t, "silu", dtype)
