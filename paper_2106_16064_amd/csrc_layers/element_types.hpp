@@ -22,11 +22,6 @@ __device__ __forceinline__ T from_float(float v) {
 
 // an element of a vector that is stored in T or, if `wide`, in float
 template <typename T>
-__device__ __forceinline__ float load_param(const void* p, int64_t i, bool wide) {
-    return wide ? static_cast<const float*>(p)[i] : to_float(static_cast<const T*>(p)[i]);
-}
-
-template <typename T>
 __device__ __forceinline__ void store_param(void* p, int64_t i, bool wide, float v) {
     if (wide)
         static_cast<float*>(p)[i] = v;
