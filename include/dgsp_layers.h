@@ -101,10 +101,11 @@ int64_t dgsp_layer_norm_backward_workspace_bytes(int64_t rows, int64_t width);
  *   workspace  dgsp_gated_ff_workspace_bytes(...) bytes, 16-byte aligned
  * Either size may be 0; the pointer is not looked at then.  (Blocks whose weights fit a CU's LDS make g, u and h again.)
  * Of 16-bit types h is rounded to `type`, as the matrix instructions take their operands; act(g) and u act'(g) are saved in
- * 32 bits.  Products of float matrices are sums of products of three bfloat16 parts of each number, as exact as 32-bit
- * arithmetic; an infinity or NaN in an operand makes infinity or NaN of the results that it belongs to, which of the two is
- * not said.
- * rows is below 2^31 - 4096, the three widths are at least 1 and below 2^22 - 7.
+ * 32 bits.  In float16 an h beyond 65504 becomes infinite, whatever w_down would have made of it.  Products of float matrices
+ * are sums of products of three bfloat16 parts of each number, as exact as 32-bit arithmetic.  An infinity or NaN in an operand,
+ * or a g or u beyond the range of 32 bits, makes infinity or NaN of the results that it belongs to; which of the two is not said.
+ * rows is below 2^31 - 4096, the three widths are at least 1 and below 2^22 - 7.  DGSP_ERR_UNSUPPORTED: a product has 2^23 tiles
+ * or more, which are 64 x 64 (of the projections 64 x 32) where it is small: float blocks of widths up to 32 from 2^29 - 63 rows on.
  */
 int dgsp_gated_ff(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type, int activation, const void *x,
                   int64_t ldx, const void *w_gate, int64_t ldg, const void *w_up, int64_t ldu, const void *w_down, int64_t ldd,
@@ -116,7 +117,7 @@ int64_t dgsp_gated_ff_workspace_bytes(int64_t rows, int64_t width, int64_t hidde
  * Its gradient.  With dh = dy w_down, dg = dh * u * act'(g) and du = dh * act(g):
  *     dx = dg w_gate + du w_up,  dw_gate = dg^T x,  dw_up = du^T x,  dw_down = dy^T h
  * dx is rows x width, the others have the shapes of the weights; NULL: not wanted.  Of 16-bit types dg and du are rounded
- * to `type`.
+ * to `type`: in float16 they become infinite beyond 65504 and lose bits below 2^-14, so that a loss wants scaling.  Limits as above.
  */
 int dgsp_gated_ff_backward(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type, int activation,
                            const void *x, int64_t ldx, const void *w_gate, int64_t ldg, const void *w_up, int64_t ldu,

@@ -113,3 +113,12 @@ def test_sizes_of_extents_that_are_refused_are_zero():
     for size in (L.dgsp_gated_ff_saved_bytes, L.dgsp_gated_ff_workspace_bytes, L.dgsp_gated_ff_backward_workspace_bytes):
         for extents in ((most + 1, 8, 8, 8), (-1, 8, 8, 8), (8, 1 << 22, 8, 8), (8, 8, 1 << 62, 8), (8, 8, 8, 0)):
             assert size(*extents, layers.F32) == 0, extents
+
+
+def test_a_block_of_more_tiles_than_a_launch_has_is_refused():
+    """Before anything is enqueued: the pointers are not looked at."""
+    L = layers.lib()
+    rows, p, most = 1 << 30, 1 << 20, (1 << 63) - 1
+    matrices = [p, 8] * 4
+    assert L.dgsp_gated_ff(rows, 8, 8, 8, layers.F32, layers.SILU, *matrices, p, 8, None, p, most, None) == dg.ERR_UNSUPPORTED
+    assert L.dgsp_gated_ff_backward(rows, 8, 8, 8, layers.F32, layers.SILU, *matrices, p, 8, p, p, p, p, p, p, most, None) == dg.ERR_UNSUPPORTED
