@@ -270,3 +270,34 @@ def test_norms_of_more_rows_than_workgroups(rows, width, dtype):
     w, b = t.normal((width,), dtype, 204, 0.2, 1.0), t.normal((width,), dtype, 205)
     t.check_norm(x, w, b, dy)
     t.check_add_norm(x, r, w, b, dy, ds, 0.25)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,width,hidden,out", [(70, 64, 128, 64), (70, 60, 100, 33), (70, 64, 256, 64), (70, 300, 264, 136), (300, 250, 333, 131), (4096, 256, 1024, 256)])
+def test_what_is_not_finite_stays_in_its_row(rows, width, hidden, out, dtype):
+    """An infinity or NaN in a row of x or dy is in that row's result and gradient, and in no other's; beside it the bits are the same."""
+    show("not finite", rows, width, hidden, out, dtype)
+    torch.manual_seed(0)
+    x, dy = torch.randn((rows, width), device="cuda").to(dtype), torch.randn((rows, out), device="cuda").to(dtype)
+    w = [(torch.randn(shape, device="cuda") * shape[1] ** -0.5).to(dtype) for shape in ((hidden, width), (hidden, width), (out, hidden))]
+
+    def passes(x, dy):
+        leaf = x.clone().requires_grad_(True)
+        y = layers.gated_ff(leaf, *w)
+        return y.detach(), torch.autograd.grad(y, leaf, dy)[0]
+
+    want = passes(x, dy)
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        spoilt, grad = x.clone(), dy.clone()
+        spoilt[[0, 37], [width - 1, 5]] = bad
+        grad[[1, rows - 1], [0, out - 1]] = bad
+        others = torch.ones(rows, dtype=torch.bool, device="cuda")
+        others[[0, 37]] = False
+        y, dx = passes(spoilt, dy)
+        assert torch.equal(y[others], want[0][others]) and torch.equal(dx[others], want[1][others])
+        assert not torch.isfinite(y[[0, 37]]).any()
+        y, dx = passes(x, grad)
+        others[:] = True
+        others[[1, rows - 1]] = False
+        assert torch.equal(y, want[0]) and torch.equal(dx[others], want[1][others])
+        assert not torch.isfinite(dx[[1, rows - 1]]).any()
