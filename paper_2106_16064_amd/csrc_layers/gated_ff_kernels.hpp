@@ -12,7 +12,7 @@ namespace dgsp {
 // (one unit in the last place of float each; the argument of the exponential is off by g 2^-24), and erf to 1.5e-7 (Abramowitz, Stegun,
 // Handbook of Mathematical Functions, 7.1.26), which is what 1 + erf(z) keeps of it in float anyway.  A third of the instructions of
 // the library's functions, which took longer than the products where the depth is small.  kFloat: results are float, and the rounding of
-// the sigmoid's argument is made up for.
+// the sigmoid's argument is made up for; the sigmoid counts as 0 from -87.3 on below, where silu is less than 1.1e-36.
 template <bool kFloat, int kCount>
 __device__ __forceinline__ void activate(int kind, const float (&g)[kCount], float (&value)[kCount], float (&slope)[kCount]) {
     if (kind == DGSP_ACT_RELU) {

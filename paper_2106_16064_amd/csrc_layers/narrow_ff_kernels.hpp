@@ -179,7 +179,8 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_forward_kernel(NarrowArgs<
 // A workgroup takes 16 rows a wave.  For 32 hidden values at a time each wave makes g, u, dh and from them dg, du and h of its rows,
 // adds to dx, and leaves dg, du and h in LDS; then each wave adds the rows of all waves to its own blocks of the weights' gradients,
 // which stay in registers until the workgroup's last tile.  For up to 256 hidden values: 64 -> 256 -> 64 at 2^18 rows 220 us, some of the
-// sums spilled (forward and backward pass 262 us, through matrix_tiles.hpp 626); 32 -> 256 -> 32 92 us.
+// sums spilled (41 registers, 48 where rows are not in whole pieces; forward and backward pass 262 us, through matrix_tiles.hpp 626, 60 -> 256
+// -> 60 288); 32 -> 256 -> 32 92 us.
 template <typename E, int kP, int kH, int kWaves, bool kFull>
 __global__ __launch_bounds__(64 * kWaves) void narrow_backward_staged_kernel(NarrowArgs<E> a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -303,8 +304,10 @@ __global__ __launch_bounds__(64 * kWaves) void narrow_backward_staged_kernel(Nar
 // The same with the weights in registers, where they and the sums fit: a wave takes 16 hidden values of all rows, so that it reads x and dy
 // where the kernel above reads weights, and the three gradients of its weights need nothing of other waves.  Here vertices are the rows of
 // g, u and dh, and the results are operands of a sum over the vertices where they lie.  dg and du go to LDS, transposed, for dx, of which
-// a wave takes 16 columns, 32 where waves are few.  128 -> 128 -> 128 at 2^18 rows: 174 us, though some of the weights are spilled, against
-// 393 us of the kernel above; 64 -> 128 -> 64 at 2^20: 200 against 307.
+// a wave takes 16 columns, 32 where waves are few.  128 -> 128 -> 128 at 2^18 rows: 174 us, though 157 registers of weights are spilled,
+// against 393 us of the kernel above; 64 -> 128 -> 64 at 2^20: 200 against 307.  Where rows are not in whole pieces or widths are between 65
+// and 127 the form of 128 x 128 spills 544: forward and backward pass 100 -> 128 -> 100 291 us, 127 -> 128 -> 65 341, 128 -> 128 -> 128 212;
+// 60 -> 128 -> 60 at 2^20, which spills none, 321 against 282.
 template <typename E, int kP, int kWaves, bool kFull>
 __global__ __launch_bounds__(64 * kWaves) void narrow_backward_kernel(NarrowArgs<E> a) {
 #if defined(__HIP_DEVICE_COMPILE__)
