@@ -301,3 +301,89 @@ def test_what_is_not_finite_stays_in_its_row(rows, width, hidden, out, dtype):
         others[[1, rows - 1]] = False
         assert torch.equal(y, want[0]) and torch.equal(dx[others], want[1][others])
         assert not torch.isfinite(dx[[1, rows - 1]]).any()
+
+
+# ---------------------------------------------------------------- offsets beyond 32 bits
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_rows_far_apart(dtype):
+    """2^30 elements from row to row of inputs, weights and gradients: the same bits as of packed ones."""
+    show("rows far apart", dtype)
+    torch.manual_seed(0)
+    rows, apart = 6, 1 << 30
+    store = torch.empty((rows - 1) * apart + 8192, dtype=dtype, device="cuda")
+
+    def far(t, at):
+        view = store.as_strided(t.shape, (apart, 1), at)
+        view.copy_(t)
+        return view
+
+    def same(call, inputs, grad):
+        found = []
+        for place in (far, lambda t, at: t):
+            grads = [place(g, 700 * (len(inputs) + i)) for i, g in enumerate(grad)]
+            leaves = [place(t, 700 * i).detach().requires_grad_(True) if t.dim() == 2 else t.requires_grad_(True) for i, t in enumerate(inputs)]
+            out = call(*leaves)
+            out = out if isinstance(out, tuple) else (out,)
+            found.append([*out, *torch.autograd.grad(out, leaves, grads)])
+        assert all(torch.equal(a, b) for a, b in zip(*found))
+
+    def normal(*shape):
+        return torch.randn(shape, device="cuda").to(dtype)
+
+    same(lambda x, w, b: layers.layer_norm(x, w, b), [normal(rows, 600), normal(600), normal(600)], [normal(rows, 600)])
+    same(lambda x, r: layers.add_layer_norm(x, r, p=0.25, seed=1), [normal(rows, 600), normal(rows, 600)], [normal(rows, 600)] * 2)
+    same(lambda x, r: layers.dropout(x, 0.25, 1, residual=r), [normal(rows, 600), normal(rows, 600)], [normal(rows, 600)])
+    for width in (64, 600):
+        same(layers.gated_ff, [normal(rows, width), normal(6, width), normal(6, width), normal(rows, 6)], [normal(rows, 6)])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_norms_of_more_than_2_to_the_31_elements(dtype):
+    """The first and the last rows give what they give alone, and the parameters' gradients are sums over all."""
+    show("many elements", dtype)
+    rows, width = (1 << 20) + 77, 2056
+    x = torch.empty((rows, width), dtype=dtype, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(0))
+    w = torch.randn(width, device="cuda").to(dtype).requires_grad_(True)
+    x.requires_grad_(True)
+    y = layers.layer_norm(x, w, None)
+    dx, dw = torch.autograd.grad(y, [x, w], x.detach())
+    for part in (slice(0, 100), slice(rows - 100, rows)):
+        alone = x.detach()[part].clone().requires_grad_(True)
+        one = layers.layer_norm(alone, w, None)
+        assert torch.equal(one, y[part]) and torch.equal(torch.autograd.grad(one, alone, alone.detach())[0], dx[part])
+    want = torch.zeros(width, dtype=torch.float64, device="cuda")
+    for part in x.detach().split(1 << 16):
+        s = part.double()
+        want += (s * torch.nn.functional.layer_norm(s, (width,))).sum(0)
+    assert ((dw.double() - want).abs() <= (UNIT[dtype] + 2.0 ** -10) * want).all()               # sums of squares: 2^-24 a term of the 1024 that a lane adds, and more
+    keep = layers.dropout(x.detach(), 0.5, 1, residual=x.detach())
+    assert torch.equal(keep[-100:, :8], torch.where(layers.dropout(torch.ones((rows, 8), device="cuda", dtype=dtype), 0.5, 1)[-100:] > 0, 3.0, 1.0).to(dtype) * x.detach()[-100:, :8])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_a_block_of_more_than_2_to_the_31_hidden_values(dtype):
+    """The first and the last rows against 64 bits with their bounds, the weights' gradients, sums over 2^20 rows, to a hundredth of their size."""
+    import test_layers_tiles as t
+    show("many hidden values", dtype)
+    rows, width, hidden, out = (1 << 20) + 77, 40, 2056, 24
+    gen = torch.Generator("cuda").manual_seed(0)
+
+    def normal(*shape, scale=1.0):
+        return torch.empty(shape, dtype=dtype, device="cuda").normal_(generator=gen).mul_(scale)
+
+    x, w, dy = normal(rows, width), [normal(hidden, width, scale=width ** -0.5), normal(hidden, width, scale=width ** -0.5),
+                                     normal(out, hidden, scale=hidden ** -0.5)], normal(rows, out)
+    y, dx, *dw = t.passes([x, *w, dy], "silu")
+    sums = [torch.zeros(v.shape, dtype=torch.float64, device="cuda") for v in w]
+    wide = [v.double() for v in w]
+    for first in range(0, rows, 1 << 16):
+        part = slice(first, min(rows, first + (1 << 16)))
+        found = t.definition(x[part].double(), *wide, dy[part].double(), "silu", dtype)
+        if first == 0 or part.stop == rows:
+            for got, (value, bound), name in zip((y[part], dx[part]), found, ("y", "dx")):
+                t.assert_within(got, value.cpu(), bound.cpu(), name)
+        for s, (value, _) in zip(sums, found[2:]):
+            s += value
+    for got, s in zip(dw, sums):
+        assert (got.double() - s).norm() <= 1e-2 * s.norm()
