@@ -13,6 +13,7 @@
 namespace dgsp {
 
 constexpr int64_t kMostRows = 2147483647LL - 4096;
+constexpr int64_t kCus = 256;
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
