@@ -1,6 +1,7 @@
 /*
  * libdgsp_layers - the layers that stand next to a sparse product in a graph network, for AMD MI355X (gfx950): layer norm,
- * dropout and the gated feed-forward block, each with its gradient.
+ * root-mean-square norm, dropout, the matrix product with its epilogue and the gated feed-forward block, each with its gradient, and
+ * the norm and the product in 8 bits.
  *
  * The dense operand of Y = A X holds one row of features per vertex.  Between two products a network adds the result to what
  * was there (a residual), normalises the rows, drops elements while it trains and runs a feed-forward block.
@@ -33,7 +34,7 @@ extern "C" {
 typedef enum { DGSP_F32 = 0, DGSP_BF16 = 1, DGSP_F16 = 2 } dgsp_type_t;
 
 /* silu(g) = g / (1 + exp(-g)); gelu(g) = g (1 + erf(g / sqrt 2)) / 2; relu(g) = max(g, 0), with derivative 0 at 0. */
-typedef enum { DGSP_ACT_SILU = 0, DGSP_ACT_GELU = 1, DGSP_ACT_RELU = 2 } dgsp_activation_t;
+typedef enum { DGSP_ACT_SILU = 0, DGSP_ACT_GELU = 1, DGSP_ACT_RELU = 2, DGSP_ACT_NONE = 3 } dgsp_activation_t;
 
 /*
  * Dropout without a stored mask: whether element (row, col) is kept is a function of seed, offset, row and col, so that the
@@ -124,6 +125,103 @@ int dgsp_gated_ff_backward(int64_t rows, int64_t width, int64_t hidden, int64_t 
                            const void *w_down, int64_t ldd, const void *dy, int64_t lddy, const void *saved, void *dx,
                            void *dw_gate, void *dw_up, void *dw_down, void *workspace, int64_t workspace_bytes, void *stream);
 int64_t dgsp_gated_ff_backward_workspace_bytes(int64_t rows, int64_t width, int64_t hidden, int64_t out_width, int type);
+
+/*
+ * Root-mean-square norm over the rows of s, where s = x, or s = residual + dropout(x) if residual is not NULL:
+ *     y = s / sqrt(mean(s^2) + eps) * weight
+ *   rstd   a float a row, 1 / sqrt(mean(s^2) + eps), for the backward pass; NULL: not wanted
+ * The other arguments and the limits are those of dgsp_layer_norm.
+ */
+int dgsp_rms_norm(int64_t rows, int64_t width, int type, int param_type, const void *x, int64_t ldx, const void *residual,
+                  int64_t ldr, const dgsp_dropout_t *dropout, const void *weight, float eps, void *y, int64_t ldy, void *sum,
+                  int64_t lds, float *rstd, void *stream);
+
+/*
+ * Its gradient.  With hat = s / sqrt(mean(s^2) + eps) and dhat = dy * weight:
+ *     dsum = (dhat - hat mean(dhat hat)) / sqrt(mean(s^2) + eps) + ds,   dweight = sum over the rows of dy hat
+ * The arguments are those of dgsp_layer_norm_backward.
+ *   workspace  dgsp_rms_norm_backward_workspace_bytes(rows, width) bytes, 16-byte aligned, if dweight is wanted
+ */
+int dgsp_rms_norm_backward(int64_t rows, int64_t width, int type, int param_type, const void *s, int64_t lds,
+                           const void *residual, int64_t ldr, const float *rstd, const void *weight, const void *dy, int64_t lddy,
+                           const void *ds, int64_t ldds, const dgsp_dropout_t *dropout, void *dsum, void *dx, void *dweight,
+                           void *workspace, int64_t workspace_bytes, void *stream);
+int64_t dgsp_rms_norm_backward_workspace_bytes(int64_t rows, int64_t width);
+
+/*
+ * Rows in 8 bits.  A row is cut into blocks of 32 columns, each with a power of two as its scale: the least 2^e with
+ * amax <= 448 2^e (DGSP_E4M3) or amax <= 127 2^e (DGSP_INT8), amax being the block's largest finite magnitude.  An element is
+ * stored as element / 2^e, in e4m3 (4 bits of exponent, 3 of fraction, no infinities) or as a whole number, rounded to nearest,
+ * ties to even.
+ *   values  rows of 32 ceil(width / 32) bytes, filled up with zeros, 16-byte aligned, ld a multiple of 16
+ *   scales  ceil(width / 128) * rows * 4 bytes, 4-byte aligned: byte b stands for 2^(b - 127), 255 for NaN; block k of row r at
+ *           ((k / 4) * rows + r) * 4 + k % 4.  Blocks of zeros have 127, as have places beyond the last block.
+ * e is at least -126 and at most 119 (DGSP_E4M3) or 121 (DGSP_INT8), for whole numbers of float16 matrices at least -24 and at
+ * most 9: what is read back is then in the range of the type; elements beyond 448 or 127 times the largest scale become that.
+ * An infinity or NaN becomes NaN: in e4m3 of the element, of whole numbers of its whole block.
+ */
+typedef enum { DGSP_E4M3 = 0, DGSP_INT8 = 1 } dgsp_kind_t;
+
+/* `type`: that of x or y.  rows and width are below 2^31 - 4096, width is at least 1. */
+int dgsp_quantise(int64_t rows, int64_t width, int type, int kind, const void *x, int64_t ldx, void *values, int64_t ldv,
+                  void *scales, void *stream);
+int dgsp_dequantise(int64_t rows, int64_t width, int type, int kind, const void *values, int64_t ldv, const void *scales, void *y,
+                    int64_t ldy, void *stream);
+
+/* dgsp_rms_norm without dropout, y in DGSP_E4M3: made from y in 32 bits. */
+int dgsp_rms_norm_8bit(int64_t rows, int64_t width, int type, int param_type, const void *x, int64_t ldx, const void *residual,
+                       int64_t ldr, const void *weight, float eps, void *values, int64_t ldv, void *scales, void *sum, int64_t lds,
+                       void *stream);
+
+/*
+ * What a product keeps for its backward pass.  DGSP_KEEP_WHOLE: x, and of z as much as the activation's derivative needs (z in
+ * `type`; of relu the derivative in a byte; without an activation nothing).  DGSP_KEEP_8BIT: x in DGSP_INT8, and act'(z) in steps of
+ * 1/112 in a byte, which has 0 and 1 exactly.
+ */
+typedef enum { DGSP_KEEP_NOTHING = 0, DGSP_KEEP_WHOLE = 1, DGSP_KEEP_8BIT = 2 } dgsp_keep_t;
+
+/*
+ * The matrix product with its epilogue:
+ *     y = act(z) + residual,   z = x weight^T + bias
+ *   x  rows x width;   weight  out_width x width;   residual, y  rows x out_width
+ *   bias        out_width elements of `bias_type`, which is `type` or DGSP_F32; NULL: 0
+ *   residual    NULL: 0
+ *   activation  DGSP_ACT_...
+ *   saved       dgsp_linear_saved_bytes(...) bytes, 16-byte aligned, for the backward pass; not looked at if that is 0
+ *   workspace   dgsp_linear_workspace_bytes(...) bytes, 16-byte aligned; not looked at if that is 0
+ * z, act(z) and the sum with the residual are held in 32 bits.  Float matrices, infinities, NaN and limits: as in dgsp_gated_ff.
+ */
+int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int type, int bias_type, int activation, int keep, const void *x,
+                int64_t ldx, const void *weight, int64_t ldw, const void *bias, const void *residual, int64_t ldr, void *y,
+                int64_t ldy, void *saved, void *workspace, int64_t workspace_bytes, void *stream);
+int64_t dgsp_linear_saved_bytes(int64_t rows, int64_t out_width, int type, int activation, int keep);
+int64_t dgsp_linear_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type);
+
+/*
+ * Its gradient.  With dz = dy act'(z):
+ *     dx = dz weight,   dweight = dz^T x,   dbias = sum over the rows of dz;   the residual's is dy
+ *   keep         what the forward pass kept, not DGSP_KEEP_NOTHING
+ *   x, x_scales  DGSP_KEEP_WHOLE: the matrix, NULL.  DGSP_KEEP_8BIT: values and scales of x in DGSP_INT8; ldx is that of the values.
+ *   dx, dweight, dbias   NULL: not wanted.  dx is rows x width, dweight out_width x width, both packed; dbias is of `bias_type`.
+ * Of 16-bit types dz is rounded to `type`, as the matrix instructions take their operands (dbias is summed before that): in
+ * float16 it becomes infinite beyond 65504 and loses bits below 2^-14.
+ */
+int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_width, int type, int bias_type, int activation, int keep,
+                         const void *x, int64_t ldx, const void *x_scales, const void *weight, int64_t ldw, const void *saved,
+                         const void *dy, int64_t lddy, void *dx, void *dweight, void *dbias, void *workspace, int64_t workspace_bytes,
+                         void *stream);
+int64_t dgsp_linear_backward_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type, int activation, int keep);
+
+/*
+ * The same product of operands in DGSP_E4M3, for serving: x is rows x width, weight out_width x width, sums in 32 bits.
+ *   type   of the residual and of y
+ *   ldx, ldw   of the values, in bytes
+ * Limits as above.
+ */
+int dgsp_linear_8bit(int64_t rows, int64_t width, int64_t out_width, int type, int bias_type, int activation, const void *x, int64_t ldx,
+                     const void *x_scales, const void *weight, int64_t ldw, const void *weight_scales, const void *bias,
+                     const void *residual, int64_t ldr, void *y, int64_t ldy, void *workspace, int64_t workspace_bytes, void *stream);
+int64_t dgsp_linear_8bit_workspace_bytes(int64_t rows, int64_t width, int64_t out_width);
 
 #ifdef __cplusplus
 }

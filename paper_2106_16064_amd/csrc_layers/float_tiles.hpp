@@ -257,7 +257,10 @@ __global__ __launch_bounds__(Shape::kThreads, 2) void float_tile_kernel(ProductA
             }
         }
     }
-    store_tile<Shape>(acc, args, tile, out);
+    if constexpr (Out::kReadLate)
+        store_tile<Shape>(acc, args, tile, argument_behind<Out, ProductArgs<float>>());
+    else
+        store_tile<Shape>(acc, args, tile, out);
 #endif
 }
 

@@ -9,6 +9,7 @@ namespace dgsp {
 // instructions take it; the other two are kept in 32 bits: rounded to 16 they would double the squared error of the gates' gradients.
 template <typename T>
 struct GatedUpOut {
+    static constexpr bool kReadLate = false;
     Kept<T> h;
     float *act, *mul;           // null: not wanted
     int activation;
@@ -61,6 +62,7 @@ struct GatedUpOut {
 // dh itself is not.
 template <typename T>
 struct GatedSlopeOut {
+    static constexpr bool kReadLate = false;
     const float *act, *mul;
     Kept<T> dg, du;
     template <int kEach>

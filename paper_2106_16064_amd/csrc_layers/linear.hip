@@ -1,0 +1,176 @@
+// Host side of the matrix product with its epilogue: argument checks, products and launches.  The C-ABI is documented in include/dgsp_layers.h.
+#include "column_sums.hpp"
+#include "linear_kernels.hpp"
+#include "products.hpp"
+#include "rows8_host.hpp"
+
+namespace {
+
+using namespace dgsp;
+
+bool linear_extents(int64_t rows, int64_t width, int64_t out_width, int type) {
+    return rows >= 0 && rows <= kMostRows && width >= 1 && width <= kMostWidth && out_width >= 1 && out_width <= kMostWidth && known_type(type);
+}
+
+bool known_epilogue(int activation) { return known_activation(activation) || activation == DGSP_ACT_NONE; }
+bool known_keep(int keep) { return keep >= DGSP_KEEP_NOTHING && keep <= DGSP_KEEP_8BIT; }
+
+// what the forward pass leaves of z: nothing, the slope in 8 bits, or z
+enum Left { kNothing, kCodes, kZ };
+Left left(int activation, int keep) {
+    if (activation == DGSP_ACT_NONE || keep == DGSP_KEEP_NOTHING) return kNothing;
+    return activation == DGSP_ACT_RELU || keep == DGSP_KEEP_8BIT ? kCodes : kZ;
+}
+
+struct ForwardPieces {
+    Cut up;
+    void *x, *weight, *partial;
+    ForwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t out_width, int type)
+        : up(cut(rows, out_width, width, 1, 1, type, false, true)), x(pieces.take(laid_out_bytes(rows, width, type))),
+          weight(pieces.take(laid_out_bytes(out_width, width, type))), partial(pieces.take(partial_bytes(up, rows, out_width, 1))) {}
+};
+
+// How the rows are dealt out for dz and the sums over them.
+struct Slices {
+    int lanes;
+    int64_t across, down;       // workgroups along a row, along the rows
+    Slices(int64_t rows, int64_t columns) {
+        const int64_t chunks = ceil_div(columns, kChunk);
+        lanes = 1;
+        while (lanes < chunks && lanes < 256) lanes *= 2;
+        across = ceil_div(chunks, lanes);
+        down = std::max<int64_t>(1, std::min(ceil_div(rows, (256 / lanes) * 4), ceil_div(8 * kCus, across)));
+    }
+};
+
+struct BackwardPieces {
+    Cut dx, dw;
+    Slices slices;
+    void *x, *weight, *dz, *partial, *sums;
+    BackwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t out_width, int type, int activation, int keep)
+        : dx(cut(rows, width, out_width, 1, 1, type, false, true)), dw(cut(out_width, width, rows, 1, 1, type, false, true)), slices(rows, out_width),
+          x(pieces.take(keep == DGSP_KEEP_8BIT ? kept_bytes(rows, width, type) : laid_out_bytes(rows, width, type))),
+          weight(pieces.take(laid_out_bytes(out_width, width, type))),
+          dz(pieces.take(activation != DGSP_ACT_NONE ? kept_bytes(rows, out_width, type) : laid_out_bytes(rows, out_width, type))),
+          partial(pieces.take(std::max(partial_bytes(dx, rows, width, 1), partial_bytes(dw, out_width, width, 1)))),
+          sums(pieces.take(slices.down * out_width * 4)) {}
+};
+
+}  // namespace
+
+extern "C" int64_t dgsp_linear_saved_bytes(int64_t rows, int64_t out_width, int type, int activation, int keep) {
+    if (!linear_extents(rows, 1, out_width, type) || !known_epilogue(activation) || !known_keep(keep)) return 0;
+    const Left what = left(activation, keep);
+    return what == kNothing ? 0 : what == kCodes ? rows * padded(out_width, 8) : kept_bytes(rows, out_width, type);
+}
+
+extern "C" int64_t dgsp_linear_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type) {
+    if (!linear_extents(rows, width, out_width, type)) return 0;
+    Pieces pieces(nullptr);
+    ForwardPieces need(pieces, rows, width, out_width, type);
+    return pieces.used();
+}
+
+extern "C" int64_t dgsp_linear_backward_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type, int activation, int keep) {
+    if (!linear_extents(rows, width, out_width, type) || !known_epilogue(activation) || !known_keep(keep)) return 0;
+    Pieces pieces(nullptr);
+    BackwardPieces need(pieces, rows, width, out_width, type, activation, keep);
+    return pieces.used();
+}
+
+extern "C" int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int type, int bias_type, int activation, int keep, const void* x,
+                           int64_t ldx, const void* weight, int64_t ldw, const void* bias, const void* residual, int64_t ldr, void* y,
+                           int64_t ldy, void* saved, void* workspace, int64_t workspace_bytes, void* stream) {
+    if (!linear_extents(rows, width, out_width, type) || !known_epilogue(activation) || !known_keep(keep) ||
+        (bias_type != type && bias_type != DGSP_F32))
+        return DGSP_ERR_INVALID_ARG;
+    if (rows == 0) return DGSP_OK;
+    const Left what = left(activation, keep);
+    if (!readable(x, rows, width, ldx) || !readable(weight, out_width, width, ldw) || (residual && !readable(residual, rows, out_width, ldr)) ||
+        !writable(y, rows, out_width, ldy) || (what != kNothing && !saved) || !aligned(saved, 16) ||
+        !enough(workspace, workspace_bytes, dgsp_linear_workspace_bytes(rows, width, out_width, type)))
+        return DGSP_ERR_INVALID_ARG;
+    Pieces pieces(workspace);
+    const ForwardPieces at(pieces, rows, width, out_width, type);
+    if (!launchable(at.up, 1)) return DGSP_ERR_UNSUPPORTED;
+    return with_type(type, [&](auto element) {
+        using T = decltype(element);
+        const auto on = static_cast<hipStream_t>(stream);
+        Operands<T> operands;
+        ProductArgs<T> args = product_args<T>(at.up, rows, out_width, width, 1);
+        args.a[0] = operands.add(x, rows, width, ldx, at.x);
+        args.b[0] = operands.add(weight, out_width, width, ldw, at.weight);
+        operands.launch(on);
+        const auto four = [](const void* p, int64_t ld) { return ld % 4 == 0 && aligned(p, 4 * sizeof(T)); };
+        const LinearOut<T> out{static_cast<T*>(y), ldy, four(y, ldy), bias, bias_type != type, static_cast<const T*>(residual), ldr, four(residual, ldr),
+                               activation, what == kZ ? static_cast<T*>(saved) : nullptr, what == kCodes ? static_cast<uint8_t*>(saved) : nullptr,
+                               padded(out_width, 8), at.up.splits > 1 ? static_cast<float*>(at.partial) : nullptr};
+        launch<T, false, true, true>(at.up, args, out, on);
+        if (out.partial)
+            linear_join_kernel<T><<<(unsigned)std::min<int64_t>(ceil_div(rows * ceil_div(out_width, 4), 256), 4096), 256, 0, on>>>(rows, out_width, at.up.splits, out);
+        return launched();
+    });
+}
+
+extern "C" int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_width, int type, int bias_type, int activation, int keep,
+                                    const void* x, int64_t ldx, const void* x_scales, const void* weight, int64_t ldw, const void* saved,
+                                    const void* dy, int64_t lddy, void* dx, void* dweight, void* dbias, void* workspace, int64_t workspace_bytes,
+                                    void* stream) {
+    if (!linear_extents(rows, width, out_width, type) || !known_epilogue(activation) || !known_keep(keep) || keep == DGSP_KEEP_NOTHING ||
+        (bias_type != type && bias_type != DGSP_F32) ||
+        !enough(workspace, workspace_bytes, dgsp_linear_backward_workspace_bytes(rows, width, out_width, type, activation, keep)))
+        return DGSP_ERR_INVALID_ARG;
+    const bool in_8bit = keep == DGSP_KEEP_8BIT;
+    const Left what = left(activation, keep);
+    if (rows > 0 && (!readable(dy, rows, out_width, lddy) || (what != kNothing && !saved) || !aligned(saved, 16) ||
+                     (dx && !readable(weight, out_width, width, ldw)) ||
+                     (dweight && !(in_8bit ? rows8_lies(x, rows, width, ldx, x_scales) : readable(x, rows, width, ldx)))))
+        return DGSP_ERR_INVALID_ARG;
+    Pieces pieces(workspace);
+    const BackwardPieces at(pieces, rows, width, out_width, type, activation, keep);
+    if (!launchable(at.dx, 1) || !launchable(at.dw, 1)) return DGSP_ERR_UNSUPPORTED;
+    return with_type(type, [&](auto element) {
+        using T = decltype(element);
+        const auto on = static_cast<hipStream_t>(stream);
+        const Slices& slices = at.slices;
+        const int64_t kept_ld = padded(out_width, 8);
+        Operands<T> operands;
+        Source<T> grad{}, in{}, w{};
+        if (activation == DGSP_ACT_NONE)
+            grad = operands.add(dy, rows, out_width, lddy, at.dz);
+        else
+            grad = {static_cast<const T*>(at.dz), rows, kept_ld, kept_ld};
+        if (dweight && in_8bit) {
+            const int64_t ld = padded(width, 8);
+            if (rows > 0)
+                launch_dequantise<T>(DGSP_INT8, rows, width, rows8(const_cast<void*>(x), rows, width, ldx, const_cast<void*>(x_scales)),
+                                     static_cast<T*>(at.x), ld, on);
+            in = {static_cast<const T*>(at.x), rows, ld, ld};
+        } else if (dweight) {
+            in = operands.add(x, rows, width, ldx, at.x);
+        }
+        if (dx) w = operands.add(weight, out_width, width, ldw, at.weight);
+        operands.launch(on);
+        if (rows > 0 && (activation != DGSP_ACT_NONE ? dx || dweight || dbias : dbias != nullptr)) {
+            const LinearSlopeArgs<T> args{rows, out_width, slices.lanes, static_cast<const T*>(dy), lddy, what == kZ ? static_cast<const T*>(saved) : nullptr,
+                                          what == kCodes ? static_cast<const uint8_t*>(saved) : nullptr, kept_ld, activation,
+                                          activation != DGSP_ACT_NONE && (dx || dweight) ? static_cast<T*>(at.dz) : nullptr,
+                                          dbias ? static_cast<float*>(at.sums) : nullptr};
+            linear_slope_kernel<T><<<dim3((unsigned)slices.across, (unsigned)slices.down), 256, 0, on>>>(args);
+        }
+        if (dbias) launch_column_sums<T>(out_width, rows > 0 ? slices.down : 0, static_cast<const float*>(at.sums), dbias, bias_type != type, on);
+        if (dx) {
+            ProductArgs<T> args = product_args<T>(at.dx, rows, width, out_width, 1);
+            args.a[0] = grad;
+            args.b[0] = w;
+            product<T, true, false>(at.dx, args, {{static_cast<T*>(dx), nullptr}, width, false, nullptr}, at.partial, on);
+        }
+        if (dweight) {
+            ProductArgs<T> args = product_args<T>(at.dw, out_width, width, rows, 1);
+            args.a[0] = grad;
+            args.b[0] = in;
+            product<T, false, false>(at.dw, args, {{static_cast<T*>(dweight), nullptr}, width, false, nullptr}, at.partial, on);
+        }
+        return launched();
+    });
+}

@@ -1,0 +1,243 @@
+// y = act(x w^T + bias) + residual on matrix_tiles.hpp: what becomes of the product of a tile, and what the backward pass makes of dy first.
+//
+// The epilogue adds the bias to the sum in 32 bits, applies the activation, adds the residual and rounds once.  For the backward pass it
+// leaves what the activation's derivative is made of: z in the matrix's type (its rounding moves act'(z) by |z act''(z)| half a step, a
+// fifth of what rounding dz itself costs), or act'(z) in steps of 1/112 in 8 bits, which has 0 and 1 exactly: all of relu's, and what gelu
+// (-0.13 ... 1.13) and silu (-0.10 ... 1.10) come to far from 0.
+#pragma once
+
+#include "product_kernels.hpp"
+
+namespace dgsp {
+
+constexpr float kSlopeSteps = 112.0f;
+
+enum Epilogue { kPlain, kSilu, kGelu, kRelu };
+
+template <bool kFloat, int kCount>
+__device__ __forceinline__ void activate_or_not(int kind, const float (&z)[kCount], float (&value)[kCount], float (&slope)[kCount]) {
+    if (kind == DGSP_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            value[i] = z[i];
+            slope[i] = 1.0f;
+        }
+    } else {
+        activate<kFloat>(kind, z, value, slope);
+    }
+}
+
+__device__ __forceinline__ int slope_code(float slope) { return (int)rintf(slope * kSlopeSteps) & 0xff; }
+
+// z as it is kept: an infinity of rounding would have no slope
+template <typename T>
+__device__ __forceinline__ float inside_range(float z) {
+    constexpr float kMost = std::is_same_v<T, f16_t> ? 65504.0f : 3.38953139e38f;
+    return fabsf(z) > kMost ? __builtin_copysignf(kMost, z) : z;
+}
+
+// How many columns there are from n on.  Rows of fragments ask each for itself: the comparisons with it, kept for all of them, would be more than
+// the scalar registers hold.
+__device__ __forceinline__ int columns_left(int64_t columns, int64_t n) {
+    int left = (int)(columns - n);
+    asm volatile("" : "+v"(left));
+    return left;
+}
+
+// four neighbours, of whatever alignment; `here` of them are there
+template <typename T>
+__device__ __forceinline__ f32x4 load4(const T* p, bool vectors, int here) {
+    using T4 = T __attribute__((ext_vector_type(4)));
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (vectors && here >= 4) {
+        const T4 t = *reinterpret_cast<const T4*>(p);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = to_float((T)t[r]);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < here) v[r] = to_float(p[r]);
+    }
+    return v;
+}
+
+template <typename T>
+struct LinearOut {
+    static constexpr bool kReadLate = true;
+    T* y;
+    int64_t ldy;
+    bool vectors;               // four neighbours of y may be written at once
+    const void* bias;           // null: none
+    bool wide;                  // the bias in float
+    const T* residual;          // null: none
+    int64_t ldr;
+    bool residual_vectors;
+    int activation;
+    T* z;                       // null: not wanted; ld is `kept_ld`, a multiple of 8
+    uint8_t* codes;             // null: not wanted; likewise
+    int64_t kept_ld;
+    float* partial;             // not null: split results, [split][m][n padded to 4], for linear_join_kernel
+
+    // `left` of its elements are there from n on
+    __device__ __forceinline__ f32x4 bias_at(int64_t n, int left) const {
+        if (!bias) return f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        return wide ? load4(static_cast<const float*>(bias) + n, false, left) : load4(static_cast<const T*>(bias) + n, false, left);
+    }
+    // four neighbours, n a multiple of 4, of `left` columns
+    __device__ __forceinline__ void put(int64_t m, int64_t n, int left, const float* value, const float* slope, const float* before, f32x4 add) const {
+        using T4 = T __attribute__((ext_vector_type(4)));
+        if (z) {
+            T4 kept;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) kept[r] = from_float<T>(inside_range<T>(before[r]));
+            *reinterpret_cast<T4*>(z + m * kept_ld + n) = kept;
+        }
+        if (codes) {
+            uint32_t word = 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) word |= (uint32_t)slope_code(slope[r]) << (8 * r);
+            *reinterpret_cast<uint32_t*>(codes + m * kept_ld + n) = word;
+        }
+        T* to = y + m * ldy + n;
+        if (vectors && left >= 4) {
+            T4 out;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) out[r] = from_float<T>(value[r] + add[r]);
+            *reinterpret_cast<T4*>(to) = out;
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r < left) to[r] = from_float<T>(value[r] + add[r]);
+        }
+    }
+
+    template <int kEach>
+    struct Added {
+        f32x4 residual[kEach];
+    };
+    template <int kEach, typename E>
+    __device__ __forceinline__ Added<kEach> ask(const ProductArgs<E>& args, int64_t m, int64_t n) const {
+        Added<kEach> out;
+        const int left = columns_left(args.n, n);
+        const bool wanted = residual && !partial && m < args.m;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            out.residual[j] = wanted && left > 16 * j ? load4(residual + m * ldr + n + 16 * j, residual_vectors, left - 16 * j) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        return out;
+    }
+    template <int kEach, typename E>
+    __device__ __forceinline__ void row(const ProductArgs<E>& args, const TileIndex& tile, int64_t m, int64_t n, const Added<kEach>& added,
+                                        const f32x4 (&v)[kEach][1]) const {
+        if (m >= args.m) return;
+        const int left = columns_left(args.n, n);
+        if (partial) {
+            const int64_t padded = (args.n + 3) / 4 * 4;
+            float* to = partial + ((int64_t)tile.split * args.m + m) * padded + n;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                if (left <= 16 * j) break;
+                *reinterpret_cast<f32x4*>(to + 16 * j) = v[j][0];
+            }
+            return;
+        }
+        float in[4 * kEach], value[4 * kEach], slope[4 * kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const f32x4 b = bias_at(n + 16 * j, left - 16 * j);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) in[4 * j + r] = v[j][0][r] + b[r];
+        }
+        activate_or_not<sizeof(T) == 4>(activation, in, value, slope);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            if (left <= 16 * j) break;
+            put(m, n + 16 * j, left - 16 * j, value + 4 * j, slope + 4 * j, in + 4 * j, added.residual[j]);
+        }
+    }
+};
+
+// The sum of the splits, in order, and the epilogue.
+template <typename T>
+__global__ __launch_bounds__(256) void linear_join_kernel(int64_t m, int64_t n, int splits, LinearOut<T> out) {
+    const int64_t quads = (n + 3) / 4, count = m * quads, step = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < count; i += step) {
+        const int64_t row = i / quads, col = (i - row * quads) * 4;
+        const int left = (int)(n - col);
+        f32x4 sum = out.bias_at(col, left);
+        const f32x4 add = out.residual ? load4(out.residual + row * out.ldr + col, out.residual_vectors, left) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < splits; s += kJoinAhead) {
+            f32x4 ahead[kJoinAhead];
+#pragma unroll
+            for (int j = 0; j < kJoinAhead; ++j)
+                ahead[j] = s + j < splits ? *reinterpret_cast<const f32x4*>(out.partial + 4 * ((s + j) * count + i)) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < kJoinAhead; ++j) sum += ahead[j];
+        }
+        float in[4] = {sum[0], sum[1], sum[2], sum[3]}, value[4], slope[4];
+        activate_or_not<sizeof(T) == 4>(out.activation, in, value, slope);
+        out.put(row, col, left, value, slope, in, add);
+    }
+}
+
+// ---------------------------------------------------------------- the backward pass
+
+template <typename T>
+struct LinearSlopeArgs {
+    int64_t rows, columns;
+    int lanes;                  // of a row, a power of two up to 256
+    const T* dy;
+    int64_t lddy;
+    const T* z;                 // one of these two, or none: the slope is 1
+    const uint8_t* codes;
+    int64_t kept_ld;
+    int activation;
+    T* dz;                      // null: not wanted; ld is `kept_ld`, and what is beyond the columns is 0
+    float* partial;             // [workgroup's slice of the rows][columns]: sums of dz before it is rounded; null: not wanted
+};
+
+// dz = dy act'(z), and the workgroup's sums of it over its rows.  A lane keeps eight columns and walks down the rows; workgroups stand side by
+// side where a row is longer than 2048 columns.
+template <typename T>
+__global__ __launch_bounds__(256) void linear_slope_kernel(LinearSlopeArgs<T> a) {
+    __shared__ float sums[256 * kChunk];
+    const int teams = 256 / a.lanes, lane = threadIdx.x & (a.lanes - 1), team = threadIdx.x / a.lanes;
+    const int64_t col = ((int64_t)blockIdx.x * a.lanes + lane) * kChunk, here = a.columns - col;
+    float db[kChunk];
+#pragma unroll
+    for (int j = 0; j < kChunk; ++j) db[j] = 0.0f;
+    if (here > 0)
+        for (int64_t row = (int64_t)blockIdx.y * teams + team; row < a.rows; row += (int64_t)gridDim.y * teams) {
+            float d[kChunk], slope[kChunk];
+            widen(load_chunk(a.dy + row * a.lddy + col, here), d);
+            if (a.codes) {
+                const uint2 codes = *reinterpret_cast<const uint2*>(a.codes + row * a.kept_ld + col);
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) slope[j] = (float)(int8_t)((j < 4 ? codes.x : codes.y) >> (8 * (j % 4)) & 0xffu) * (1.0f / kSlopeSteps);
+            } else if (a.z) {
+                float z[kChunk], value[kChunk];
+                widen(load_chunk(a.z + row * a.kept_ld + col, kChunk), z);
+                activate<sizeof(T) == 4>(a.activation, z, value, slope);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) slope[j] = 1.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j) {
+                d[j] = j < here ? d[j] * slope[j] : 0.0f;
+                db[j] += d[j];
+            }
+            if (a.dz) store_chunk(a.dz + row * a.kept_ld + col, kChunk, d);
+        }
+    if (!a.partial) return;
+#pragma unroll
+    for (int j = 0; j < kChunk; ++j) sums[threadIdx.x * kChunk + j] = db[j];
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.lanes * kChunk; c += 256) {
+        float v = 0.0f;
+        for (int t = 0; t < teams; ++t) v += sums[t * a.lanes * kChunk + c];
+        const int64_t column = (int64_t)blockIdx.x * a.lanes * kChunk + c;
+        if (column < a.columns) a.partial[blockIdx.y * a.columns + column] = v;
+    }
+}
+
+}  // namespace dgsp

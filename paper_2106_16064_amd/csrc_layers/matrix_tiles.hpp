@@ -371,6 +371,23 @@ __device__ __forceinline__ void store_tile(const f32x4 (&acc)[Shape::kFragsN][Sh
 
 struct Nothing {};
 
+// A kernel's argument, read where it stands, `at` bytes behind the first one's.  What an epilogue needs would be read ahead of the products
+// otherwise, and its scalars be spilled meanwhile.
+template <typename Out, typename... Before>
+__device__ __forceinline__ Out argument_behind() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr size_t at = (sizeof(Before) + ... + 0);       // all of them whole words of 8 bytes
+    static_assert(alignof(Out) == 8 && ((alignof(Before) == 8) && ...));
+    auto* p = (const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    Out out;
+    __builtin_memcpy(&out, p + at, sizeof(Out));
+    return out;
+#else
+    return {};
+#endif
+}
+
 // A workgroup per tile.
 template <typename E, typename Shape, bool kARows, bool kBRows, typename Out>
 __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesASimd) void tile_kernel(ProductArgs<E> args, Out out) {
@@ -378,7 +395,10 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesASimd) void tile_kern
     const TileIndex tile = tile_of(args);
     TileProduct<E, Shape, kARows, kBRows> product;
     product.run(args, tile);
-    store_tile<Shape>(product.acc, args, tile, out);
+    if constexpr (Out::kReadLate)
+        store_tile<Shape>(product.acc, args, tile, argument_behind<Out, ProductArgs<E>>());
+    else
+        store_tile<Shape>(product.acc, args, tile, out);
 #endif
 }
 

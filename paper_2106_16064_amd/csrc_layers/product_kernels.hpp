@@ -101,6 +101,7 @@ __global__ __launch_bounds__(256) void lay_out_kernel(Layouts<T> all) {
 
 template <typename T>
 struct ProductOut {
+    static constexpr bool kReadLate = false;
     T* c[2];                    // one per batch
     int64_t ld;
     bool vectors;               // four neighbours may be written at once

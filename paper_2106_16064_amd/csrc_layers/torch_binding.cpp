@@ -658,12 +658,19 @@ PyObject* gated_ff_backward(PyObject* const* a, Py_ssize_t n) {
     return wrap_all({out[0], out[1], out[2], out[3]});
 }
 
+#include "torch_rms_norm.hpp"
+
+#include "torch_linear.hpp"
+
 #define LAYERS_ENTRY(name) \
     {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(&entry<checked<name>>)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
     {"set_error_type", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(&entry<set_error_type>)), METH_FASTCALL, nullptr},
     LAYERS_ENTRY(dropout), LAYERS_ENTRY(layer_norm), LAYERS_ENTRY(add_layer_norm), LAYERS_ENTRY(gated_ff), LAYERS_ENTRY(layer_norm_forward),
     LAYERS_ENTRY(layer_norm_backward), LAYERS_ENTRY(dropout_forward), LAYERS_ENTRY(gated_ff_forward), LAYERS_ENTRY(gated_ff_backward),
+    LAYERS_ENTRY(rms_norm), LAYERS_ENTRY(add_rms_norm), LAYERS_ENTRY(rms_norm_forward), LAYERS_ENTRY(rms_norm_backward), LAYERS_ENTRY(rms_norm_8bit),
+    LAYERS_ENTRY(quantise), LAYERS_ENTRY(dequantise), LAYERS_ENTRY(linear), LAYERS_ENTRY(linear_forward), LAYERS_ENTRY(linear_backward),
+    LAYERS_ENTRY(linear_8bit),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_dgsp_layers_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

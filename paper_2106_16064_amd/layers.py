@@ -1,4 +1,4 @@
-"""The layers beside a sparse product: layer norm, dropout and the gated feed-forward block, on the dense rows of features.
+"""The layers beside a sparse product: norms, dropout, the matrix product and the gated feed-forward block, on the dense rows of features.
 
 ``SparseOperator`` (``autograd.py``) multiplies by the matrix; a graph network then works on the result row by row.  Here are
 these steps as differentiable functions of GPU tensors in float32, bfloat16 or float16, over the HIP library
@@ -7,6 +7,10 @@ bits every time.
 
     s = residual + dropout(A x);  y = layer norm of s:      y, s = add_layer_norm(op(x), x, weight, bias, p=0.1, seed=7, offset=step)
     s + dropout(feed-forward block of y):                    dropout(gated_ff(y, w_gate, w_up, w_down), 0.1, 7, step, residual=s)
+
+    root-mean-square norm, and the product after it:        linear(rms_norm(x, g), w, b, "gelu", residual=x)
+    the same with activations kept in 8 bits:               linear(rms_norm(x, g), w, b, "gelu", residual=x, keep_8bit=True)
+    and in 8 bits, for serving:                             linear_8bit(rms_norm_8bit(x, g), quantise(w), b, "gelu", residual=x)
 
 Tensors may have any number of leading axes; the last one is the width.  Rows that lie at one distance from each other (a
 column slice, a broadcast row) are taken as they are, other orders are copied first.  Work runs on the current stream and can be
@@ -22,6 +26,7 @@ import ctypes
 import functools
 import importlib.util
 from pathlib import Path
+from typing import NamedTuple
 
 from . import binding as dg
 
@@ -31,11 +36,17 @@ NATIVE_PATH = LIB_PATH.with_name("_dgsp_layers_torch.so")
 F32, BF16, F16 = 0, 1, 2
 SILU, GELU, RELU = 0, 1, 2
 ACTIVATIONS = {"silu": SILU, "gelu": GELU, "relu": RELU}
+NO_ACTIVATION = 3
+E4M3, INT8 = 0, 1
+KINDS = {"e4m3": E4M3, "int8": INT8}
+KEEP_NOTHING, KEEP_WHOLE, KEEP_8BIT = 0, 1, 2
 
 EXPORTS = (
     "dgsp_dropout", "dgsp_layer_norm", "dgsp_layer_norm_backward", "dgsp_layer_norm_backward_workspace_bytes", "dgsp_gated_ff",
     "dgsp_gated_ff_saved_bytes", "dgsp_gated_ff_workspace_bytes", "dgsp_gated_ff_backward",
-    "dgsp_gated_ff_backward_workspace_bytes",
+    "dgsp_gated_ff_backward_workspace_bytes", "dgsp_rms_norm", "dgsp_rms_norm_backward", "dgsp_rms_norm_backward_workspace_bytes",
+    "dgsp_quantise", "dgsp_dequantise", "dgsp_rms_norm_8bit", "dgsp_linear", "dgsp_linear_saved_bytes", "dgsp_linear_workspace_bytes",
+    "dgsp_linear_backward", "dgsp_linear_backward_workspace_bytes", "dgsp_linear_8bit", "dgsp_linear_8bit_workspace_bytes",
 )
 
 
@@ -66,6 +77,19 @@ def lib():
         L.dgsp_layer_norm_backward_workspace_bytes.argtypes = [i64, i64]
         for name in ("saved", "workspace", "backward_workspace"):
             getattr(L, f"dgsp_gated_ff_{name}_bytes").argtypes = [i64, i64, i64, i64, ci]
+        L.dgsp_rms_norm.argtypes = [i64, i64, ci, ci, vp, i64, vp, i64, drop, vp, cf, vp, i64, vp, i64, vp, vp]
+        L.dgsp_rms_norm_backward.argtypes = [i64, i64, ci, ci, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, drop, vp, vp, vp, vp, i64, vp]
+        L.dgsp_rms_norm_backward_workspace_bytes.argtypes = [i64, i64]
+        L.dgsp_quantise.argtypes = [i64, i64, ci, ci, vp, i64, vp, i64, vp, vp]
+        L.dgsp_dequantise.argtypes = [i64, i64, ci, ci, vp, i64, vp, vp, i64, vp]
+        L.dgsp_rms_norm_8bit.argtypes = [i64, i64, ci, ci, vp, i64, vp, i64, vp, cf, vp, i64, vp, vp, i64, vp]
+        L.dgsp_linear.argtypes = [i64] * 3 + [ci] * 4 + [vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp]
+        L.dgsp_linear_saved_bytes.argtypes = [i64, i64, ci, ci, ci]
+        L.dgsp_linear_workspace_bytes.argtypes = [i64, i64, i64, ci]
+        L.dgsp_linear_backward.argtypes = [i64] * 3 + [ci] * 4 + [vp, i64, vp, vp, i64, vp, vp, i64, vp, vp, vp, vp, i64, vp]
+        L.dgsp_linear_backward_workspace_bytes.argtypes = [i64, i64, i64, ci, ci, ci]
+        L.dgsp_linear_8bit.argtypes = [i64] * 3 + [ci] * 3 + [vp, i64, vp, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp]
+        L.dgsp_linear_8bit_workspace_bytes.argtypes = [i64, i64, i64]
         _lib = L
     return _lib
 
@@ -120,6 +144,103 @@ def gated_ff(x, w_gate, w_up, w_down, activation="silu"):
         raise dg.DgspError(f"activation must be one of {', '.join(ACTIVATIONS)}") from None
     y = (_native or native()).gated_ff(x, w_gate, w_up, w_down, act)
     return _functions().gated.apply(x, w_gate, w_up, w_down, act) if y is None else y
+
+
+def rms_norm(x, weight=None, eps=1e-5):
+    """``x / sqrt(mean(x^2) + eps) * weight`` over the last axis.  ``weight``: one axis as long, in the type of ``x`` or float32, or None."""
+    y = (_native or native()).rms_norm(x, weight, eps)
+    return _functions().rms.apply(x, None, weight, eps, 0.0, 0, 0)[0] if y is None else y
+
+
+def add_rms_norm(x, residual, weight=None, eps=1e-5, p=0.0, seed=0, offset=0):
+    """``s = residual + dropout(x)`` and the root-mean-square norm of ``s``, in one pass; returns ``(y, s)`` as ``add_layer_norm`` does."""
+    out = (_native or native()).add_rms_norm(x, residual, weight, eps, p, seed, offset)
+    return _functions().rms.apply(x, residual, weight, eps, p, seed, offset) if out is None else out
+
+
+class Rows8(NamedTuple):
+    """Rows in 8 bits: blocks of 32 columns, each with a power of two as its scale.
+
+    ``values``: the rows' elements over their scales, float8_e4m3fn or int8, the last axis filled up with zeros to whole blocks.
+    ``scales``: uint8, ``ceil(width / 128) x rows x 4``, byte ``b`` for ``2^(b - 127)``: block ``k`` of row ``r`` at ``[k // 4, r, k % 4]``;
+    255 is NaN, and places beyond the last block hold 127.  ``width``: how many columns there are."""
+    values: object
+    scales: object
+    width: int
+
+
+def quantise(x, kind="e4m3"):
+    """``x`` as :class:`Rows8`: "e4m3", which ``linear_8bit`` reads, or "int8", which is nearer to ``x``.  Each element is rounded to the
+    nearest value, ties to even; it has no gradient."""
+    if kind not in ("e4m3", "int8"):
+        raise dg.DgspError(f"kind must be one of {', '.join(KINDS)}")
+    return Rows8(*(_native or native()).quantise(x, KINDS[kind]), x.shape[-1])
+
+
+def dequantise(rows, dtype=None):
+    """The numbers that :class:`Rows8` stand for, as a tensor of ``dtype`` (float32 if None, bfloat16 or float16)."""
+    values, scales, width = _as_rows8(rows, "rows")
+    return (_native or native()).dequantise(values, scales, width, F32 if dtype is None else _type_number(dtype))
+
+
+def rms_norm_8bit(x, weight=None, eps=1e-5):
+    """The root-mean-square norm of ``x`` as :class:`Rows8` in e4m3, rounded once; for serving: it has no gradient."""
+    return Rows8(*(_native or native()).rms_norm_8bit(x, None, weight, eps), x.shape[-1])
+
+
+def add_rms_norm_8bit(x, residual, weight=None, eps=1e-5):
+    """``s = residual + x`` and the root-mean-square norm of ``s`` as :class:`Rows8` in e4m3; returns ``(y, s)``.  It has no gradient."""
+    _need_tensor(residual, "residual")
+    values, scales, s = (_native or native()).rms_norm_8bit(x, residual, weight, eps)
+    return Rows8(values, scales, x.shape[-1]), s
+
+
+def linear(x, weight, bias=None, activation=None, residual=None, keep_8bit=False):
+    """``act(x weight^T + bias) + residual`` in one pass; ``activation``: "silu", "gelu", "relu" or None.
+
+    ``weight`` is out_width x width in the type of ``x``; ``bias`` has one axis of out_width, in the type of ``x`` or float32;
+    ``residual`` has the shape and type of the result.  ``keep_8bit``: what the backward pass needs of the activations is kept in 8 bits,
+    ``x`` as whole numbers with a scale for every 32 columns and the activation's derivative in steps of 1/112.  The result is the same; the
+    weight's gradient is that of the ``x`` kept, and those of ``x``, weight and bias are made with the derivative kept."""
+    act = _epilogue(activation)
+    y = (_native or native()).linear(x, weight, bias, act, residual, bool(keep_8bit))
+    return _functions().linear.apply(x, weight, bias, act, residual, bool(keep_8bit)) if y is None else y
+
+
+def linear_8bit(x, weight, bias=None, activation=None, residual=None, dtype=None):
+    """``linear`` of :class:`Rows8` in e4m3, for serving: products of 8 bits, sums in 32, a result of ``dtype`` (bfloat16 if None, float32
+    or float16).  ``bias``: of that type or float32; ``residual``: of that type.  It has no gradient."""
+    act = _epilogue(activation)
+    type_number = BF16 if dtype is None else _type_number(dtype)
+    return (_native or native()).linear_8bit(*_as_rows8(x, "x"), *_as_rows8(weight, "weight"), bias, act, residual, type_number)
+
+
+def _epilogue(activation):
+    if activation is None:
+        return NO_ACTIVATION
+    try:
+        return ACTIVATIONS[activation]
+    except (KeyError, TypeError):
+        raise dg.DgspError(f"activation must be None or one of {', '.join(ACTIVATIONS)}") from None
+
+
+def _as_rows8(rows, name):
+    if not isinstance(rows, tuple) or len(rows) != 3:
+        raise dg.DgspError(f"{name} must be Rows8: values, scales and width")
+    return rows
+
+
+def _need_tensor(t, name):
+    if t is None:
+        raise dg.DgspError(f"{name} must be a tensor")
+
+
+def _type_number(dtype):
+    import torch
+    try:
+        return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}[dtype]
+    except (KeyError, TypeError):
+        raise dg.DgspError("dtype must be float32, bfloat16 or float16") from None
 
 
 @functools.lru_cache(maxsize=None)
@@ -184,4 +305,37 @@ def _functions():
             x, w_gate, w_up, w_down, saved = ctx.saved_tensors
             return (*native().gated_ff_backward(x, w_gate, w_up, w_down, ctx.activation, dy, saved), None)
 
-    return types.SimpleNamespace(norm=Norm, dropout=Dropped, gated=Gated)
+    class Rms(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, residual, weight, eps, p, seed, offset):
+            y, s, rstd = native().rms_norm_forward(x, residual, weight, eps, p, seed, offset)
+            ctx.residual = residual is not None
+            again = ctx.residual and x.dtype != torch.float32
+            saved, ctx.drop = keep((p, seed, offset), s if ctx.residual and not again else x, residual if again else None, rstd, weight)
+            ctx.save_for_backward(*saved)
+            return (y, s) if ctx.residual else (y,)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dy, ds=None):
+            s, added, rstd, weight, offset = ctx.saved_tensors
+            dropped = ctx.residual and ctx.drop[0] > 0
+            dsum, dx, dweight = native().rms_norm_backward(s, added, rstd, weight, dy, ds, int(dropped), *given(ctx.drop, offset))
+            return dx if dropped else dsum, dsum if ctx.residual else None, dweight, None, None, None, None
+
+    class Linear(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, activation, residual, keep_8bit):
+            y, saved, values, scales = native().linear_forward(x, weight, bias, activation, residual, keep_8bit)
+            ctx.activation, ctx.residual = activation, residual is not None
+            ctx.save_for_backward(values if keep_8bit else x, scales, weight, bias, saved)
+            return y
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dy):
+            x, scales, weight, bias, saved = ctx.saved_tensors
+            dx, dweight, dbias = native().linear_backward(x, scales, weight, bias, saved, dy, ctx.activation)
+            return dx, dweight, dbias, None, dy if ctx.residual else None, None
+
+    return types.SimpleNamespace(norm=Norm, dropout=Dropped, gated=Gated, rms=Rms, linear=Linear)
