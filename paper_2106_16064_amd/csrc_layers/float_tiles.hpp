@@ -258,7 +258,7 @@ __global__ __launch_bounds__(Shape::kThreads, 2) void float_tile_kernel(ProductA
         }
     }
     if constexpr (Out::kReadLate)
-        store_tile<Shape>(acc, args, tile, argument_behind<Out, ProductArgs<float>>());
+        argument_behind<Out, ProductArgs<float>>().template store<Shape>(acc, args, tile);
     else
         store_tile<Shape>(acc, args, tile, out);
 #endif

@@ -1,7 +1,6 @@
 // Host side of the matrix product with its epilogue: argument checks, products and launches.  The C-ABI is documented in include/dgsp_layers.h.
 #include "column_sums.hpp"
-#include "linear_kernels.hpp"
-#include "products.hpp"
+#include "linear_host.hpp"
 #include "rows8_host.hpp"
 
 namespace {
@@ -101,10 +100,8 @@ extern "C" int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int t
         args.a[0] = operands.add(x, rows, width, ldx, at.x);
         args.b[0] = operands.add(weight, out_width, width, ldw, at.weight);
         operands.launch(on);
-        const auto four = [](const void* p, int64_t ld) { return ld % 4 == 0 && aligned(p, 4 * sizeof(T)); };
-        const LinearOut<T> out{static_cast<T*>(y), ldy, four(y, ldy), bias, bias_type != type, static_cast<const T*>(residual), ldr, four(residual, ldr),
-                               activation, what == kZ ? static_cast<T*>(saved) : nullptr, what == kCodes ? static_cast<uint8_t*>(saved) : nullptr,
-                               padded(out_width, 8), at.up.splits > 1 ? static_cast<float*>(at.partial) : nullptr};
+        const LinearOut<T> out = linear_out<T>(y, ldy, bias, bias_type != type, residual, ldr, activation, what == kZ ? saved : nullptr,
+                                               what == kCodes ? saved : nullptr, out_width, at.up.splits > 1 ? at.partial : nullptr);
         launch<T, false, true, true>(at.up, args, out, on);
         if (out.partial)
             linear_join_kernel<T><<<(unsigned)std::min<int64_t>(ceil_div(rows * ceil_div(out_width, 4), 256), 4096), 256, 0, on>>>(rows, out_width, at.up.splits, out);

@@ -1,6 +1,5 @@
 // Host side of the matrix product of rows in 8 bits: argument checks and launches.  The C-ABI is documented in include/dgsp_layers.h.
-#include "linear_kernels.hpp"
-#include "products.hpp"
+#include "linear_host.hpp"
 #include "rows8_host.hpp"
 #include "tiles_8bit.hpp"
 
@@ -60,9 +59,8 @@ extern "C" int dgsp_linear_8bit(int64_t rows, int64_t width, int64_t out_width, 
         args.a[0] = source8(x, rows, width, ldx);
         args.b[0] = source8(weight, out_width, width, ldw);
         const Scales8 scales{static_cast<const uint8_t*>(x_scales), static_cast<const uint8_t*>(weight_scales), rows, out_width, ceil_div(width, 4 * kBlock)};
-        const auto four = [](const void* p, int64_t ld) { return ld % 4 == 0 && aligned(p, 4 * sizeof(T)); };
-        const LinearOut<T> out{static_cast<T*>(y), ldy, four(y, ldy), bias, bias_type != type, static_cast<const T*>(residual), ldr, four(residual, ldr),
-                               activation, nullptr, nullptr, padded(out_width, 8), c.splits > 1 ? static_cast<float*>(workspace) : nullptr};
+        const LinearOut<T> out = linear_out<T>(y, ldy, bias, bias_type != type, residual, ldr, activation, nullptr, nullptr, out_width,
+                                               c.splits > 1 ? workspace : nullptr);
         launch8(c, args, scales, out, on);
         if (out.partial)
             linear_join_kernel<T><<<(unsigned)std::min<int64_t>(ceil_div(rows * ceil_div(out_width, 4), 256), 4096), 256, 0, on>>>(rows, out_width, c.splits, out);

@@ -14,22 +14,21 @@ constexpr float kSlopeSteps = 112.0f;
 
 enum Epilogue { kPlain, kSilu, kGelu, kRelu };
 
+// act(z) alone (activate() without the derivative, which is then never made)
 template <bool kFloat, int kCount>
-__device__ __forceinline__ void activate_or_not(int kind, const float (&z)[kCount], float (&value)[kCount], float (&slope)[kCount]) {
+__device__ __forceinline__ void activate_only(int kind, const float (&z)[kCount], float (&value)[kCount]) {
     if (kind == DGSP_ACT_NONE) {
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) {
-            value[i] = z[i];
-            slope[i] = 1.0f;
-        }
+        for (int i = 0; i < kCount; ++i) value[i] = z[i];
     } else {
+        float slope[kCount];
         activate<kFloat>(kind, z, value, slope);
     }
 }
 
 __device__ __forceinline__ int slope_code(float slope) { return (int)rintf(slope * kSlopeSteps) & 0xff; }
 
-// z as it is kept: an infinity of rounding would have no slope
+// z as it was kept: an infinity, of z or of its rounding, has the slope of a number far from 0
 template <typename T>
 __device__ __forceinline__ float inside_range(float z) {
     constexpr float kMost = std::is_same_v<T, f16_t> ? 65504.0f : 3.38953139e38f;
@@ -44,7 +43,7 @@ __device__ __forceinline__ int columns_left(int64_t columns, int64_t n) {
     return left;
 }
 
-// four neighbours, of whatever alignment; `here` of them are there
+// four neighbours, at once where they lie so; `here` of them are there
 template <typename T>
 __device__ __forceinline__ f32x4 load4(const T* p, bool vectors, int here) {
     using T4 = T __attribute__((ext_vector_type(4)));
@@ -66,12 +65,11 @@ struct LinearOut {
     static constexpr bool kReadLate = true;
     T* y;
     int64_t ldy;
-    bool vectors;               // four neighbours of y may be written at once
-    const void* bias;           // null: none
+    bool vectors, bias_vectors, residual_vectors;       // four neighbours may be read or written at once
     bool wide;                  // the bias in float
+    const void* bias;           // null: none
     const T* residual;          // null: none
     int64_t ldr;
-    bool residual_vectors;
     int activation;
     T* z;                       // null: not wanted; ld is `kept_ld`, a multiple of 8
     uint8_t* codes;             // null: not wanted; likewise
@@ -81,77 +79,104 @@ struct LinearOut {
     // `left` of its elements are there from n on
     __device__ __forceinline__ f32x4 bias_at(int64_t n, int left) const {
         if (!bias) return f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        return wide ? load4(static_cast<const float*>(bias) + n, false, left) : load4(static_cast<const T*>(bias) + n, false, left);
+        return wide ? load4(static_cast<const float*>(bias) + n, bias_vectors, left) : load4(static_cast<const T*>(bias) + n, bias_vectors, left);
     }
-    // four neighbours, n a multiple of 4, of `left` columns
-    __device__ __forceinline__ void put(int64_t m, int64_t n, int left, const float* value, const float* slope, const float* before, f32x4 add) const {
+    // kCount groups of four neighbours, kStep apart: z -> what is kept, and y
+    template <bool kWhole, int kCount, int kStep>
+    __device__ __forceinline__ void finish(int64_t m, int64_t n, int left, const float (&in)[4 * kCount], const f32x4 (&add)[kCount]) const {
         using T4 = T __attribute__((ext_vector_type(4)));
-        if (z) {
-            T4 kept;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) kept[r] = from_float<T>(inside_range<T>(before[r]));
-            *reinterpret_cast<T4*>(z + m * kept_ld + n) = kept;
-        }
+        float value[4 * kCount];
         if (codes) {
-            uint32_t word = 0;
+            float slope[4 * kCount];
+            activate<sizeof(T) == 4>(activation, in, value, slope);
+            uint8_t* to = codes + m * kept_ld + n;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) word |= (uint32_t)slope_code(slope[r]) << (8 * r);
-            *reinterpret_cast<uint32_t*>(codes + m * kept_ld + n) = word;
+            for (int j = 0; j < kCount; ++j) {
+                uint32_t word = 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) word |= (uint32_t)slope_code(slope[4 * j + r]) << (8 * r);
+                if (kWhole || left > kStep * j) *reinterpret_cast<uint32_t*>(to + kStep * j) = word;
+            }
+        } else {
+            activate_only<sizeof(T) == 4>(activation, in, value);
+        }
+        if (z) {
+            T* to = z + m * kept_ld + n;
+#pragma unroll
+            for (int j = 0; j < kCount; ++j)
+                if (kWhole || left > kStep * j)
+                    *reinterpret_cast<T4*>(to + kStep * j) = T4{from_float<T>(in[4 * j]), from_float<T>(in[4 * j + 1]), from_float<T>(in[4 * j + 2]), from_float<T>(in[4 * j + 3])};
         }
         T* to = y + m * ldy + n;
-        if (vectors && left >= 4) {
+#pragma unroll
+        for (int j = 0; j < kCount; ++j) {
+            if (!kWhole && left <= kStep * j) break;
             T4 out;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) out[r] = from_float<T>(value[r] + add[r]);
-            *reinterpret_cast<T4*>(to) = out;
-        } else {
+            for (int r = 0; r < 4; ++r) out[r] = from_float<T>(value[4 * j + r] + add[j][r]);
+            if (kWhole || (vectors && left - kStep * j >= 4)) {
+                *reinterpret_cast<T4*>(to + kStep * j) = out;
+            } else {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (r < left) to[r] = from_float<T>(value[r] + add[r]);
+                for (int r = 0; r < 4; ++r)
+                    if (kStep * j + r < left) to[kStep * j + r] = out[r];
+            }
         }
     }
 
-    template <int kEach>
-    struct Added {
-        f32x4 residual[kEach];
-    };
-    template <int kEach, typename E>
-    __device__ __forceinline__ Added<kEach> ask(const ProductArgs<E>& args, int64_t m, int64_t n) const {
-        Added<kEach> out;
-        const int left = columns_left(args.n, n);
-        const bool wanted = residual && !partial && m < args.m;
+    // The results of a tile; kWhole: all of it is inside, and lies in whole vectors.
+    template <bool kWhole, typename Shape, typename E>
+    __device__ __forceinline__ void rows(const f32x4 (&acc)[Shape::kFragsN][Shape::kFragsM], const ProductArgs<E>& args, const TileIndex& tile, int64_t m, int64_t n) const {
+        constexpr int kEach = Shape::kFragsN;
+        const int all = columns_left(args.n, n);
+        f32x4 b[kEach], add[kEach];
 #pragma unroll
-        for (int j = 0; j < kEach; ++j)
-            out.residual[j] = wanted && left > 16 * j ? load4(residual + m * ldr + n + 16 * j, residual_vectors, left - 16 * j) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        return out;
-    }
-    template <int kEach, typename E>
-    __device__ __forceinline__ void row(const ProductArgs<E>& args, const TileIndex& tile, int64_t m, int64_t n, const Added<kEach>& added,
-                                        const f32x4 (&v)[kEach][1]) const {
-        if (m >= args.m) return;
-        const int left = columns_left(args.n, n);
-        if (partial) {
-            const int64_t padded = (args.n + 3) / 4 * 4;
-            float* to = partial + ((int64_t)tile.split * args.m + m) * padded + n;
+        for (int j = 0; j < kEach; ++j) b[j] = bias_at(n + 16 * j, kWhole ? 4 : all - 16 * j);
+        auto ask = [&](int i) {
+            const int left = columns_left(args.n, n);
+            const T* from = residual + (m + 16 * i) * ldr + n;
+            const bool wanted = kWhole || m + 16 * i < args.m;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                add[j] = wanted && (kWhole || left > 16 * j) ? load4(from + 16 * j, kWhole || residual_vectors, kWhole ? 4 : left - 16 * j) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        };
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) add[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (residual) ask(0);
+#pragma unroll
+        for (int i = 0; i < Shape::kFragsM; ++i) {
+            float in[4 * kEach];
+            f32x4 now[kEach];
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
-                if (left <= 16 * j) break;
-                *reinterpret_cast<f32x4*>(to + 16 * j) = v[j][0];
+                now[j] = add[j];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) in[4 * j + r] = acc[j][i][r] + b[j][r];
             }
-            return;
+            if (residual && i + 1 < Shape::kFragsM) ask(i + 1);
+            if (kWhole || m + 16 * i < args.m) finish<kWhole, kEach, 16>(m + 16 * i, n, columns_left(args.n, n), in, now);
         }
-        float in[4 * kEach], value[4 * kEach], slope[4 * kEach];
+    }
+    template <typename Shape, typename E>
+    __device__ __forceinline__ void store(const f32x4 (&acc)[Shape::kFragsN][Shape::kFragsM], const ProductArgs<E>& args, const TileIndex& tile) const {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int64_t m = tile.m * Shape::kM + wave / Shape::kWavesN * Shape::kFragsM * 16 + lane % 16;
+        const int64_t n = tile.n * Shape::kColumns + wave % Shape::kWavesN * Shape::kFragsN * 16 + lane / 16 * 4;
+        if (partial) {
+            const int64_t padded = (args.n + 3) / 4 * 4;
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            const f32x4 b = bias_at(n + 16 * j, left - 16 * j);
+            for (int i = 0; i < Shape::kFragsM; ++i) {
+                if (m + 16 * i >= args.m) break;
+                float* to = partial + ((int64_t)tile.split * args.m + m + 16 * i) * padded + n;
+                const int left = columns_left(args.n, n);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) in[4 * j + r] = v[j][0][r] + b[r];
-        }
-        activate_or_not<sizeof(T) == 4>(activation, in, value, slope);
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            if (left <= 16 * j) break;
-            put(m, n + 16 * j, left - 16 * j, value + 4 * j, slope + 4 * j, in + 4 * j, added.residual[j]);
+                for (int j = 0; j < Shape::kFragsN; ++j)
+                    if (left > 16 * j) *reinterpret_cast<f32x4*>(to + 16 * j) = acc[j][i];
+            }
+        } else if ((tile.m + 1) * Shape::kM <= args.m && (tile.n + 1) * Shape::kColumns <= args.n && vectors && (!residual || residual_vectors)) {
+            rows<true, Shape>(acc, args, tile, m, n);
+        } else {
+            rows<false, Shape>(acc, args, tile, m, n);
         }
     }
 };
@@ -173,9 +198,9 @@ __global__ __launch_bounds__(256) void linear_join_kernel(int64_t m, int64_t n, 
 #pragma unroll
             for (int j = 0; j < kJoinAhead; ++j) sum += ahead[j];
         }
-        float in[4] = {sum[0], sum[1], sum[2], sum[3]}, value[4], slope[4];
-        activate_or_not<sizeof(T) == 4>(out.activation, in, value, slope);
-        out.put(row, col, left, value, slope, in, add);
+        const float in[4] = {sum[0], sum[1], sum[2], sum[3]};
+        const f32x4 adds[1] = {add};
+        out.template finish<false, 1, 16>(row, col, left, in, adds);
     }
 }
 
@@ -216,6 +241,8 @@ __global__ __launch_bounds__(256) void linear_slope_kernel(LinearSlopeArgs<T> a)
             } else if (a.z) {
                 float z[kChunk], value[kChunk];
                 widen(load_chunk(a.z + row * a.kept_ld + col, kChunk), z);
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) z[j] = inside_range<T>(z[j]);
                 activate<sizeof(T) == 4>(a.activation, z, value, slope);
             } else {
 #pragma unroll

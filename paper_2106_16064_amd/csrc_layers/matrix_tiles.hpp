@@ -396,7 +396,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesASimd) void tile_kern
     TileProduct<E, Shape, kARows, kBRows> product;
     product.run(args, tile);
     if constexpr (Out::kReadLate)
-        store_tile<Shape>(product.acc, args, tile, argument_behind<Out, ProductArgs<E>>());
+        argument_behind<Out, ProductArgs<E>>().template store<Shape>(product.acc, args, tile);
     else
         store_tile<Shape>(product.acc, args, tile, out);
 #endif

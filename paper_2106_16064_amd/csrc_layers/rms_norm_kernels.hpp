@@ -26,6 +26,14 @@ struct RmsArgs {
 
 constexpr ScaleRange kE4m3Range{1, 246};
 
+// 1 / sqrt(mean + eps).  Before a rounding to 8 bits the last steps are made in 64 bits: an error of the mean's quotient or of the root would move a
+// whole row, and carry as many of its elements across a border between two steps as their own roundings do.
+template <bool k8bit>
+__device__ __forceinline__ float reciprocal_root(float squares, int64_t width, float part, float eps) {
+    if constexpr (k8bit) return (float)(1.0 / sqrt((double)squares / (double)width + (double)eps));
+    return 1.0f / sqrtf(squares * part + eps);
+}
+
 template <typename T, bool kWhole, bool kAdd, bool k8bit>
 __global__ __launch_bounds__(kWhole ? 1024 : 256) void rms_norm_kernel(RmsArgs<T> a) {
     const Team<kWhole> team(a.lanes);
@@ -63,7 +71,7 @@ __global__ __launch_bounds__(kWhole ? 1024 : 256) void rms_norm_kernel(RmsArgs<T
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) squares[0] += s[j] * s[j];
         team.sum(squares, turn);
-        const float rstd = 1.0f / sqrtf(squares[0] * part + a.eps);
+        const float rstd = reciprocal_root<k8bit>(squares[0], a.width, part, a.eps);
         float out[kChunk];
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) out[j] = inside && j < here ? s[j] * rstd * w[j] : 0.0f;
@@ -216,7 +224,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(RmsArgs<T> a) {
             for (int j = 0; j < kChunk; ++j) squares[0] += c * kChunk + j < a.width ? v[j] * v[j] : 0.0f;
         }
         team.sum(squares, turn);
-        const float rstd = 1.0f / sqrtf(squares[0] * part + a.eps);
+        const float rstd = reciprocal_root<k8bit>(squares[0], a.width, part, a.eps);
         for (int64_t c = threadIdx.x; c < chunks; c += blockDim.x) {
             const int64_t col = c * kChunk, here = a.width - col;
             float w[kChunk], out[kChunk];

@@ -22,11 +22,12 @@ struct Scales8 {
     int64_t groups;
 };
 
-#if defined(__HIP_DEVICE_COMPILE__)
-__device__ __forceinline__ f32x4 multiply8(i32x8 a, i32x8 b, f32x4 c, int scale_a, int scale_b) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, scale_a, 0, scale_b);
+// c += a b in place, written out for the same reasons as accumulate(); the wait is for operands and scales that vector instructions wrote.
+__device__ __forceinline__ void accumulate8(i32x8 a, i32x8 b, f32x4& c, int scale_a, int scale_b) {
+    asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]"
+                 : "+v"(c)
+                 : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b));
 }
-#endif
 
 template <typename Shape>
 struct Tile8Product {
@@ -59,8 +60,8 @@ struct Tile8Product {
         a_loader.init(lane, wave * kARowsEach, args.a[0].ld);
         b_loader.init(lane, wave * kBRowsEach, args.b[0].ld);
         const uint32_t a_lds = lds_at + wave * ALoader::kInstructions * kWaveBytes, b_lds = lds_at + kABytes + wave * BLoader::kInstructions * kWaveBytes;
-        auto a_at = ALoader::begin(args.a[0], i0, k_first, wave * kARowsEach);
-        auto b_at = BLoader::begin(args.b[0], j0, k_first, wave * kBRowsEach);
+        auto a_from = ALoader::begin(args.a[0], i0, k_first, wave * kARowsEach);
+        auto b_from = BLoader::begin(args.b[0], j0, k_first, wave * kBRowsEach);
 
         // the first half of the waves brings A's scales, the second B's, 64 rows each; where there are more waves than that, some the same
         constexpr int kHalf = Shape::kWaves / 2;
@@ -72,8 +73,8 @@ struct Tile8Product {
         const uint32_t scales_lds = lds_at + kABytes + kBBytes + (of_a ? 0 : kAScales) + part * 256;
 
         auto load = [&](uint32_t buffer) {
-            a_loader.issue(a_at, args.a[0].ld, a_lds + buffer);
-            b_loader.issue(b_at, args.b[0].ld, b_lds + buffer);
+            a_loader.issue(a_from, args.a[0].ld, a_lds + buffer);
+            b_loader.issue(b_from, args.b[0].ld, b_lds + buffer);
             const int64_t at = (group * scale_rows + scale_row) * 4, left = scales.groups * scale_rows * 4 - at;
             const uint64_t address = reinterpret_cast<uint64_t>(scales_from + at);
             const u32x4 resource = {(uint32_t)address, (uint32_t)(address >> 32) & 0xffffu, left > 256 ? 256u : left > 0 ? (uint32_t)left : 0u, 0x00020000u};
@@ -92,40 +93,88 @@ struct Tile8Product {
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
-        // of a fragment's row, block lane / 16
+        // Where a fragment's chunks and scale stand in a stage; those of further fragments are constants away.
+        struct Places {
+            uint32_t low, high, scale;
+            __device__ __forceinline__ Places in(uint32_t buffer) const {
+                Places p = {low + buffer, high + buffer, scale + buffer};
+                asm volatile("" : "+v"(p.low), "+v"(p.high), "+v"(p.scale));        // one addition a stage, not one a fragment
+                return p;
+            }
+        };
         const int row = lane % 16, a_first = wave_m * Shape::kFragsM * 16 + row, b_first = wave_n * Shape::kFragsN * 16 + row;
-        const int in_row = ((lane / 16) ^ (row & 7)) * 16;
-        auto fragment = [&](const char* from) {
-            const u32x4 low = *reinterpret_cast<const u32x4*>(from + in_row), high = *reinterpret_cast<const u32x4*>(from + (in_row ^ 64));
-            return i32x8{(int)low[0], (int)low[1], (int)low[2], (int)low[3], (int)high[0], (int)high[1], (int)high[2], (int)high[3]};
+        const uint32_t in_row = (lane / 16 ^ (row & 7)) * 16;
+        const Places of_a_stage = {lds_at + a_first * kStageBytes + in_row, lds_at + a_first * kStageBytes + (in_row ^ 64), lds_at + kABytes + kBBytes + a_first * 4 + lane / 16};
+        const Places of_b_stage = {lds_at + kABytes + b_first * kStageBytes + in_row, lds_at + kABytes + b_first * kStageBytes + (in_row ^ 64),
+                                   lds_at + kABytes + kBBytes + kAScales + b_first * 4 + lane / 16};
+        struct Fragment {
+            i32x8 elements;
+            int scale;
+        };
+        auto fragment = [&](const Places& at, int i) {
+            using Quads = const __attribute__((address_space(3))) u32x4*;
+            using Byte = const __attribute__((address_space(3))) uint8_t*;
+            const u32x4 low = *(Quads)(uintptr_t)(at.low + i * 16 * kStageBytes), high = *(Quads)(uintptr_t)(at.high + i * 16 * kStageBytes);
+            return Fragment{i32x8{(int)low[0], (int)low[1], (int)low[2], (int)low[3], (int)high[0], (int)high[1], (int)high[2], (int)high[3]},
+                            *(Byte)(uintptr_t)(at.scale + i * 64)};
+        };
+        // Fragments of B stay for a stage and have a second place for the next one's.  Those of A come kAhead rows before they are multiplied; when
+        // the last ones of a stage are there all waves meet, and from then on fragments are read of the next stage, which has arrived, while
+        // the last rows are multiplied, and the buffer takes the stage after that.
+        constexpr int kAhead = 2, kRows = Shape::kFragsM;
+        static_assert(kRows % kAhead == 0);
+        Fragment a[kAhead], b[Shape::kFragsN], b_next[Shape::kFragsN];
+        auto multiply_row = [&](int i) {
+#pragma unroll
+            for (int j = 0; j < Shape::kFragsN; ++j) accumulate8(b[j].elements, a[i % kAhead].elements, acc[j][i], b[j].scale, a[i % kAhead].scale);
+        };
+        auto first_rows = [&](const Places& at) {
+#pragma unroll
+            for (int i = 0; i < kRows - kAhead; ++i) {
+                multiply_row(i);
+                a[i % kAhead] = fragment(at, i + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         };
         for (int i = 0; i < min(total, Shape::kBuffers); ++i) load(i * kStage);
+        arrive(min(total, Shape::kBuffers) - 1);
         uint32_t here = 0;
-        for (int step = 0; step < total; ++step) {
-            arrive(min(total - 1 - step, Shape::kBuffers - 1));
-            const char* const stage = lds + here;
-            const uint8_t* const stage_scales = reinterpret_cast<const uint8_t*>(stage + kABytes + kBBytes) + lane / 16;
-            i32x8 b[Shape::kFragsN];
-            int b_scale[Shape::kFragsN];
+        Places a_at = of_a_stage.in(0), b_at = of_b_stage.in(0);
+#pragma unroll
+        for (int j = 0; j < Shape::kFragsN; ++j) b[j] = fragment(b_at, j);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) a[i] = fragment(a_at, i);
+        first_rows(a_at);
+        for (int step = 0; step + 1 < total; ++step) {
+            const uint32_t next = here + kStage == kRing ? 0 : here + kStage;
+            arrive(min(total - 2 - step, Shape::kBuffers - 2));
+            if (step + Shape::kBuffers < total) load(here);
+            a_at = of_a_stage.in(next);
+            b_at = of_b_stage.in(next);
+#pragma unroll
+            for (int j = 0; j < Shape::kFragsN; ++j) b_next[j] = fragment(b_at, j);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = kRows - kAhead; i < kRows; ++i) {
+                multiply_row(i);
+                a[i % kAhead] = fragment(a_at, i - (kRows - kAhead));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int j = 0; j < Shape::kFragsN; ++j) b[j] = b_next[j];
+            here = next;
+            first_rows(a_at);
+        }
+#pragma unroll
+        for (int i = kRows - kAhead; i < kRows; ++i) multiply_row(i);
+        // other instructions may read a result 19 cycles after its matrix instruction has begun; the compiler does not see these
+#pragma unroll
+        for (int i = 0; i < Shape::kFragsM; ++i)
 #pragma unroll
             for (int j = 0; j < Shape::kFragsN; ++j) {
-                b[j] = fragment(stage + kABytes + (b_first + 16 * j) * kStageBytes);
-                b_scale[j] = stage_scales[kAScales + (b_first + 16 * j) * 4];
+                if (i == 0 && j == 0) asm volatile("s_nop 15\n\ts_nop 15" : "+v"(acc[0][0]));
+                asm volatile("" : "+v"(acc[j][i]));
             }
-#pragma unroll
-            for (int i = 0; i < Shape::kFragsM; ++i) {
-                const i32x8 a = fragment(stage + (a_first + 16 * i) * kStageBytes);
-                const int a_scale = stage_scales[(a_first + 16 * i) * 4];
-#pragma unroll
-                for (int j = 0; j < Shape::kFragsN; ++j) acc[j][i] = multiply8(b[j], a, acc[j][i], b_scale[j], a_scale);
-            }
-            // all waves have read the stage
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (step + Shape::kBuffers < total) load(here);
-            here = here + kStage == kRing ? 0 : here + kStage;
-        }
     }
 };
 
@@ -136,7 +185,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWavesASimd) void product_8
     const TileIndex tile = tile_of(args);
     Tile8Product<Shape> product;
     product.run(args, scales, tile);
-    store_tile<Shape>(product.acc, args, tile, argument_behind<Out, ProductArgs<Pair8>, Scales8>());
+    argument_behind<Out, ProductArgs<Pair8>, Scales8>().template store<Shape>(product.acc, args, tile);
 #endif
 }
 
