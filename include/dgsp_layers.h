@@ -188,12 +188,13 @@ typedef enum { DGSP_KEEP_NOTHING = 0, DGSP_KEEP_WHOLE = 1, DGSP_KEEP_8BIT = 2 } 
  *   residual    NULL: 0
  *   activation  DGSP_ACT_...
  *   saved       dgsp_linear_saved_bytes(...) bytes, 16-byte aligned, for the backward pass; not looked at if that is 0
+ *   x_values, x_scales   x in DGSP_INT8 for the backward pass, only with DGSP_KEEP_8BIT; NULL: not wanted
  *   workspace   dgsp_linear_workspace_bytes(...) bytes, 16-byte aligned; not looked at if that is 0
  * z, act(z) and the sum with the residual are held in 32 bits.  Float matrices, infinities, NaN and limits: as in dgsp_gated_ff.
  */
 int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int type, int bias_type, int activation, int keep, const void *x,
                 int64_t ldx, const void *weight, int64_t ldw, const void *bias, const void *residual, int64_t ldr, void *y,
-                int64_t ldy, void *saved, void *workspace, int64_t workspace_bytes, void *stream);
+                int64_t ldy, void *saved, void *x_values, int64_t ldv, void *x_scales, void *workspace, int64_t workspace_bytes, void *stream);
 int64_t dgsp_linear_saved_bytes(int64_t rows, int64_t out_width, int type, int activation, int keep);
 int64_t dgsp_linear_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type);
 

@@ -9,25 +9,9 @@
 #pragma once
 
 #include "chunks.hpp"
+#include "lanes.hpp"
 
 namespace dgsp {
-
-// v of the lane that differs by the pattern, for sums over 2, 4, 8, 16 lanes
-template <int kPattern>
-__device__ __forceinline__ float moved(float v) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kPattern, 0xf, 0xf, true));
-}
-
-// over `lanes` (a power of two up to 64) neighbouring lanes; every lane has the sum
-__device__ __forceinline__ float lanes_sum(float v, int lanes) {
-    if (lanes > 1) v += moved<0xb1>(v);          // neighbours of a pair
-    if (lanes > 2) v += moved<0x4e>(v);          // pairs of four
-    if (lanes > 4) v += moved<0x141>(v);         // eight, mirrored
-    if (lanes > 8) v += moved<0x140>(v);         // sixteen, mirrored
-    if (lanes > 16) v += __shfl_xor(v, 16, 64);
-    if (lanes > 32) v += __shfl_xor(v, 32, 64);
-    return v;
-}
 
 constexpr int kMostWaves = 16;
 

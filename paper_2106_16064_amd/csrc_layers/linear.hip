@@ -1,6 +1,7 @@
 // Host side of the matrix product with its epilogue: argument checks, products and launches.  The C-ABI is documented in include/dgsp_layers.h.
 #include "column_sums.hpp"
 #include "linear_host.hpp"
+#include "narrow_linear.hpp"
 #include "rows8_host.hpp"
 
 namespace {
@@ -64,7 +65,7 @@ extern "C" int64_t dgsp_linear_saved_bytes(int64_t rows, int64_t out_width, int 
 }
 
 extern "C" int64_t dgsp_linear_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type) {
-    if (!linear_extents(rows, width, out_width, type)) return 0;
+    if (!linear_extents(rows, width, out_width, type) || narrow_linear_fits(width, out_width, type)) return 0;
     Pieces pieces(nullptr);
     ForwardPieces need(pieces, rows, width, out_width, type);
     return pieces.used();
@@ -72,6 +73,7 @@ extern "C" int64_t dgsp_linear_workspace_bytes(int64_t rows, int64_t width, int6
 
 extern "C" int64_t dgsp_linear_backward_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type, int activation, int keep) {
     if (!linear_extents(rows, width, out_width, type) || !known_epilogue(activation) || !known_keep(keep)) return 0;
+    if (narrow_linear_fits(width, out_width, type)) return narrow_linear_backward_bytes(rows, width, out_width);
     Pieces pieces(nullptr);
     BackwardPieces need(pieces, rows, width, out_width, type, activation, keep);
     return pieces.used();
@@ -79,7 +81,7 @@ extern "C" int64_t dgsp_linear_backward_workspace_bytes(int64_t rows, int64_t wi
 
 extern "C" int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int type, int bias_type, int activation, int keep, const void* x,
                            int64_t ldx, const void* weight, int64_t ldw, const void* bias, const void* residual, int64_t ldr, void* y,
-                           int64_t ldy, void* saved, void* workspace, int64_t workspace_bytes, void* stream) {
+                           int64_t ldy, void* saved, void* x_values, int64_t ldv, void* x_scales, void* workspace, int64_t workspace_bytes, void* stream) {
     if (!linear_extents(rows, width, out_width, type) || !known_epilogue(activation) || !known_keep(keep) ||
         (bias_type != type && bias_type != DGSP_F32))
         return DGSP_ERR_INVALID_ARG;
@@ -87,8 +89,20 @@ extern "C" int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int t
     const Left what = left(activation, keep);
     if (!readable(x, rows, width, ldx) || !readable(weight, out_width, width, ldw) || (residual && !readable(residual, rows, out_width, ldr)) ||
         !writable(y, rows, out_width, ldy) || (what != kNothing && !saved) || !aligned(saved, 16) ||
+        (x_values && (keep != DGSP_KEEP_8BIT || !rows8_lies(x_values, rows, width, ldv, x_scales) || (rows > 1 && ldv < rows8_bytes(width)))) ||
         !enough(workspace, workspace_bytes, dgsp_linear_workspace_bytes(rows, width, out_width, type)))
         return DGSP_ERR_INVALID_ARG;
+    if (narrow_linear_fits(width, out_width, type)) {
+        const auto call = [&](auto element) {
+            using T = decltype(element);
+            return narrow_linear<T>({rows, width, out_width, activation, static_cast<const T*>(x), static_cast<const T*>(weight), ldx, ldw, bias, bias_type != type,
+                                     static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, what == kZ ? static_cast<T*>(saved) : nullptr,
+                                     what == kCodes ? static_cast<uint8_t*>(saved) : nullptr, padded(out_width, 8),
+                                     x_values ? rows8(x_values, rows, width, ldv, x_scales) : Rows8{}, scale_range(DGSP_INT8, type)},
+                                    static_cast<hipStream_t>(stream));
+        };
+        return type == DGSP_BF16 ? call(bf16_t{}) : call(f16_t{});
+    }
     Pieces pieces(workspace);
     const ForwardPieces at(pieces, rows, width, out_width, type);
     if (!launchable(at.up, 1)) return DGSP_ERR_UNSUPPORTED;
@@ -103,6 +117,7 @@ extern "C" int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int t
         const LinearOut<T> out = linear_out<T>(y, ldy, bias, bias_type != type, residual, ldr, activation, what == kZ ? saved : nullptr,
                                                what == kCodes ? saved : nullptr, out_width, at.up.splits > 1 ? at.partial : nullptr);
         launch<T, false, true, true>(at.up, args, out, on);
+        if (x_values) launch_quantise<T>(DGSP_INT8, rows, width, static_cast<const T*>(x), ldx, rows8(x_values, rows, width, ldv, x_scales), on);
         if (out.partial)
             linear_join_kernel<T><<<(unsigned)std::min<int64_t>(ceil_div(rows * ceil_div(out_width, 4), 256), 4096), 256, 0, on>>>(rows, out_width, at.up.splits, out);
         return launched();
@@ -123,6 +138,19 @@ extern "C" int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_wid
                      (dx && !readable(weight, out_width, width, ldw)) ||
                      (dweight && !(in_8bit ? rows8_lies(x, rows, width, ldx, x_scales) : readable(x, rows, width, ldx)))))
         return DGSP_ERR_INVALID_ARG;
+    if (narrow_linear_fits(width, out_width, type)) {
+        if (!dx && !dweight && !dbias) return DGSP_OK;
+        const auto call = [&](auto element) {
+            using T = decltype(element);
+            return narrow_linear_backward<T>({rows, width, out_width, activation, in_8bit ? nullptr : static_cast<const T*>(x), static_cast<const T*>(weight),
+                                              static_cast<const T*>(dy), ldx, ldw, lddy, what == kZ ? static_cast<const T*>(saved) : nullptr,
+                                              what == kCodes ? static_cast<const uint8_t*>(saved) : nullptr, padded(out_width, 8),
+                                              in_8bit && dweight ? rows8(const_cast<void*>(x), rows, width, ldx, const_cast<void*>(x_scales)) : Rows8{},
+                                              static_cast<T*>(dx), nullptr, nullptr},
+                                             dweight, dbias, bias_type != type, workspace, static_cast<hipStream_t>(stream));
+        };
+        return type == DGSP_BF16 ? call(bf16_t{}) : call(f16_t{});
+    }
     Pieces pieces(workspace);
     const BackwardPieces at(pieces, rows, width, out_width, type, activation, keep);
     if (!launchable(at.dx, 1) || !launchable(at.dw, 1)) return DGSP_ERR_UNSUPPORTED;

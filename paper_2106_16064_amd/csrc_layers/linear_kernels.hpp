@@ -26,7 +26,14 @@ __device__ __forceinline__ void activate_only(int kind, const float (&z)[kCount]
     }
 }
 
-__device__ __forceinline__ int slope_code(float slope) { return (int)rintf(slope * kSlopeSteps) & 0xff; }
+// A NaN has a code of its own, below all slopes.
+__device__ __forceinline__ uint32_t slope_code(float slope) { return slope == slope ? (uint32_t)(int)rintf(slope * kSlopeSteps) & 0xffu : 0x80u; }
+
+// of eight codes the j-th
+__device__ __forceinline__ float slope_of(uint2 codes, int j) {
+    const int code = (int8_t)((j < 4 ? codes.x : codes.y) >> (8 * (j % 4)) & 0xffu);
+    return code == -128 ? __builtin_nanf("") : (float)code * (1.0f / kSlopeSteps);
+}
 
 // z as it was kept: an infinity, of z or of its rounding, has the slope of a number far from 0
 template <typename T>
@@ -94,7 +101,7 @@ struct LinearOut {
             for (int j = 0; j < kCount; ++j) {
                 uint32_t word = 0;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) word |= (uint32_t)slope_code(slope[4 * j + r]) << (8 * r);
+                for (int r = 0; r < 4; ++r) word |= slope_code(slope[4 * j + r]) << (8 * r);
                 if (kWhole || left > kStep * j) *reinterpret_cast<uint32_t*>(to + kStep * j) = word;
             }
         } else {
@@ -237,7 +244,7 @@ __global__ __launch_bounds__(256) void linear_slope_kernel(LinearSlopeArgs<T> a)
             if (a.codes) {
                 const uint2 codes = *reinterpret_cast<const uint2*>(a.codes + row * a.kept_ld + col);
 #pragma unroll
-                for (int j = 0; j < kChunk; ++j) slope[j] = (float)(int8_t)((j < 4 ? codes.x : codes.y) >> (8 * (j % 4)) & 0xffu) * (1.0f / kSlopeSteps);
+                for (int j = 0; j < kChunk; ++j) slope[j] = slope_of(codes, j);
             } else if (a.z) {
                 float z[kChunk], value[kChunk];
                 widen(load_chunk(a.z + row * a.kept_ld + col, kChunk), z);

@@ -1,0 +1,389 @@
+// y = act(x w^T + bias) + residual where the weight fits a CU's LDS: the features of many vertices, narrow rows of 16-bit elements.  What bounds it is
+// reading and writing the matrices that are as long as the rows, so each is touched once: the forward pass writes y and what is kept, x in 8 bits
+// among it, and the backward pass makes dz = dy act'(z) in registers and all three gradients of it.
+//
+// A lane has a vertex (l % 16 of 16) and, q = l / 16, columns 32 t + 8 q ... + 7 of every 32: a piece of 16 bytes, which is also what the matrix
+// instructions take of it as an operand, and 16 lanes of a block of 32 columns are 64 bytes of a row.  The weight's rows are put in such an order
+// that a lane's results are neighbours as well: row 4 q + i of a 16 x 16 result is its column 32 t + 8 q + 4 h + i, for two results h.
+#pragma once
+
+#include "chunks.hpp"
+#include "fragments.hpp"
+#include "lanes.hpp"
+#include "linear_kernels.hpp"
+#include "rows8.hpp"
+
+namespace dgsp {
+
+template <typename E>
+struct NarrowLinearArgs {
+    int64_t rows, width, out_width;
+    int activation;
+    const E *x, *weight;
+    int64_t ldx, ldw;
+    const void* bias;
+    bool wide;                  // the bias in float
+    const E* residual;
+    int64_t ldr;
+    E* y;
+    int64_t ldy;
+    E* z;                       // kept: one of these two, or none; ld is `kept_ld`, a multiple of 8
+    uint8_t* codes;
+    int64_t kept_ld;
+    Rows8 x8;                   // x in whole numbers of 8 bits: written by the forward pass, read by the backward pass; or not
+    ScaleRange range;
+};
+
+// Which row of the weight a fragment's row is, among 32.
+__device__ __forceinline__ int place_in_32(int row, int half) { return 8 * (row / 4) + 4 * half + row % 4; }
+
+// eight 16-bit numbers as they are rounded
+template <typename E>
+__device__ __forceinline__ s16x8 pack8(const float (&v)[kChunk]) {
+    return join(pack<E>(f32x4{v[0], v[1], v[2], v[3]}), pack<E>(f32x4{v[4], v[5], v[6], v[7]}));
+}
+
+// the largest of the four lanes that have a vertex's block
+__device__ __forceinline__ uint32_t vertex_max(uint32_t v) {
+    const auto far = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max((uint32_t)far[0], (uint32_t)far[1]);
+    const auto near = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return max((uint32_t)near[0], (uint32_t)near[1]);
+}
+
+// A lane's eight elements of a vertex -> whole numbers of 8 bits, as to_8bit() of a row's four neighbouring lanes.
+template <typename E>
+__device__ __forceinline__ uint2 vertex_bytes(const RawChunk<E>& raw, ScaleRange range, uint32_t& scale) {
+    using Pair = uint16_t __attribute__((ext_vector_type(2)));
+    Pair most = {0, 0};                                        // magnitudes of 16-bit numbers are in the order of their bits
+#pragma unroll
+    for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(Pair, raw.q[0][j] & 0x7fff7fffu));
+    const uint32_t largest = vertex_max(max(most[0], most[1]));
+    const float amax = to_float(__builtin_bit_cast(E, (uint16_t)largest));
+    const bool finite = amax < __builtin_inff();
+    scale = scale_byte<false>(finite ? __builtin_bit_cast(uint32_t, amax) : 0u, range);
+    const float inverse = __builtin_bit_cast(float, (254u - scale) << 23);
+    float v[kChunk];
+    widen(raw, v);
+    uint2 bytes = whole_bytes(v, inverse, __builtin_amdgcn_ballot_w64((int)scale == range.most) != 0);
+    if (!finite) {
+        scale = 255u;
+        bytes = {0u, 0u};
+    }
+    return bytes;
+}
+
+// slope_code() of eight, together where none is NaN
+__device__ __forceinline__ uint2 slope_bytes(const float (&slope)[kChunk]) {
+    uint2 bytes = whole_bytes(slope, kSlopeSteps, false);
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kChunk; ++j) sum += slope[j];
+    if (__builtin_amdgcn_ballot_w64(sum != sum) != 0) {
+        bytes = {0u, 0u};
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) (j < 4 ? bytes.x : bytes.y) |= slope_code(slope[j]) << (8 * (j % 4));
+    }
+    return bytes;
+}
+
+// A lane's eight elements of a row at `col`.  Where rows are whole, rows that are not there are read as the first one, and what comes of them is
+// not written or counts as 0; else what is not there is 0.
+template <bool kWhole, typename E>
+__device__ __forceinline__ RawChunk<E> row_chunk(const E* p, int64_t row, int64_t ld, int col, int columns, bool inside) {
+    if constexpr (kWhole) return load_chunk(p + (inside ? row * ld : 0) + col, kChunk);
+    const bool some = inside && col < columns;
+    return load_chunk(p + (some ? row * ld + col : 0), some ? columns - col : 0);
+}
+
+// kP: width, kO: out_width, each padded to 32, 64 or 128; kX8: x is written in 8 bits; kWhole: nothing is padded
+template <typename E, int kP, int kO, bool kX8, bool kWhole>
+__global__ __launch_bounds__(256, kP * kO > 64 * 64 ? 3 : 4) void narrow_linear_kernel(NarrowLinearArgs<E> a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int kU = kP / 32, kT = kO / 32, kFragments = 2 * kT * kU;
+    __shared__ u32x4 weights[kFragments * 64];
+    __shared__ __attribute__((aligned(16))) float bias[kO];
+    for (int c = threadIdx.x; c < kO; c += 256)
+        bias[c] = !a.bias || c >= a.out_width ? 0.0f : a.wide ? static_cast<const float*>(a.bias)[c] : to_float(static_cast<const E*>(a.bias)[c]);
+    for (int i = threadIdx.x; i < kFragments * 64; i += 256) {
+        const int f = i / 64, l = i % 64, u = f % kU, out = f / kU / 2 * 32 + place_in_32(l % 16, f / kU % 2), k = 32 * u + l / 16 * 8;
+        weights[i] = out < a.out_width && k < a.width ? load_chunk(a.weight + out * a.ldw + k, a.width - k).q[0] : u32x4{0u, 0u, 0u, 0u};
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 63, first = lane / 16 * 8;           // of the lane's columns in every 32
+    const int width = kWhole ? kP : (int)a.width, out_width = kWhole ? kO : (int)a.out_width, blocks = (width + kBlock - 1) / kBlock;
+    const int64_t step = (int64_t)gridDim.x * 64;
+    int64_t row = (int64_t)blockIdx.x * 64 + threadIdx.x / 64 * 16 + lane % 16;
+    RawChunk<E> x[kU];
+    auto ask = [&](int64_t at) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) x[u] = row_chunk<kWhole>(a.x, at, a.ldx, 32 * u + first, width, at < a.rows);
+    };
+    ask(row);
+    for (int64_t base = (int64_t)blockIdx.x * 64; base < a.rows; base += step, row += step) {
+        const bool inside = row < a.rows;
+        RawChunk<E> residual[kT];
+        if (a.residual)
+#pragma unroll
+            for (int t = 0; t < kT; ++t) residual[t] = row_chunk<kWhole>(a.residual, row, a.ldr, 32 * t + first, out_width, inside);
+        s16x8 operand[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) operand[u] = __builtin_bit_cast(s16x8, x[u].q[0]);
+        if constexpr (kX8) {
+            uint32_t word = 0;
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                uint32_t scale;
+                const uint2 bytes = vertex_bytes<E>(x[u], a.range, scale);
+                if (inside && (kWhole || u < blocks)) *reinterpret_cast<uint2*>(a.x8.values + row * a.x8.ldv + 32 * u + first) = bytes;
+                word |= (kWhole || u < blocks ? scale : 127u) << (8 * u);
+            }
+            if (kU < 4) word |= 0x7f7f7f7fu << (8 * kU % 32);
+            if (inside && first == 0) *reinterpret_cast<uint32_t*>(a.x8.scales + row * 4) = word;
+        }
+        ask(row + step);
+        int piece = lane;                                               // of a fragment; read again for every row where all would not fit the registers
+        if constexpr (kP * kO >= 64 * 64) asm volatile("" : "+v"(piece));
+#pragma unroll
+        for (int t = 0; t < kT; ++t) {
+            f32x4 part[2] = {*reinterpret_cast<const f32x4*>(bias + 32 * t + piece / 16 * 8), *reinterpret_cast<const f32x4*>(bias + 32 * t + piece / 16 * 8 + 4)};
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int u = 0; u < kU; ++u)
+                    part[h] = multiply<E>(__builtin_bit_cast(s16x8, weights[((t * 2 + h) * kU + u) * 64 + piece]), operand[u], part[h]);
+            float z[kChunk], value[kChunk];
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j) z[j] = part[j / 4][j % 4];
+            const int col = 32 * t + first, here = kWhole ? kChunk : out_width - col;
+            const bool store = inside && here > 0;
+            if (a.codes) {
+                float slope[kChunk];
+                activate<false>(a.activation, z, value, slope);
+                const uint2 bytes = slope_bytes(slope);
+                if (store) *reinterpret_cast<uint2*>(a.codes + row * a.kept_ld + col) = bytes;
+            } else {
+                activate_only<false>(a.activation, z, value);
+                if (a.z && store) store_chunk(a.z + row * a.kept_ld + col, kChunk, z);
+            }
+            if (a.residual) {
+                float add[kChunk];
+                widen(residual[t], add);
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) value[j] += add[j];
+            }
+            if (store) store_chunk(a.y + row * a.ldy + col, here, value);
+        }
+    }
+#endif
+}
+
+template <typename E>
+struct NarrowLinearBackwardArgs {
+    int64_t rows, width, out_width;
+    int activation;
+    const E *x, *weight, *dy;
+    int64_t ldx, ldw, lddy;
+    const E* z;                 // what was kept: one of these two, or none
+    const uint8_t* codes;
+    int64_t kept_ld;
+    Rows8 x8;                   // in place of x
+    E* dx;                      // packed; null: not wanted
+    float *weight_sums;         // [workgroup and part of the vertices][out_width][width]; null: not wanted
+    float *bias_sums;           // [workgroup][out_width]; null: not wanted
+};
+
+constexpr int kNarrowWaves = 8, kNarrowTile = 16 * kNarrowWaves;       // vertices of a workgroup
+
+// How the waves share the weight's gradient: kDown x kAcross of them have a block each, of kParts parts of the vertices.
+template <int kP, int kO>
+struct NarrowShare {
+    static constexpr int kDown = 2, kAcross = kP / 16 < 4 ? kP / 16 : 4, kParts = kNarrowWaves / (kDown * kAcross);
+    static constexpr int kFragsO = kO / 16 / kDown, kFragsP = kP / 16 / kAcross;
+    static constexpr int kLdO = kO + 8, kLdP = kP + 8;                  // rows of LDS start in different banks
+    static constexpr int kLds = 2 * kO * kP + 2 * kNarrowTile * (kLdO + kLdP);
+};
+
+// dz stays in registers as an operand for dx; for the weight's gradient, a sum over the vertices, dz and x pass through LDS, which hands them out by
+// columns.  Sums over the vertices stay in registers until the end; the workgroups' are added in their order (column_sums.hpp).
+template <typename E, int kP, int kO, bool kX8, bool kWhole>
+__global__ __launch_bounds__(64 * kNarrowWaves, 2) void narrow_linear_backward_kernel(NarrowLinearBackwardArgs<E> a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    using Share = NarrowShare<kP, kO>;
+    constexpr int kU = kP / 32, kT = kO / 32, kFragments = 2 * kT * kU;
+    __shared__ u32x4 weights[kFragments * 64];                          // by columns: 16 of width, 32 of out_width
+    __shared__ uint16_t dz_rows[kNarrowTile * Share::kLdO], x_rows[kNarrowTile * Share::kLdP];
+    if (a.dx)
+        for (int i = threadIdx.x; i < kFragments * 64; i += 64 * kNarrowWaves) {
+            const int f = i / 64, l = i % 64, t = f % kT, k = f / kT / 2 * 32 + place_in_32(l % 16, f / kT % 2), out = 32 * t + l / 16 * 8;
+            u32x4 v = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j)
+                if (k < a.width && out + j < a.out_width)
+                    v[j / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, a.weight[(out + j) * a.ldw + k]) << (j % 2 * 16);
+            weights[i] = v;
+        }
+    __syncthreads();
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = lane / 16 * 8;
+    const int in_tile = wave * 16 + lane % 16;
+    const int width = kWhole ? kP : (int)a.width, out_width = kWhole ? kO : (int)a.out_width, blocks = (width + kBlock - 1) / kBlock;
+    const int down = wave % Share::kDown, across = wave / Share::kDown % Share::kAcross, part = wave / (Share::kDown * Share::kAcross);
+    RawChunk<E> dy[kT], z[kT], x[kU];
+    uint2 codes[kT], x8[kU];
+    uint32_t scales = 0;
+    auto ask = [&](int64_t row) {
+        const bool inside = row < a.rows;
+        const int64_t kept_row = inside ? row * a.kept_ld : 0;
+#pragma unroll
+        for (int t = 0; t < kT; ++t) {
+            const int col = 32 * t + first;
+            const int64_t at = kWhole || col < out_width ? kept_row + col : 0;
+            dy[t] = row_chunk<kWhole>(a.dy, row, a.lddy, col, out_width, inside);
+            if (a.codes) codes[t] = *reinterpret_cast<const uint2*>(a.codes + at);
+            if (a.z) z[t] = load_chunk(a.z + at, kChunk);
+        }
+        if (!a.weight_sums) return;
+        if constexpr (kX8) scales = *reinterpret_cast<const uint32_t*>(a.x8.scales + (inside ? row * 4 : 0));
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const int col = 32 * u + first;
+            if constexpr (kX8)
+                x8[u] = *reinterpret_cast<const uint2*>(a.x8.values + (inside ? row * a.x8.ldv : 0) + (kWhole || u < blocks ? col : 0));
+            else
+                x[u] = row_chunk<kWhole>(a.x, row, a.ldx, col, width, inside);
+        }
+    };
+    f32x4 sums[Share::kFragsO][Share::kFragsP];
+#pragma unroll
+    for (int i = 0; i < Share::kFragsO; ++i)
+#pragma unroll
+        for (int j = 0; j < Share::kFragsP; ++j) sums[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    float db[kT][kChunk];
+#pragma unroll
+    for (int t = 0; t < kT; ++t)
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) db[t][j] = 0.0f;
+
+    const int64_t step = (int64_t)gridDim.x * kNarrowTile;
+    int64_t row = (int64_t)blockIdx.x * kNarrowTile + in_tile;
+    ask(row);
+    for (int64_t base = (int64_t)blockIdx.x * kNarrowTile; base < a.rows; base += step, row += step) {
+        s16x8 dz[kT];
+#pragma unroll
+        for (int t = 0; t < kT; ++t) {
+            float d[kChunk], slope[kChunk];
+            widen(dy[t], d);
+            if (a.codes) {
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) slope[j] = slope_of(codes[t], j);
+            } else if (a.z) {
+                float at[kChunk], value[kChunk];
+                widen(z[t], at);
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) at[j] = inside_range<E>(at[j]);
+                activate<false>(a.activation, at, value, slope);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) slope[j] = 1.0f;
+            }
+            const int here = row < a.rows ? (kWhole ? kChunk : out_width - 32 * t - first) : 0;
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j) {
+                d[j] = (kWhole ? here > 0 : j < here) ? d[j] * slope[j] : 0.0f;
+                db[t][j] += d[j];
+            }
+            dz[t] = pack8<E>(d);
+        }
+        if (a.weight_sums) {
+            s16x8 in[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                if constexpr (kX8) {
+                    float v[kChunk];
+                    from_8bit<false>(x8[u], scales >> (8 * u) & 0xffu, v);
+                    in[u] = pack8<E>(v);
+                } else {
+                    in[u] = __builtin_bit_cast(s16x8, x[u].q[0]);
+                }
+                // 0 times what a row that is not there, or columns behind a block's last, read instead could be NaN
+                if (row >= a.rows || !(kWhole || !kX8 || u < blocks)) in[u] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+            }
+            __syncthreads();                                            // the tile before has been read
+#pragma unroll
+            for (int t = 0; t < kT; ++t) *reinterpret_cast<s16x8*>(dz_rows + in_tile * Share::kLdO + 32 * t + first) = dz[t];
+#pragma unroll
+            for (int u = 0; u < kU; ++u) *reinterpret_cast<s16x8*>(x_rows + in_tile * Share::kLdP + 32 * u + first) = in[u];
+        }
+        ask(row + step);
+        if (a.weight_sums) __syncthreads();
+        if (a.dx) {
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                f32x4 out[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    out[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int t = 0; t < kT; ++t) out[h] = multiply<E>(__builtin_bit_cast(s16x8, weights[((u * 2 + h) * kT + t) * 64 + lane]), dz[t], out[h]);
+                }
+                float v[kChunk];
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) v[j] = out[j / 4][j % 4];
+                const int col = 32 * u + first, here = kWhole ? kChunk : width - col;
+                if (row < a.rows && here > 0) store_chunk(a.dx + row * a.width + col, here, v);
+            }
+        }
+        if (a.weight_sums) {
+            auto columns = [&](const uint16_t* rows, int ld, int vertex, int column) {        // 16 columns of 32 vertices
+                const uint16_t* at = rows + (vertex + first) * ld + column;
+                return join(read_column(at, ld, lane), read_column(at + 4 * ld, ld, lane));
+            };
+#pragma unroll
+            for (int s = 0; s < kNarrowTile / 32 / Share::kParts; ++s) {
+                const int vertex = (part * (kNarrowTile / 32 / Share::kParts) + s) * 32;
+                s16x8 across_x[Share::kFragsP];
+#pragma unroll
+                for (int j = 0; j < Share::kFragsP; ++j) across_x[j] = columns(x_rows, Share::kLdP, vertex, (across * Share::kFragsP + j) * 16);
+#pragma unroll
+                for (int i = 0; i < Share::kFragsO; ++i) {
+                    const s16x8 of_dz = columns(dz_rows, Share::kLdO, vertex, (down * Share::kFragsO + i) * 16);
+#pragma unroll
+                    for (int j = 0; j < Share::kFragsP; ++j) sums[i][j] = multiply<E>(of_dz, across_x[j], sums[i][j]);
+                }
+            }
+        }
+    }
+    if (a.weight_sums) {
+        float* to = a.weight_sums + ((int64_t)blockIdx.x * Share::kParts + part) * a.out_width * a.width;
+#pragma unroll
+        for (int i = 0; i < Share::kFragsO; ++i)
+#pragma unroll
+            for (int j = 0; j < Share::kFragsP; ++j) {
+                const int64_t out = (down * Share::kFragsO + i) * 16 + lane / 16 * 4, k = (across * Share::kFragsP + j) * 16 + lane % 16;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (out + r < a.out_width && k < a.width) to[(out + r) * a.width + k] = sums[i][j][r];
+            }
+    }
+    if (a.bias_sums) {
+        __shared__ float waves_sums[kNarrowWaves][kO];
+#pragma unroll
+        for (int t = 0; t < kT; ++t)
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j) {
+                const float v = lanes_sum(db[t][j], 16);
+                if (lane % 16 == 0) waves_sums[wave][32 * t + first + j] = v;
+            }
+        __syncthreads();
+        for (int c = threadIdx.x; c < kO; c += 64 * kNarrowWaves)
+            if (c < a.out_width) {
+                float v = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kNarrowWaves; ++w) v += waves_sums[w][c];
+                a.bias_sums[(int64_t)blockIdx.x * a.out_width + c] = v;
+            }
+    }
+#endif
+}
+
+}  // namespace dgsp

@@ -12,6 +12,7 @@
 
 #include "../../include/dgsp_layers.h"
 #include "chunks.hpp"
+#include "lanes.hpp"
 
 namespace dgsp {
 
@@ -24,11 +25,6 @@ struct Rows8 {
     int64_t lds;            // rows from a group of four blocks to the next
     int64_t blocks;         // of a row
 };
-
-template <int kPattern>
-__device__ __forceinline__ uint32_t moved_bits(uint32_t v) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kPattern, 0xf, 0xf, true);
-}
 
 // Of the four lanes of a block.
 __device__ __forceinline__ uint32_t block_max(uint32_t v) {
@@ -55,6 +51,26 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax, ScaleRange range) 
     return amax == 0 ? 127u : (uint32_t)min(max(exponent - (kE4m3 ? 8 : 6) + up, range.least), range.most);
 }
 
+// Eight numbers times `inverse` as whole numbers in a byte each, to nearest even.  Adding 1.5 * 2^23 in the same step rounds to whole numbers, which are
+// then the lowest byte.  `cut`: some may lie beyond 127 (a scale at the end of its range).
+__device__ __forceinline__ uint2 whole_bytes(const float (&v)[kChunk], float inverse, bool cut) {
+    uint32_t bits[kChunk];
+    if (cut) {
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) bits[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(rintf(v[j] * inverse), -127.0f, 127.0f) + 12582912.0f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) bits[j] = __builtin_bit_cast(uint32_t, fmaf(v[j], inverse, 12582912.0f));
+    }
+    uint32_t out[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const uint32_t low = __builtin_amdgcn_perm(bits[4 * q + 1], bits[4 * q], 0x0c0c0400u), high = __builtin_amdgcn_perm(bits[4 * q + 3], bits[4 * q + 2], 0x0c0c0400u);
+        out[q] = __builtin_amdgcn_perm(high, low, 0x05040100u);
+    }
+    return {out[0], out[1]};
+}
+
 // Eight elements of a row as a lane holds them -> eight bytes, and the scale's byte.  All four lanes of a block call it; elements beyond
 // the row are 0.  A NaN or an infinity is a NaN in e4m3, which has no infinity; of whole numbers, which have neither, it makes the
 // block's scale 255, a NaN.
@@ -73,30 +89,22 @@ __device__ __forceinline__ uint2 to_8bit(const float (&v)[kChunk], ScaleRange ra
     const bool finite = largest < 0x7f800000u;
     scale = scale_byte<kE4m3>(finite ? largest : 0u, range);
     const float inverse = __builtin_bit_cast(float, (254u - scale) << 23);
+    if constexpr (!kE4m3) {
+        if (finite) return whole_bytes(v, inverse, __builtin_amdgcn_ballot_w64((int)scale == range.most) != 0);
+        scale = 255u;
+        return {0u, 0u};
+    }
     uint32_t out[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        if constexpr (kE4m3) {
-            float s[4];
+        float s[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float scaled = v[4 * q + j] * inverse;
-                s[j] = fabsf(v[4 * q + j]) < __builtin_inff() ? __builtin_amdgcn_fmed3f(scaled, -448.0f, 448.0f) : __builtin_nanf("");
-            }
-            const int low = __builtin_amdgcn_cvt_pk_fp8_f32(s[0], s[1], 0, false);
-            out[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(s[2], s[3], low, true);
-        } else {
-            out[q] = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float scaled = __builtin_amdgcn_fmed3f(rintf(v[4 * q + j] * inverse), -127.0f, 127.0f);
-                out[q] |= ((uint32_t)(int)scaled & 0xffu) << (8 * j);
-            }
+        for (int j = 0; j < 4; ++j) {
+            const float scaled = v[4 * q + j] * inverse;
+            s[j] = fabsf(v[4 * q + j]) < __builtin_inff() ? __builtin_amdgcn_fmed3f(scaled, -448.0f, 448.0f) : __builtin_nanf("");
         }
-    }
-    if (!kE4m3 && !finite) {
-        scale = 255u;
-        out[0] = out[1] = 0u;
+        const int low = __builtin_amdgcn_cvt_pk_fp8_f32(s[0], s[1], 0, false);
+        out[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(s[2], s[3], low, true);
     }
     return {out[0], out[1]};
 }

@@ -45,8 +45,12 @@ LinearCall linear_arguments(const at::Tensor& x, const at::Tensor& weight, const
     return c;
 }
 
-// y and what it leaves of z
-std::pair<at::Tensor, at::Tensor> run_linear(const LinearCall& c, const at::Tensor& x) {
+struct LinearResult {
+    at::Tensor y, saved;        // what is left of z
+    InBits x;                   // x in 8 bits, if it is wanted
+};
+
+LinearResult run_linear(const LinearCall& c, const at::Tensor& x, bool x_in_8bit) {
     const c10::DeviceGuard guard(x.device());
     const int64_t rows = c.rows(), width = c.width(), out_width = c.out_width();
     at::Tensor y = empty_on(with_last(x, out_width), x.scalar_type(), x), saved;
@@ -54,10 +58,12 @@ std::pair<at::Tensor, at::Tensor> run_linear(const LinearCall& c, const at::Tens
     if (c.keep != DGSP_KEEP_NOTHING) saved = empty_bytes(kept, x);
     const int64_t bytes = dgsp_linear_workspace_bytes(rows, width, out_width, c.type);
     const at::Tensor workspace = bytes ? empty_bytes(bytes, x) : at::Tensor();
+    const InBits in_8bit = x_in_8bit ? empty_in_8bit(x.sizes(), rows, DGSP_INT8, x) : InBits{};
     check(dgsp_linear(rows, width, out_width, c.type, c.bias_type, c.activation, c.keep, ptr(c.x.t), c.x.ld, ptr(c.weight.t), c.weight.ld, at_or_null(c.bias),
-                      at_or_null(c.residual.t), c.residual.ld, ptr(y), out_width, at_or_null(saved), at_or_null(workspace), bytes, stream()),
+                      at_or_null(c.residual.t), c.residual.ld, ptr(y), out_width, at_or_null(saved), at_or_null(in_8bit.values), in_8bit.ld,
+                      at_or_null(in_8bit.scales), at_or_null(workspace), bytes, stream()),
           "dgsp_linear");
-    return {y, saved};
+    return {y, saved, in_8bit};
 }
 
 struct LinearGradient {
@@ -144,13 +150,11 @@ PyObject* linear(PyObject* const* a, Py_ssize_t n) {
     const bool in_8bit = as_int(a[5]) != 0, graph = wants_grad({x, weight, bias, residual});
     const bool of_x = graph && asks_gradient(x), of_weight = graph && asks_gradient(weight), of_bias = graph && asks_gradient(bias);
     const int keep = !(of_x || of_weight || of_bias) ? DGSP_KEEP_NOTHING : in_8bit ? DGSP_KEEP_8BIT : DGSP_KEEP_WHOLE;
-    std::pair<at::Tensor, at::Tensor> out;
-    InBits kept;
+    LinearResult out;
     {
         at::NoGradGuard no_grad;
         const Unlocked unlocked;
-        out = run_linear(linear_arguments(x, weight, bias, activation, residual, keep), x);
-        if (of_weight && in_8bit) kept = run_quantise(x, DGSP_INT8);
+        out = run_linear(linear_arguments(x, weight, bias, activation, residual, keep), x, of_weight && in_8bit);
     }
     if (graph) {
         auto node = new_node<LinearBackward>();
@@ -162,19 +166,19 @@ PyObject* linear(PyObject* const* a, Py_ssize_t n) {
         node->bias_type = bias.defined() ? bias.scalar_type() : x.scalar_type();
         node->keeps_x = of_weight;
         node->keeps_weight = of_x;
-        node->keeps_saved = out.second.defined();
+        node->keeps_saved = out.saved.defined();
         if (of_weight && in_8bit) {
-            node->x = SavedVariable(kept.values, false);
-            node->scales = SavedVariable(kept.scales, false);
+            node->x = SavedVariable(out.x.values, false);
+            node->scales = SavedVariable(out.x.scales, false);
         } else if (of_weight) {
             node->x = SavedVariable(x, false);
         }
         if (of_x) node->weight = SavedVariable(weight, false);
-        if (node->keeps_saved) node->saved = SavedVariable(out.second, false);
+        if (node->keeps_saved) node->saved = SavedVariable(out.saved, false);
         node->set_next_edges(torch::autograd::collect_next_edges(x, weight, bias, residual));
-        torch::autograd::set_history(out.first, node);
+        torch::autograd::set_history(out.y, node);
     }
-    return wrap(out.first);
+    return wrap(out.y);
 }
 
 // (x, weight, bias, activation, residual, keep_8bit) -> (y, saved, values and scales of x or None)
@@ -183,10 +187,9 @@ PyObject* linear_forward(PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& x = as_tensor(a[0], "x");
     at::NoGradGuard no_grad;
     const bool in_8bit = as_int(a[5]) != 0;
-    const auto out = run_linear(linear_arguments(x, as_tensor(a[1], "weight"), optional_tensor(a[2], "bias"), (int)as_int(a[3]), optional_tensor(a[4], "residual"),
-                                                 in_8bit ? DGSP_KEEP_8BIT : DGSP_KEEP_WHOLE), x);
-    const InBits kept = in_8bit ? run_quantise(x, DGSP_INT8) : InBits{};
-    return wrap_all({out.first, out.second, kept.values, kept.scales});
+    const LinearResult out = run_linear(linear_arguments(x, as_tensor(a[1], "weight"), optional_tensor(a[2], "bias"), (int)as_int(a[3]), optional_tensor(a[4], "residual"),
+                                                 in_8bit ? DGSP_KEEP_8BIT : DGSP_KEEP_WHOLE), x, in_8bit);
+    return wrap_all({out.y, out.saved, out.x.values, out.x.scales});
 }
 
 // (x or values, scales, weight, bias, saved, dy, activation) -> (dx, dweight, dbias)

@@ -394,14 +394,16 @@ def test_refusals_of_the_c_entry_points():
     space = torch.empty(4096 + need, dtype=torch.uint8, device="cuda")
     S = space.data_ptr()
 
-    def there(rows=6, width=16, out=24, type=0, btype=0, act=0, keep=1, xp=X, ldx=16, ldw=16, r=None, yp=Y, ldy=24, saved=S, ws=S + 4096, size=need):
-        return L.dgsp_linear(rows, width, out, type, btype, act, keep, xp, ldx, W, ldw, None, r, 24, yp, ldy, saved, ws, size, stream)
+    def there(rows=6, width=16, out=24, type=0, btype=0, act=0, keep=1, xp=X, ldx=16, ldw=16, r=None, yp=Y, ldy=24, saved=S, ws=S + 4096, size=need, v=None, ldv=32, s=S + 2048):
+        return L.dgsp_linear(rows, width, out, type, btype, act, keep, xp, ldx, W, ldw, None, r, 24, yp, ldy, saved, v, ldv, s, ws, size, stream)
 
     assert there() == dg.OK and there(rows=0, xp=None, yp=None) == dg.OK and there(act=3, saved=None) == dg.OK and there(keep=0, saved=None) == dg.OK
     assert there(rows=-1) == bad and there(width=0) == bad and there(out=0) == bad and there(type=3) == bad and there(btype=1) == bad
     assert there(act=4) == bad and there(act=-1) == bad and there(keep=3) == bad and there(xp=None) == bad and there(ldx=15) == bad and there(ldw=15) == bad
     assert there(yp=None) == bad and there(ldy=23) == bad and there(ldy=0) == bad and there(saved=None) == bad and there(saved=S + 4) == bad
     assert there(width=1 << 22) == bad and there(rows=1 << 31) == bad
+    assert there(keep=2, v=S + 1024) == dg.OK
+    assert there(v=S + 1024) == bad and there(keep=2, v=S + 1028) == bad and there(keep=2, v=S + 1024, ldv=0) == bad and there(keep=2, v=S + 1024, s=None) == bad
     back_need = L.dgsp_linear_backward_workspace_bytes(6, 16, 24, 0, 0, 1)
     big = torch.empty(back_need + 16, dtype=torch.uint8, device="cuda")
 
@@ -430,7 +432,7 @@ def test_sizes_without_a_gpu():
             assert 0 <= L.dgsp_linear_workspace_bytes(*extents, t) <= L.dgsp_linear_workspace_bytes(1, *extents[1:], t)
             assert 0 <= L.dgsp_linear_backward_workspace_bytes(*extents, t, 0, 2) <= L.dgsp_linear_backward_workspace_bytes(1, *extents[1:], t, 0, 2)
     p = 1 << 20
-    assert L.dgsp_linear(1 << 30, 8, 1 << 12, layers.F32, 0, 3, 0, p, 8, p, 8, None, None, 0, p, 1 << 12, None, p, (1 << 63) - 1, None) == dg.ERR_UNSUPPORTED
+    assert L.dgsp_linear(1 << 30, 8, 1 << 12, layers.F32, 0, 3, 0, p, 8, p, 8, None, None, 0, p, 1 << 12, None, None, 0, None, p, (1 << 63) - 1, None) == dg.ERR_UNSUPPORTED
     x = torch.randn((4, 8))
     with pytest.raises(dg.DgspError, match="GPU"):
         layers.linear(x, x)
