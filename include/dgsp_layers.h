@@ -214,9 +214,10 @@ int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_width, int typ
 int64_t dgsp_linear_backward_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type, int activation, int keep);
 
 /*
- * The same product of operands in DGSP_E4M3, for serving: x is rows x width, weight out_width x width, sums in 32 bits.
+ * The same product of operands in DGSP_E4M3, for serving: x is rows x width, weight out_width x width.  Products of eight neighbouring
+ * columns are added aligned to the largest of them and cut off 2^-13 below its power of two; sums of these are held in 32 bits.
  *   type   of the residual and of y
- *   ldx, ldw   of the values, in bytes
+ *   ldx, ldw   of the values, in bytes, below 2^23
  * Limits as above.
  */
 int dgsp_linear_8bit(int64_t rows, int64_t width, int64_t out_width, int type, int bias_type, int activation, const void *x, int64_t ldx,

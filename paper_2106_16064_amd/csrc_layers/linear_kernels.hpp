@@ -162,6 +162,7 @@ struct LinearOut {
             }
             if (residual && i + 1 < Shape::kFragsM) ask(i + 1);
             if (kWhole || m + 16 * i < args.m) finish<kWhole, kEach, 16>(m + 16 * i, n, columns_left(args.n, n), in, now);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     template <typename Shape, typename E>

@@ -208,7 +208,7 @@ def linear(x, weight, bias=None, activation=None, residual=None, keep_8bit=False
 
 
 def linear_8bit(x, weight, bias=None, activation=None, residual=None, dtype=None):
-    """``linear`` of :class:`Rows8` in e4m3, for serving: products of 8 bits, sums in 32, a result of ``dtype`` (bfloat16 if None, float32
+    """``linear`` of :class:`Rows8` in e4m3, for serving: sums of eight products cut off 2^-13 below the largest, sums of those in 32 bits, a result of ``dtype`` (bfloat16 if None, float32
     or float16).  ``bias``: of that type or float32; ``residual``: of that type.  It has no gradient."""
     act = _epilogue(activation)
     type_number = BF16 if dtype is None else _type_number(dtype)

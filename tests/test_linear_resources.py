@@ -1,0 +1,80 @@
+"""What the compiler made of the kernels of the 8-bit product: distances around matrix instructions that are written in assembly, which it does not
+know about, and registers."""
+import os
+import re
+
+import pytest
+
+from test_layers_resources import objects, registers, tool  # noqa: F401
+
+
+def early_uses(lines, results_after, operands_after):
+    """Instructions of one kernel's listing, other than matrix ones, that touch a matrix instruction's result, matrix instructions that read such a result as an
+    operand, and those that read what another vector instruction wrote, before the wait states are over; counted along the code as it stands."""
+    now, results, written, found = 0, {}, {}, []
+    for line in lines:
+        op, _, rest = line.partition(" ")
+        now += 1
+        if op == "s_nop":
+            now += int(rest, 0)
+        elif op.startswith("v_mfma"):
+            into, a, b, _, *scales = rest.split(" op_sel")[0].split(", ")
+            sources = registers(a) | registers(b) | set().union(*(registers(s) for s in scales))
+            if any(now - written.get(r, -99) <= operands_after for r in sources) or any(now - results.get(r, -99) <= results_after for r in sources):
+                found.append(line)
+            results.update((r, now) for r in registers(into))
+        elif op.startswith(("v_", "ds_", "buffer_", "global_", "scratch_")):
+            if any(now - results.get(r, -99) <= results_after for r in registers(rest)):
+                found.append(line)
+            if op.startswith("v_"):
+                written.update((r, now) for r in registers(rest.split(", ")[0]))
+        elif op in ("s_branch", "s_endpgm"):
+            results, written = {}, {}
+    return found
+
+
+def test_the_scan_finds_what_it_looks_for():
+    product = "v_mfma_scale_f32_16x16x128_f8f6f4 v[0:3], v[4:11], v[12:19], v[0:3], v20, v21 op_sel_hi:[0,0,0]"
+    scan = lambda lines: early_uses(lines, 19, 2)  # noqa: E731
+    assert scan([product, product, "s_nop 15", "s_nop 15", "v_mov_b32_e32 v9, v1"]) == []
+    assert scan([product, "s_nop 9", "v_mov_b32_e32 v9, v1"]) == ["v_mov_b32_e32 v9, v1"]
+    assert scan(["v_mov_b32_e32 v20, v30", product]) == [product]
+    assert scan(["v_mov_b32_e32 v20, v30", "s_nop 1", product]) == []
+
+
+def test_wait_states_and_spills_of_the_8bit_product(objects):  # noqa: F811
+    kernels, spills, name = {}, {}, None
+    for code in objects:
+        lines = []
+        for line in tool("llvm-objdump", "-d", "--no-show-raw-insn", code).splitlines():
+            m = re.match(r"[0-9a-f]+ <(\S+)>:", line)
+            if m:
+                lines = kernels.setdefault(m[1], [])
+            elif line.startswith("\t"):
+                lines.append(re.sub(r"\s+", " ", line.split("//")[0]).strip())
+        for line in tool("llvm-readelf", "--notes", code).splitlines():
+            m = re.match(r"    \.(name|vgpr_spill_count): +(\S+)", line)
+            if m and m[1] == "name":
+                name = m[2]
+            elif m:
+                spills[name] = int(m[2])
+    found = {name: lines for name, lines in kernels.items() if "product_8bit_kernel" in name}
+    assert len(found) == 9                                           # three tiles, three types
+    for name, lines in found.items():
+        assert sum(line.startswith("v_mfma_scale") for line in lines) >= 4 * 3, name
+        assert early_uses(lines, 19, 2) == [], name
+        assert spills[name] == 0, name
+
+
+@pytest.mark.parametrize("kernel", ["narrow_linear_kernel", "narrow_linear_backward_kernel", "rms_norm_kernel", "rms_norm_backward_kernel", "linear_slope_kernel", "quantise_kernel"])
+def test_vector_registers_are_not_spilled(objects, kernel):  # noqa: F811
+    name, count = None, 0
+    for code in objects:
+        for line in tool("llvm-readelf", "--notes", code).splitlines():
+            m = re.match(r"    \.(name|vgpr_spill_count): +(\S+)", line)
+            if m and m[1] == "name":
+                name = m[2]
+            elif m and re.search(rf"\d{kernel}I", name):
+                assert int(m[2]) == 0, name
+                count += 1
+    assert count >= 2, os.listdir(os.path.dirname(objects[0]))
