@@ -1,5 +1,6 @@
 // Host side of the matrix product with its epilogue: argument checks, products and launches.  The C-ABI is documented in include/dgsp_layers.h.
 #include "column_sums.hpp"
+#include "few_rows_kernels.hpp"
 #include "linear_host.hpp"
 #include "narrow_linear.hpp"
 #include "rows8_host.hpp"
@@ -10,6 +11,11 @@ using namespace dgsp;
 
 bool linear_extents(int64_t rows, int64_t width, int64_t out_width, int type) {
     return rows >= 0 && rows <= kMostRows && width >= 1 && width <= kMostWidth && out_width >= 1 && out_width <= kMostWidth && known_type(type);
+}
+
+// Products of few rows take kernels of their own, that need no workspace.
+bool few_rows(int64_t rows, int64_t width, int64_t out_width, int type) {
+    return type != DGSP_F32 && dgsp::few_rows(rows, width, out_width, kFewElements);
 }
 
 bool known_epilogue(int activation) { return known_activation(activation) || activation == DGSP_ACT_NONE; }
@@ -26,7 +32,7 @@ struct ForwardPieces {
     Cut up;
     void *x, *weight, *partial;
     ForwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t out_width, int type)
-        : up(cut(rows, out_width, width, 1, 1, type, false, true)), x(pieces.take(laid_out_bytes(rows, width, type))),
+        : up(cut(rows, out_width, width, 1, 1, type, false, true, rows <= 64 ? 2 * kCus : kCus)), x(pieces.take(laid_out_bytes(rows, width, type))),
           weight(pieces.take(laid_out_bytes(out_width, width, type))), partial(pieces.take(partial_bytes(up, rows, out_width, 1))) {}
 };
 
@@ -65,7 +71,7 @@ extern "C" int64_t dgsp_linear_saved_bytes(int64_t rows, int64_t out_width, int 
 }
 
 extern "C" int64_t dgsp_linear_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type) {
-    if (!linear_extents(rows, width, out_width, type) || narrow_linear_fits(width, out_width, type)) return 0;
+    if (!linear_extents(rows, width, out_width, type) || narrow_linear_fits(width, out_width, type) || few_rows(rows, width, out_width, type)) return 0;
     Pieces pieces(nullptr);
     ForwardPieces need(pieces, rows, width, out_width, type);
     return pieces.used();
@@ -100,6 +106,22 @@ extern "C" int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int t
                                      what == kCodes ? static_cast<uint8_t*>(saved) : nullptr, padded(out_width, 8),
                                      x_values ? rows8(x_values, rows, width, ldv, x_scales) : Rows8{}, scale_range(DGSP_INT8, type)},
                                     static_cast<hipStream_t>(stream));
+        };
+        return type == DGSP_BF16 ? call(bf16_t{}) : call(f16_t{});
+    }
+    if (few_rows(rows, width, out_width, type)) {
+        const auto call = [&](auto element) {
+            using T = decltype(element);
+            const auto on = static_cast<hipStream_t>(stream);
+            const LinearOut<T> out = linear_out<T>(y, ldy, bias, bias_type != type, residual, ldr, activation, what == kZ ? saved : nullptr,
+                                                   what == kCodes ? saved : nullptr, out_width, nullptr);
+            const FewRowsArgs<T> args{rows, width, out_width, static_cast<const T*>(x), static_cast<const T*>(weight), rows == 1 ? 0 : ldx, out_width == 1 ? 0 : ldw};
+            with_few_rows(rows, out_width, false, [&](auto sets, auto outs, auto waves) {
+                constexpr int kSets = decltype(sets)::value, kOuts = decltype(outs)::value, kWaves = decltype(waves)::value;
+                few_rows_kernel<T, kSets, kOuts, kWaves><<<(unsigned)ceil_div(out_width, 16 * kOuts), 64 * kWaves, 0, on>>>(args, out);
+            });
+            if (x_values) launch_quantise<T>(DGSP_INT8, rows, width, static_cast<const T*>(x), ldx, rows8(x_values, rows, width, ldv, x_scales), on);
+            return launched();
         };
         return type == DGSP_BF16 ? call(bf16_t{}) : call(f16_t{});
     }

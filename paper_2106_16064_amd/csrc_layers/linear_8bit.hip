@@ -1,4 +1,5 @@
 // Host side of the matrix product of rows in 8 bits: argument checks and launches.  The C-ABI is documented in include/dgsp_layers.h.
+#include "few_rows_kernels.hpp"
 #include "linear_host.hpp"
 #include "rows8_host.hpp"
 #include "tiles_8bit.hpp"
@@ -35,7 +36,7 @@ void launch8(const Cut& c, const ProductArgs<Pair8>& args, const Scales8& scales
 }  // namespace
 
 extern "C" int64_t dgsp_linear_8bit_workspace_bytes(int64_t rows, int64_t width, int64_t out_width) {
-    if (!extents(rows, width, out_width)) return 0;
+    if (!extents(rows, width, out_width) || few_rows(rows, width, out_width, kFewBytes)) return 0;
     return partial_bytes(cut8(rows, width, out_width), rows, out_width, 1);
 }
 
@@ -50,6 +51,19 @@ extern "C" int dgsp_linear_8bit(int64_t rows, int64_t width, int64_t out_width, 
         (out_width > 1 && ldw > kMostLd) || (residual && !readable(residual, rows, out_width, ldr)) || !writable(y, rows, out_width, ldy) ||
         !enough(workspace, workspace_bytes, dgsp_linear_8bit_workspace_bytes(rows, width, out_width)))
         return DGSP_ERR_INVALID_ARG;
+    const Scales8 scales{static_cast<const uint8_t*>(x_scales), static_cast<const uint8_t*>(weight_scales), rows, out_width, ceil_div(width, 4 * kBlock)};
+    if (few_rows(rows, width, out_width, kFewBytes))
+        return with_type(type, [&](auto element) {
+            using T = decltype(element);
+            const LinearOut<T> out = linear_out<T>(y, ldy, bias, bias_type != type, residual, ldr, activation, nullptr, nullptr, out_width, nullptr);
+            const FewRows8Args args{rows, rows8_bytes(width), out_width, static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(weight), rows == 1 ? 0 : ldx,
+                                    out_width == 1 ? 0 : ldw, scales};
+            with_few_rows(rows, out_width, true, [&](auto sets, auto outs, auto waves) {
+                constexpr int kSets = decltype(sets)::value, kOuts = decltype(outs)::value, kWaves = decltype(waves)::value;
+                few_rows_8bit_kernel<T, kSets, kOuts, kWaves><<<(unsigned)ceil_div(out_width, 16 * kOuts), 64 * kWaves, 0, static_cast<hipStream_t>(stream)>>>(args, out);
+            });
+            return launched();
+        });
     const Cut c = cut8(rows, width, out_width);
     if (!launchable(c, 1)) return DGSP_ERR_UNSUPPORTED;
     return with_type(type, [&](auto element) {
@@ -58,7 +72,6 @@ extern "C" int dgsp_linear_8bit(int64_t rows, int64_t width, int64_t out_width, 
         ProductArgs<Pair8> args = product_args<Pair8>(c, rows, out_width, rows8_bytes(width) / 2, 1);
         args.a[0] = source8(x, rows, width, ldx);
         args.b[0] = source8(weight, out_width, width, ldw);
-        const Scales8 scales{static_cast<const uint8_t*>(x_scales), static_cast<const uint8_t*>(weight_scales), rows, out_width, ceil_div(width, 4 * kBlock)};
         const LinearOut<T> out = linear_out<T>(y, ldy, bias, bias_type != type, residual, ldr, activation, nullptr, nullptr, out_width,
                                                c.splits > 1 ? workspace : nullptr);
         launch8(c, args, scales, out, on);

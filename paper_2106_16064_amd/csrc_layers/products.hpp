@@ -54,8 +54,8 @@ struct Cut {
 // and 256 alone in float, 65536 rows, 128 -> 512 -> 128, made the slopes 284 us where 128 took 231: float has no tiles of 256 (with 64
 // alone it takes 776 us, by this rule 638).  Where tiles are fewer than CUs the depth is split, to as many workgroups as are resident
 // together (two of 128, three of 64 a CU; one token, 4096 -> 16384: 97, 88, 81 and 88 us with one to four a CU), down to 256 each, of
-// float matrices 128.
-inline Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, int type, bool dual, bool may_split) {
+// float matrices 128.  `enough_tiles`: from how many on the depth is not split.
+inline Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, int type, bool dual, bool may_split, int64_t enough_tiles = kCus) {
     auto tiles = [&](int size) { return ceil_div(m, size) * ceil_div(n, dual ? size / 2 : size) * batch; };
     const bool splits = may_split && depth >= (type == DGSP_F32 ? 512 : 1024);
     Cut c{kSmall, 0, 0, 1, padded(std::max<int64_t>(depth, 1), kDepth)};
@@ -66,7 +66,7 @@ inline Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, int ty
     c.tiles_m = ceil_div(m, c.size);
     c.tiles_n = ceil_div(n, dual ? c.size / 2 : c.size);
     const int64_t count = tiles(c.size);
-    if (splits && count > 0 && count < kCus) {               // no tiles: a batch without rows
+    if (splits && count > 0 && count < enough_tiles) {               // no tiles: a batch without rows
         const int64_t most = std::min<int64_t>(ceil_div((c.size == kMiddle ? 2 : 3) * kCus, count), depth / (type == DGSP_F32 ? 128 : 256));
         c.split_depth = padded(ceil_div(depth, most), kDepth);
         c.splits = (int)ceil_div(depth, c.split_depth);

@@ -58,10 +58,13 @@ SIZES = [(1, 1, 1), (1, 4096, 200), (2, 3, 5), (5, 64, 64), (37, 100, 273), (129
          (64, 8, 2048), (2050, 128, 16)]
 
 
+FEW = [(16, 520, 70), (17, 300, 200), (32, 2049, 33), (33, 136, 1000), (64, 1000, 47), (65, 1000, 47)]
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", KINDS, ids=str)
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
-@pytest.mark.parametrize("rows,width,out", SIZES)
+@pytest.mark.parametrize("rows,width,out", SIZES + FEW)
 def test_linear(rows, width, out, dtype, kind):
     print("[case] linear", rows, width, out, dtype, kind, flush=True)
     for params in {dtype, torch.float32}:

@@ -44,7 +44,7 @@ def check(rows, width, out, dtype, kind, seed=0, residual=True, at="cpu"):
 @pytest.mark.parametrize("kind", [None, "silu", "gelu", "relu"], ids=str)
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("rows,width,out", [(1, 1, 1), (1, 4096, 200), (2, 3, 5), (5, 31, 64), (16, 32, 16), (37, 100, 273), (129, 130, 131), (64, 128, 64), (65, 160, 63),
-                                            (257, 33, 300), (70, 1030, 515), (3, 257, 2048)])
+                                            (257, 33, 300), (70, 1030, 515), (3, 257, 2048), (17, 300, 200), (32, 2049, 33), (33, 136, 1000), (64, 1500, 47), (65, 1500, 47)])
 def test_linear_8bit(rows, width, out, dtype, kind):
     print("[case] linear_8bit", rows, width, out, dtype, kind, flush=True)
     check(rows, width, out, dtype, kind)
@@ -200,9 +200,9 @@ def test_refusals_of_the_c_entry_point():
     assert call(x=None) == bad and call(xs=None) == bad and call(w=None) == bad and call(ws=None) == bad and call(yp=None) == bad
     assert call(x=X + 8) == bad and call(xs=XS + 1) == bad and call(ldx=96) == bad and call(ldw=136) == bad and call(ldy=23) == bad and call(ldx=1 << 23) == bad
     assert call(rows=1 << 31) == bad and call(width=1 << 22) == bad
-    need = L.dgsp_linear_8bit_workspace_bytes(1, 8192, 64)
+    need = L.dgsp_linear_8bit_workspace_bytes(65, 8192, 64)
     assert need > 0                                                  # split along the depth
-    assert L.dgsp_linear_8bit(1, 8192, 64, 0, 0, 3, X, 8192, XS, W, 8192, WS, None, None, 0, y.data_ptr(), 64, y.data_ptr(), need - 1, stream) == bad
+    assert L.dgsp_linear_8bit(65, 8192, 64, 0, 0, 3, X, 8192, XS, W, 8192, WS, None, None, 0, y.data_ptr(), 64, y.data_ptr(), need - 1, stream) == bad
     torch.cuda.synchronize()
 
 
@@ -210,4 +210,4 @@ def test_sizes_without_a_gpu():
     L = layers.lib()
     for extents in ((-1, 8, 8), (1 << 31, 8, 8), (8, 0, 8), (8, 8, 0), (8, 1 << 22, 8), (8, 8, 1 << 62)):
         assert L.dgsp_linear_8bit_workspace_bytes(*extents) == 0
-    assert 0 <= L.dgsp_linear_8bit_workspace_bytes(0, 8192, 64) <= L.dgsp_linear_8bit_workspace_bytes(1, 8192, 64)
+    assert 0 <= L.dgsp_linear_8bit_workspace_bytes(0, 8192, 64) <= L.dgsp_linear_8bit_workspace_bytes(100, 8192, 64)
