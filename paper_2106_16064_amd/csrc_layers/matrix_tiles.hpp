@@ -93,10 +93,7 @@ struct Loader {
     static constexpr int kInstructions = kRows * kDepth * 2 / kWaveBytes / kWaves;
     static constexpr int kChunks = kAlongK ? kDepth / 8 : kRows / 8;        // of 16 bytes in a row of LDS
     static constexpr int kRowsEach = 64 / kChunks;                          // rows of LDS per instruction
-    // Which chunk a lane takes depends on the instruction in the first or in the second bit of its number, or not at all.
-    static constexpr int kPatternBit = kAlongK || kRows == 64 ? -1 : kRows == 256 ? 0 : 1;
-    static constexpr int kPatterns = kPatternBit < 0 ? 1 : 2;
-    uint32_t offset[kPatterns];             // of the lane in the rows of an instruction
+    uint32_t offset[kInstructions];         // of the lane from where the wave's rows begin
     int chunk;                              // along k
 
     static __device__ __forceinline__ int exchange(int k) { return ((k & 3) + 4 * ((k >> 3) & 3)) & (kRows / 16 - 1); }
@@ -105,10 +102,10 @@ struct Loader {
     __device__ __forceinline__ void init(int lane, int row0, int64_t ld) {
         const int row = lane / kChunks, c = lane % kChunks;
 #pragma unroll
-        for (int p = 0; p < kPatterns; ++p) {
-            const int k = row0 + (kPatternBit > 0 ? p << kPatternBit : p) * kRowsEach + row;
+        for (int j = 0; j < kInstructions; ++j) {
+            const int here = j * kRowsEach + row, k = row0 + here;
             chunk = kAlongK ? c ^ (k & 7) : (((c >> 1) ^ exchange(k)) << 1) + (c & 1);
-            offset[p] = (uint32_t)(row * ld + chunk * 8) * 2u;
+            offset[j] = (uint32_t)(here * ld + chunk * 8) * 2u;
         }
     }
 
@@ -124,30 +121,31 @@ struct Loader {
         const int64_t origin = kAlongK ? (i0 + row0) * s.ld + k0 : (k0 + row0) * s.ld + i0, end = (s.rows - 1) * s.ld + s.cols;
         return {reinterpret_cast<const char*>(s.p + origin), (end - origin) * 2, (int)(s.cols - k0)};
     }
-    // A stage on its way to byte `lds` of LDS, where the wave's rows begin.  The instruction is written out because the compiler waits for
-    // one of its own before any read of LDS that it cannot tell from where it goes; the waits are arrive()'s.  It has no result in
-    // registers.
-    __device__ __forceinline__ void issue(Cursor& c, int64_t ld, uint32_t lds) const {
-        const bool beyond = kAlongK && chunk * 8 >= c.depth_left;           // the next row lies there
-        const char* at = c.at;
-        int64_t left = c.left;
-#pragma unroll
-        for (int j = 0; j < kInstructions; ++j) {
-            // in halves, as there are no 64-bit comparisons of scalars
-            const int high = (int)(left >> 32);
-            const uint32_t low = (uint32_t)left, some = high > 0 ? 0x7fffffffu : low < 0x7fffffffu ? low : 0x7fffffffu;
-            const uint64_t address = reinterpret_cast<uint64_t>(at);
-            const u32x4 buffer = {(uint32_t)address, (uint32_t)(address >> 32) & 0xffffu, high < 0 ? 0u : some, 0x00020000u};
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + j * kWaveBytes),
-                         "v"(beyond ? kNowhere : offset[kPatternBit < 0 ? 0 : j >> kPatternBit & 1]), "s"(buffer)
-                         : "memory", "m0");
-            at += kRowsEach * 2 * ld;
-            left -= kRowsEach * 2 * ld;
-        }
+    // What the instructions of a stage need, all lanes alike but for the last.  `c` goes on to the next stage.
+    struct Stage {
+        u32x4 buffer;
+        uint32_t away;          // added to an offset: where the row ends in front of the lane's chunk, beyond the buffer
+    };
+    __device__ __forceinline__ Stage stage(Cursor& c, int64_t ld) const {
+        // in halves, as there are no 64-bit comparisons of scalars
+        const int high = (int)(c.left >> 32);
+        const uint32_t low = (uint32_t)c.left, some = high > 0 ? 0x7fffffffu : low < 0x7fffffffu ? low : 0x7fffffffu;
+        const uint64_t address = reinterpret_cast<uint64_t>(c.at);
+        Stage out = {{(uint32_t)address, (uint32_t)(address >> 32) & 0xffffu, high < 0 ? 0u : some, 0x00020000u},
+                     kAlongK && chunk * 8 >= c.depth_left ? kNowhere : 0u};
         const int64_t step = kAlongK ? kDepth * 2 : kDepth * 2 * ld;
         c.at += step;
         c.left -= step;
         c.depth_left -= kDepth;
+        return out;
+    }
+    // One of them, on its way to byte `lds` of LDS, where the wave's rows begin.  The instruction is written out because the compiler waits for
+    // one of its own before any read of LDS that it cannot tell from where it goes; the waits are arrive()'s.  It has no result in
+    // registers.
+    __device__ __forceinline__ void issue(int j, const Stage& stage, uint32_t lds) const {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + j * kWaveBytes), "v"(offset[j] | stage.away),
+                     "s"(stage.buffer)
+                     : "memory", "m0");
     }
 };
 
@@ -256,15 +254,25 @@ struct TileProduct {
             b_at = BLoader::begin(args.b[Shape::kDual ? side : pair], j0, k_first, b_wave * kBRowsEach);
         };
         enter();
-        auto load = [&](uint32_t buffer) {
+        typename ALoader::Stage a_stage;
+        typename BLoader::Stage b_stage;
+        uint32_t into = 0;
+        auto begin_load = [&](uint32_t buffer) {
             if (stages_left == 0) {
                 ++pair;
                 stages_left = steps;
                 enter();
             }
             --stages_left;
-            a_loader.issue(a_at, a_ld, a_lds + buffer);
-            b_loader.issue(b_at, b_ld, b_lds + buffer);
+            a_stage = a_loader.stage(a_at, a_ld);
+            b_stage = b_loader.stage(b_at, b_ld);
+            into = buffer;
+        };
+        auto load_piece = [&](int i) {
+            if (i < ALoader::kInstructions)
+                a_loader.issue(i, a_stage, a_lds + into);
+            else if (i < ALoader::kInstructions + BLoader::kInstructions)
+                b_loader.issue(i - ALoader::kInstructions, b_stage, b_lds + into);
         };
         auto read_a = [&](uint32_t buffer, int s, int i) { return a_reader.read(lds + buffer, s, i); };
         auto read_b = [&](uint32_t buffer, int s, s16x8 (&f)[Shape::kFragsN]) {
@@ -295,7 +303,11 @@ struct TileProduct {
 #pragma unroll
             for (int j = 0; j < Shape::kFragsN; ++j) accumulate<E>(b[j], a[i], acc[j][i]);
         };
-        for (int i = 0; i < min(total, Shape::kBuffers); ++i) load(i * kStage);
+        for (int i = 0; i < min(total, Shape::kBuffers); ++i) {
+            begin_load(i * kStage);
+#pragma unroll
+            for (int piece = 0; piece < kOfAStage; ++piece) load_piece(piece);
+        }
         arrive(min(total, Shape::kBuffers) - 1);
         read_b(0, 0, b_low);
 #pragma unroll
@@ -318,15 +330,22 @@ struct TileProduct {
         for (int step = 0; step + 1 < total; ++step) {          // begins where no read is on its way that has to be waited for
             const uint32_t next = here + kStage == kRing ? 0 : here + kStage;
             arrive(min(total - 2 - step, Shape::kBuffers - 2));
-            if (step + Shape::kBuffers < total) load(here);
+            const bool more = step + Shape::kBuffers < total;
+            if (more) begin_load(here);
             read_b(next, 0, b_low);
 #pragma unroll
             for (int i = 0; i < kEarly; ++i) a[i] = read_a(next, 0, i);
             __builtin_amdgcn_sched_barrier(0);
+            // the loads go between the products, a few a row: all waves are here at once, and asking for everything first would leave the matrix
+            // units without work
+            constexpr int kRowsLeft = Shape::kFragsM - kEarly, kPieces = (kOfAStage + kRowsLeft - 1) / kRowsLeft;
 #pragma unroll
             for (int i = kEarly; i < Shape::kFragsM; ++i) {
                 multiply_row(i, b_high);
                 a[i] = read_a(next, 0, i);
+                if (more)
+#pragma unroll
+                    for (int piece = 0; piece < kPieces; ++piece) load_piece((i - kEarly) * kPieces + piece);
                 __builtin_amdgcn_sched_barrier(0);
             }
             here = next;

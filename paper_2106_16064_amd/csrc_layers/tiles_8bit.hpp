@@ -79,15 +79,27 @@ struct Tile8Product {
         const char* const scales_from = reinterpret_cast<const char*>(of_a ? scales.a : scales.b);
         const uint32_t scales_lds = lds_at + kABytes + kBBytes + (of_a ? 0 : kAScales) + part * 256;
 
-        auto load = [&](uint32_t buffer) {
-            a_loader.issue(a_from, args.a[0].ld, a_lds + buffer);
-            b_loader.issue(b_from, args.b[0].ld, b_lds + buffer);
+        typename ALoader::Stage a_stage;
+        typename BLoader::Stage b_stage;
+        u32x4 scales_stage;
+        uint32_t into = 0;
+        auto begin_load = [&](uint32_t buffer) {
+            a_stage = a_loader.stage(a_from, args.a[0].ld);
+            b_stage = b_loader.stage(b_from, args.b[0].ld);
             const int64_t at = (group * scale_rows + scale_row) * 4, left = scales.groups * scale_rows * 4 - at;
             const uint64_t address = reinterpret_cast<uint64_t>(scales_from + at);
-            const u32x4 resource = {(uint32_t)address, (uint32_t)(address >> 32) & 0xffffu, left > 256 ? 256u : left > 0 ? (uint32_t)left : 0u, 0x00020000u};
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(scales_lds + buffer), "v"(lane * 4), "s"(resource)
-                         : "memory", "m0");
+            scales_stage = {(uint32_t)address, (uint32_t)(address >> 32) & 0xffffu, left > 256 ? 256u : left > 0 ? (uint32_t)left : 0u, 0x00020000u};
             ++group;
+            into = buffer;
+        };
+        auto load_piece = [&](int i) {
+            if (i < ALoader::kInstructions)
+                a_loader.issue(i, a_stage, a_lds + into);
+            else if (i < ALoader::kInstructions + BLoader::kInstructions)
+                b_loader.issue(i - ALoader::kInstructions, b_stage, b_lds + into);
+            else if (i == ALoader::kInstructions + BLoader::kInstructions)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(scales_lds + into), "v"(lane * 4), "s"(scales_stage)
+                             : "memory", "m0");
         };
         constexpr int kOfAStage = ALoader::kInstructions + BLoader::kInstructions + 1;
         auto arrive = [&](int later) {
@@ -129,7 +141,7 @@ struct Tile8Product {
         // instead took a tenth of the time: 8192 x 4096 x 16384 590 us against 495).  Those of A come kAhead rows before they are multiplied; when
         // the last ones of a stage are there all waves meet, and from then on fragments are read of the next stage, which has arrived, while
         // the last rows are multiplied, and the buffer takes the stage after that.
-        constexpr int kAhead = 2, kRows = Shape::kFragsM;
+        constexpr int kAhead = 2, kRows = Shape::kFragsM, kPieces = (kOfAStage + kAhead - 1) / kAhead;
         static_assert(kRows % kAhead == 0);
         using Columns = Fragment[Shape::kFragsN];
         Fragment a[kAhead];
@@ -147,7 +159,11 @@ struct Tile8Product {
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-        for (int i = 0; i < min(total, Shape::kBuffers); ++i) load(i * kStage);
+        for (int i = 0; i < min(total, Shape::kBuffers); ++i) {
+            begin_load(i * kStage);
+#pragma unroll
+            for (int piece = 0; piece < kOfAStage; ++piece) load_piece(piece);
+        }
         arrive(min(total, Shape::kBuffers) - 1);
         uint32_t here = 0;
         int step = 0;
@@ -160,7 +176,8 @@ struct Tile8Product {
         auto advance = [&](const Columns& b, Columns& b_next) {
             const uint32_t next = here + kStage == kRing ? 0 : here + kStage;
             arrive(min(total - 2 - step, Shape::kBuffers - 2));
-            if (step + Shape::kBuffers < total) load(here);
+            const bool more = step + Shape::kBuffers < total;
+            if (more) begin_load(here);
             const Places a_at = of_a_stage.in(next), b_at = of_b_stage.in(next);
 #pragma unroll
             for (int j = 0; j < Shape::kFragsN; ++j) b_next[j] = fragment(b_at, j);
@@ -169,6 +186,9 @@ struct Tile8Product {
             for (int i = kRows - kAhead; i < kRows; ++i) {
                 multiply_row(i, b);
                 a[i % kAhead] = fragment(a_at, i - (kRows - kAhead));
+                if (more)
+#pragma unroll
+                    for (int piece = 0; piece < kPieces; ++piece) load_piece((i - (kRows - kAhead)) * kPieces + piece);
                 __builtin_amdgcn_sched_barrier(0);
             }
             here = next;
