@@ -4,6 +4,9 @@
 // leaves what the activation's derivative is made of: z in the matrix's type (its rounding moves act'(z) by |z act''(z)| half a step, a
 // fifth of what rounding dz itself costs), or act'(z) in steps of 1/112 in 8 bits, which has 0 and 1 exactly: all of relu's, and what gelu
 // (-0.13 ... 1.13) and silu (-0.10 ... 1.10) come to far from 0.
+//
+// What it costs beside the product, bfloat16, 8192 x 4096 -> 16384, gelu, z kept: 1050 to 1090 us against 900 of the product alone, of which
+// 110 is writing y and z; nothing runs beside it, as a tile of 256 takes a CU.  dz, from dy and z: 200 us, 4.0 TB/s.
 #pragma once
 
 #include "product_kernels.hpp"

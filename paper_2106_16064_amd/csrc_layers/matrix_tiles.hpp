@@ -8,7 +8,8 @@
 //   rows of m/n   an operand that is contiguous along m or n (transposed): rows of one k, pairs of chunks (16 elements) exchanged by k.
 //                 Fragments come from the transposing reads: 16 lanes read 4 k's of 16 elements and receive 4 k's of one element each.
 //
-// What bounds it: of a long sum the matrix instructions, at the 2.0 GHz that the card holds under them.  bfloat16, 8192 x 4096 x 16384:
+// What bounds it: of a long sum the loads' way through the CU beside the matrix instructions, which are busy 0.53 to 0.61 of the time at the 1.85 GHz
+// that the card's power leaves them (without loads a stage takes 0.8 of the time, without waiting for them 0.98).  bfloat16, 8192 x 4096 x 16384:
 // both along k 0.90 ms, 1.22 PFLOP/s; one transposed, two pairs 1.69 ms, 1.30; both transposed 0.94 ms, 1.17; with the epilogues of
 // gated_ff_kernels.hpp, 1.6 GB each, that nothing runs beside: both projections 2.06 ms, 1.07, the slopes 1.25 ms, 0.88.  A library's
 // products reach 1.35 to 1.58 and 1.05 to 1.15.  Of a few rows the weights' way from memory: one token, 4096 x 16384, 400 MB in 80 us,
