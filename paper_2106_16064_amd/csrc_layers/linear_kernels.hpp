@@ -15,8 +15,6 @@ namespace dgsp {
 
 constexpr float kSlopeSteps = 112.0f;
 
-enum Epilogue { kPlain, kSilu, kGelu, kRelu };
-
 // act(z) alone (activate() without the derivative, which is then never made)
 template <bool kFloat, int kCount>
 __device__ __forceinline__ void activate_only(int kind, const float (&z)[kCount], float (&value)[kCount]) {
