@@ -176,7 +176,7 @@ int dgsp_rms_norm_8bit(int64_t rows, int64_t width, int type, int param_type, co
 /*
  * What a product keeps for its backward pass.  DGSP_KEEP_WHOLE: x, and of z as much as the activation's derivative needs (z in
  * `type`; of relu the derivative in a byte; without an activation nothing).  DGSP_KEEP_8BIT: x in DGSP_INT8, and act'(z) in steps of
- * 1/112 in a byte, which has 0 and 1 exactly.
+ * 1/112 in a byte, which has 0 and 1 exactly and a code for NaN.
  */
 typedef enum { DGSP_KEEP_NOTHING = 0, DGSP_KEEP_WHOLE = 1, DGSP_KEEP_8BIT = 2 } dgsp_keep_t;
 

@@ -354,11 +354,26 @@ struct SavedDrop {
     at::Tensor unpack_offset() const { return on_gpu ? offset.unpack() : at::Tensor(); }
 };
 
+bool captured() {
+    const hipStream_t on = c10::hip::getCurrentHIPStream().stream();
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    return on != nullptr && hipStreamIsCapturing(on, &status) == hipSuccess && status == hipStreamCaptureStatusActive;
+}
+
 // What the nodes share: they are not differentiable themselves, as their kernels are not, and say so.  All tensors that they keep are
 // SavedVariables: hooks may move them elsewhere, and changes in between are noticed.
 struct LayerNode : public torch::autograd::Node {
+    // Of a leaf that another graph holds, torch adds the gradients on the stream where that graph began.  From a capture it would send them to the default
+    // stream, which can take part in none, and end the process; other streams join the capture.
     void once_only() const {
         TORCH_CHECK(!at::GradMode::is_enabled(), name(), ": gradients of gradients are not supported (create_graph=True)");
+        if (!captured()) return;
+        for (uint32_t i = 0; i < num_outputs(); ++i) {
+            const auto& to = next_edge(i).function;
+            if (!to || !task_should_compute_output(i)) continue;
+            const auto where = to->stream();
+            TORCH_CHECK(!where || where->id() != 0, name(), ": the gradient of a leaf cannot be captured while a graph made on the default stream holds the leaf");
+        }
     }
 };
 

@@ -14,7 +14,8 @@ bits every time.
 
 Tensors may have any number of leading axes; the last one is the width.  Rows that lie at one distance from each other (a
 column slice, a broadcast row) are taken as they are, other orders are copied first.  Work runs on the current stream and can be
-captured into a graph.  Wrong arguments raise ``DgspError``.  Gradients of gradients are refused.
+captured into a graph.  Wrong arguments raise ``DgspError``.  Gradients of gradients are refused, and so is capturing the gradient
+of a leaf while a result made from it on the default stream is still held.
 
 Dropout's random numbers are a function of ``seed``, ``offset`` and the place of the element, and the mask is never stored:
 give every call of a step its own ``offset`` (or its own ``seed``), and every step new ones.  ``offset`` may be an int64 GPU
@@ -208,8 +209,9 @@ def linear(x, weight, bias=None, activation=None, residual=None, keep_8bit=False
 
 
 def linear_8bit(x, weight, bias=None, activation=None, residual=None, dtype=None):
-    """``linear`` of :class:`Rows8` in e4m3, for serving: sums of eight products cut off 2^-13 below the largest, sums of those in 32 bits, a result of ``dtype`` (bfloat16 if None, float32
-    or float16).  ``bias``: of that type or float32; ``residual``: of that type.  It has no gradient."""
+    """``linear`` of :class:`Rows8` in e4m3, for serving: products of eight neighbouring columns are added cut off 2^-13 below the power of two of
+    the largest, and sums of those in 32 bits.  The result is of ``dtype`` (bfloat16 if None, float32 or float16); ``bias``: of that type or
+    float32; ``residual``: of that type.  It has no gradient."""
     act = _epilogue(activation)
     type_number = BF16 if dtype is None else _type_number(dtype)
     return (_native or native()).linear_8bit(*_as_rows8(x, "x"), *_as_rows8(weight, "weight"), bias, act, residual, type_number)
