@@ -32,7 +32,7 @@ struct ForwardPieces {
     Cut up;
     void *x, *weight, *partial;
     ForwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t out_width, int type)
-        : up(cut(rows, out_width, width, 1, 1, type, false, true, rows <= 64 ? 2 * kCus : kCus)), x(pieces.take(laid_out_bytes(rows, width, type))),
+        : up(cut_to_fill(rows, out_width, width, type, rows <= 64 ? 2 * kCus : kCus)), x(pieces.take(laid_out_bytes(rows, width, type))),
           weight(pieces.take(laid_out_bytes(out_width, width, type))), partial(pieces.take(partial_bytes(up, rows, out_width, 1))) {}
 };
 
@@ -54,12 +54,12 @@ struct BackwardPieces {
     Slices slices;
     void *x, *weight, *dz, *partial, *sums;
     BackwardPieces(Pieces& pieces, int64_t rows, int64_t width, int64_t out_width, int type, int activation, int keep)
-        : dx(cut(rows, width, out_width, 1, 1, type, false, true)), dw(cut(out_width, width, rows, 1, 1, type, false, true)), slices(rows, out_width),
-          x(pieces.take(keep == DGSP_KEEP_8BIT ? kept_bytes(rows, width, type) : laid_out_bytes(rows, width, type))),
+        : dx(cut_to_fill(rows, width, out_width, type)), dw(cut_to_fill(out_width, width, rows, type)), slices(rows, out_width),
+          x(pieces.take(keep == DGSP_KEEP_8BIT && type != DGSP_F32 ? kept_bytes(rows, width, type) : laid_out_bytes(rows, width, type))),
           weight(pieces.take(laid_out_bytes(out_width, width, type))),
           dz(pieces.take(activation != DGSP_ACT_NONE ? kept_bytes(rows, out_width, type) : laid_out_bytes(rows, out_width, type))),
           partial(pieces.take(std::max(partial_bytes(dx, rows, width, 1), partial_bytes(dw, out_width, width, 1)))),
-          sums(pieces.take(slices.down * out_width * 4)) {}
+          sums(pieces.take(std::max<int64_t>(slices.down, type == DGSP_F32 ? dw.splits : 0) * out_width * 4)) {}
 };
 
 }  // namespace
@@ -187,25 +187,28 @@ extern "C" int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_wid
             grad = operands.add(dy, rows, out_width, lddy, at.dz);
         else
             grad = {static_cast<const T*>(at.dz), rows, kept_ld, kept_ld};
-        if (dweight && in_8bit) {
+        constexpr bool kFloat = sizeof(T) == 4;
+        Rows8 x8{};
+        if (dweight && in_8bit) x8 = rows8(const_cast<void*>(x), rows, width, ldx, const_cast<void*>(x_scales));
+        if (dweight && in_8bit && !kFloat) {
             const int64_t ld = padded(width, 8);
             if (rows > 0)
-                launch_dequantise<T>(DGSP_INT8, rows, width, rows8(const_cast<void*>(x), rows, width, ldx, const_cast<void*>(x_scales)),
-                                     static_cast<T*>(at.x), ld, on);
+                launch_dequantise<T>(DGSP_INT8, rows, width, x8, static_cast<T*>(at.x), ld, on);
             in = {static_cast<const T*>(at.x), rows, ld, ld};
-        } else if (dweight) {
+        } else if (dweight && !in_8bit) {
             in = operands.add(x, rows, width, ldx, at.x);
         }
         if (dx) w = operands.add(weight, out_width, width, ldw, at.weight);
         operands.launch(on);
-        if (rows > 0 && (activation != DGSP_ACT_NONE ? dx || dweight || dbias : dbias != nullptr)) {
+        // the sums over the rows: with dz, or with the weight's gradient, or on their own
+        const bool sums_beside = kFloat && activation == DGSP_ACT_NONE && dweight && dbias;
+        if (rows > 0 && (activation != DGSP_ACT_NONE ? dx || dweight || dbias : dbias && !sums_beside)) {
             const LinearSlopeArgs<T> args{rows, out_width, slices.lanes, static_cast<const T*>(dy), lddy, what == kZ ? static_cast<const T*>(saved) : nullptr,
                                           what == kCodes ? static_cast<const uint8_t*>(saved) : nullptr, kept_ld, activation,
                                           activation != DGSP_ACT_NONE && (dx || dweight) ? static_cast<T*>(at.dz) : nullptr,
                                           dbias ? static_cast<float*>(at.sums) : nullptr};
             linear_slope_kernel<T><<<dim3((unsigned)slices.across, (unsigned)slices.down), 256, 0, on>>>(args);
         }
-        if (dbias) launch_column_sums<T>(out_width, rows > 0 ? slices.down : 0, static_cast<const float*>(at.sums), dbias, bias_type != type, on);
         if (dx) {
             ProductArgs<T> args = product_args<T>(at.dx, rows, width, out_width, 1);
             args.a[0] = grad;
@@ -216,8 +219,13 @@ extern "C" int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_wid
             ProductArgs<T> args = product_args<T>(at.dw, out_width, width, rows, 1);
             args.a[0] = grad;
             args.b[0] = in;
-            product<T, false, false>(at.dw, args, {{static_cast<T*>(dweight), nullptr}, width, false, nullptr}, at.partial, on);
+            const ProductOut<T> out{{static_cast<T*>(dweight), nullptr}, width, false, nullptr};
+            if constexpr (kFloat)
+                weight_gradient(at.dw, args, in_8bit ? &x8 : nullptr, sums_beside ? static_cast<float*>(at.sums) : nullptr, out, at.partial, on);
+            else
+                product<T, false, false>(at.dw, args, out, at.partial, on);
         }
+        if (dbias) launch_column_sums<T>(out_width, rows == 0 ? 0 : sums_beside ? at.dw.splits : slices.down, static_cast<const float*>(at.sums), dbias, bias_type != type, on);
         return launched();
     });
 }

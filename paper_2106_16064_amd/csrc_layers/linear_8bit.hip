@@ -15,7 +15,7 @@ bool extents(int64_t rows, int64_t width, int64_t out_width) {
 }
 
 // a product of pairs of elements
-Cut cut8(int64_t rows, int64_t width, int64_t out_width) { return cut(rows, out_width, rows8_bytes(width) / 2, 1, 1, DGSP_BF16, false, true); }
+Cut cut8(int64_t rows, int64_t width, int64_t out_width) { return cut_to_fill(rows, out_width, rows8_bytes(width) / 2, DGSP_BF16); }
 
 Source<Pair8> source8(const void* values, int64_t rows, int64_t width, int64_t ld) {
     const int64_t pairs = rows8_bytes(width) / 2;

@@ -74,6 +74,32 @@ inline Cut cut(int64_t m, int64_t n, int64_t depth, int terms, int batch, int ty
     return c;
 }
 
+// As cut(), for products of which some are as deep as there are rows.  Splits make at most as many workgroups as are resident together: a few more
+// than that are a second turn of the whole GPU.  Deep sums are split also where there is a tile for every CU but not two (three) of them,
+// and tiles of 256 take over where cut so they come to 0.8 of the share of the CUs that is busy otherwise: their sums have to stay deep, as
+// a CU has nothing else to do while one begins and ends, and their parts few, as each leaves 256 KB.  By cut() and this, us: the weight's gradient,
+// bfloat16, 16384 rows, 1024 -> 4096 202 and 123 (128 split in two: 146), 65536 rows, 1024 -> 2048 293 and 241, 32768 rows, 1500 -> 2000 363
+// and 237, 50000 rows, 301 -> 777 105 and 79; float, 4096 rows, 2048 -> 2048 244 and 187; the product, 200 rows, 4096 -> 5000 31 and 23.
+inline Cut cut_to_fill(int64_t m, int64_t n, int64_t depth, int type, int64_t enough_tiles = kCus) {
+    Cut c = cut(m, n, depth, 1, 1, type, false, true, enough_tiles);
+    if (c.size == kLarge || m == 0) return c;
+    const int64_t count = c.tiles_m * c.tiles_n, resident = (c.size == kMiddle ? 2 : 3) * kCus;
+    int64_t splits = c.splits;
+    if (count <= resident && (splits > 1 || (2 * count <= resident && depth >= 4096)))
+        splits = std::min<int64_t>(resident / count, depth / (type == DGSP_F32 ? 128 : 256));
+    const int64_t turns = ceil_div(count * splits, resident), large = ceil_div(m, kLarge) * ceil_div(n, kLarge), of_large = std::min<int64_t>(kCus / large, 16);
+    if (type != DGSP_F32 && c.size == kMiddle && of_large > 0 && 4 * large <= count + count / 8 && depth >= 2048 * of_large &&
+        10 * (large * of_large) * (turns * resident) >= 8 * (count * splits) * kCus) {
+        c.size = kLarge;
+        c.tiles_m = ceil_div(m, kLarge);
+        c.tiles_n = ceil_div(n, kLarge);
+        splits = of_large;
+    }
+    c.split_depth = padded(ceil_div(std::max<int64_t>(depth, 1), splits), kDepth);
+    c.splits = (int)ceil_div(std::max<int64_t>(depth, 1), c.split_depth);
+    return c;
+}
+
 inline bool launchable(const Cut& c, int batch) { return c.groups(batch) < (1LL << 32) / 512; }
 
 template <bool kDual>
@@ -107,9 +133,9 @@ void launch(const Cut& c, const ProductArgs<T>& args, const Out& out, hipStream_
     const auto groups = (unsigned)c.groups(args.batch);
     if constexpr (sizeof(T) == 4) {
         if (c.size == kMiddle)
-            float_tile_kernel<Middle<kDual>, kARows, kBRows, Out><<<groups, Middle<kDual>::kThreads, 0, stream>>>(args, out);
+            float_tile_kernel<Middle<kDual>, kARows, kBRows, Out><<<groups, Middle<kDual>::kThreads, 0, stream>>>(args, out, Nothing{});
         else
-            float_tile_kernel<Small<kDual>, kARows, kBRows, Out><<<groups, Small<kDual>::kThreads, 0, stream>>>(args, out);
+            float_tile_kernel<Small<kDual>, kARows, kBRows, Out><<<groups, Small<kDual>::kThreads, 0, stream>>>(args, out, Nothing{});
     } else if (c.size == kLarge) {
         tile_kernel<T, Large<kDual>, kARows, kBRows, Out><<<groups, Large<kDual>::kThreads, 0, stream>>>(args, out);
     } else if (c.size == kMiddle) {
@@ -122,6 +148,10 @@ void launch(const Cut& c, const ProductArgs<T>& args, const Out& out, hipStream_
 // c[0 ... batch - 1] = the product (products.hip)
 template <typename T, bool kARows, bool kBRows>
 void product(const Cut& c, const ProductArgs<T>& args, ProductOut<T> out, void* partial, hipStream_t stream);
+
+// A weight's gradient of float matrices, a[0] rows x m and b[0] rows x n.  `b8`: in place of b[0]; null: b[0].  `sums`: over the rows of a[0], [split][m];
+// null: not wanted.
+void weight_gradient(const Cut& c, const ProductArgs<float>& args, const Rows8* b8, float* sums, ProductOut<float> out, void* partial, hipStream_t stream);
 
 // ---------------------------------------------------------------- operands
 

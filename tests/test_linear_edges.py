@@ -9,6 +9,7 @@ import torch
 import linear_reference as lin
 from layer_reference import UNIT
 from paper_2106_16064_amd import layers
+from test_linear import check, inputs
 
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 
@@ -242,6 +243,20 @@ def test_widest_products(width, out, rows, dtype):
     assert torch.equal(kept, y) and all(torch.equal(p, q) for p, q in zip(torch.autograd.grad(kept, [x, w, b], dy), got))
     with torch.no_grad():
         assert torch.equal(layers.linear_8bit(layers.quantise(x), layers.quantise(w), b, dtype=dtype), y)
+
+
+# ---------------------------------------------------------------- deep sums
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,rows,width,out", [
+    (torch.bfloat16, 12000, 1500, 2000), (torch.float16, 10300, 1040, 1024), (torch.bfloat16, 8200, 1024, 4096), (torch.bfloat16, 50000, 301, 777),
+    (torch.bfloat16, 200, 4096, 5000), (torch.float32, 50000, 64, 64), (torch.float32, 40000, 33, 70), (torch.float32, 20001, 129, 130), (torch.float32, 8200, 128, 512),
+    (torch.float32, 4100, 2048, 2050), (torch.float32, 3000, 31, 33), (torch.float32, 1000, 300, 200)], ids=str)
+def test_deep_sums(dtype, rows, width, out):
+    """Weights' gradients that are split to fill the GPU, with tiles of each size, few and many splits and results; of float their bias's beside them."""
+    show("deep sums", dtype, rows, width, out)
+    for seed, (kind, params, keep) in enumerate([(None, dtype, False), (None, torch.float32, True), ("gelu", dtype, True)]):
+        check(inputs(rows, width, out, dtype, params, 200 + 10 * seed), kind, keep, at="cuda")
 
 
 # ---------------------------------------------------------------- numbers that are none
