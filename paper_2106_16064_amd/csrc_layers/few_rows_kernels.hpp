@@ -1,8 +1,8 @@
-// y = act(x w^T + bias) + residual for up to 64 rows of x: one token, a small batch.  What bounds it is the weight's way from memory, so it passes through
-// no LDS: a fragment of the matrix instructions is 16 rows of the weight and, in each lane, 16 bytes of one of them, which a lane reads itself,
-// wherever they lie.  A workgroup has 16 or 32 columns of y and all of the sum, of which its waves take pieces in turn, so that nothing is
-// left for another launch; their parts are added in order.  One token, 4096 -> 16384: bfloat16 25 us, 5.3 TB/s, in 8 bits 15.4 us, 4.4 TB/s
-// (tiles of 64: 35 and 18.5).
+// y = act(x w^T + bias) + residual for up to 64 rows of x: one token, a small batch, sums that are not too deep.  What bounds it is the weight's
+// way from memory, so it passes through no LDS: a fragment of the matrix instructions is 16 rows of the weight and, in each lane, 16 bytes of
+// one of them, which a lane reads itself, wherever they lie.  A workgroup has 16 or 32 columns of y and all of the sum, of which its waves
+// take pieces in turn, so that nothing is left for another launch; their parts are added in order.  One token, 4096 -> 16384, a new weight a
+// call: bfloat16 25 us, 5.3 TB/s, in 8 bits 15.4 us, 4.4 TB/s (tiles of 64: 35 and 18.5).
 #pragma once
 
 #include "chunks.hpp"
@@ -165,15 +165,25 @@ __global__ __launch_bounds__(64 * kWaves, 4) void few_rows_8bit_kernel(FewRows8A
 #endif
 }
 
-// Up to 16 rows; up to 64 where the weight is small.  Beyond, x takes as much of the way as the weight, and the tiles, which read it once for 64 columns, are
-// faster.  bfloat16, us, this and tiles (of 65 rows): 64 rows 1024 -> 1024 8.2 and 9.6, 4096 -> 4096 32 rows 16.5 and 16.5, 64 rows 24 and 16.5;
-// in 8 bits 32 rows 4096 -> 4096 12 and 15, 64 rows 15.6 and 15.
-inline bool few_rows(int64_t rows, int64_t width, int64_t out_width, int64_t most) { return rows <= 16 || (rows <= kFewRows && width * out_width <= most); }
-constexpr int64_t kFewElements = 1 << 22, kFewBytes = 1 << 23;          // of the weight
+// Where one launch without splits of the sum is faster than tiles, which split it and read a row of the weight once for 64 rows of x.  Against it are
+// deep sums of few columns, which few workgroups add up, the deeper the more rows there are, and, from some rows on, weights that are long in
+// coming.  bfloat16, us, this and tiles:
+//     1 row     4096 -> 16384 22 and 25    4096 -> 1024 7.3 and 7.9     8192 -> 4096 15 and 16       8192 -> 256 11.3 and 7.7     16384 -> 512 21 and 12
+//     16 rows   4096 -> 16384 31 and 26    4096 -> 4096 10.4 and 12.6   8192 -> 2048 17 and 13       2048 -> 256 5.9 and 7.1
+//     32 rows   1024 -> 16384 11 and 14    2048 -> 4096 9.0 and 11.2    2048 -> 512 7.9 and 7.2      4096 -> 512 13 and 8
+//     64 rows   512 -> 16384 9.6 and 8.5   1024 -> 8192 9.3 and 14.0    1024 -> 1024 7.2 and 7.6     2048 -> 512 11.4 and 7.5
+// In 8 bits the same holds of widths twice as large: 1 row 8192 -> 1024 7.6 and 8.1, 16384 -> 512 12 and 9; 64 rows 2048 -> 2048 8.0 and 8.5, 4096 -> 1024 13.5 and 8.6.
+inline bool few_rows(int64_t rows, int64_t width, int64_t out_width, int64_t element_bytes) {
+    const int64_t depth = width * element_bytes, weight = depth * out_width;
+    if (rows <= 16) return (out_width >= 4096 || depth * (rows <= 4 ? 1 : 2) < 16384) && (rows <= 8 || weight < (64 << 20));
+    if (rows <= 32) return depth <= 4096 && weight <= (32 << 20);
+    return rows <= kFewRows && depth <= 2048 && weight <= (16 << 20);
+}
 
 // launch(sets, outs, waves): how the rows and columns are cut.  Columns beyond 8192 fill the GPU by workgroups of 8 waves; fewer take 16 (one token, bfloat16,
 // 16384 -> 4096: 36 and 31 us with 8 and 16; 4096 -> 16384: 25 and 30).  In 8 bits more than 4 rows pay for 32 columns a workgroup, which read x half as
-// often (8 rows 4096 -> 16384: 18.9 and 17.0 us with 16 and 32; bfloat16 30.0 and 33.3).
+// often (8 rows 4096 -> 16384: 18.9 and 17.0 us with 16 and 32; bfloat16 30.0 and 33.3), and so do more than 16 rows of both (40 rows 512 -> 8192 6.8 and
+// 5.9; where they leave CUs without work they do not: 37 rows 1000 -> 2731 float16 6.3 and 7.7).
 template <typename F>
 void with_few_rows(int64_t rows, int64_t out_width, bool in_8bit, F&& launch) {
     std::integral_constant<int, 1> one;
@@ -181,8 +191,12 @@ void with_few_rows(int64_t rows, int64_t out_width, bool in_8bit, F&& launch) {
     std::integral_constant<int, 4> four;
     std::integral_constant<int, 8> eight;
     std::integral_constant<int, 16> sixteen;
-    if (rows > 32)
+    if (rows > 32 && out_width < 8192)
+        launch(four, one, eight);
+    else if (rows > 32)
         launch(four, two, eight);
+    else if (rows > 16 && out_width < 8192)
+        launch(two, one, eight);
     else if (rows > 16)
         launch(two, two, eight);
     else if (in_8bit && rows > 4 && out_width >= 8192)

@@ -15,7 +15,7 @@ bool linear_extents(int64_t rows, int64_t width, int64_t out_width, int type) {
 
 // Products of few rows take kernels of their own, that need no workspace.
 bool few_rows(int64_t rows, int64_t width, int64_t out_width, int type) {
-    return type != DGSP_F32 && dgsp::few_rows(rows, width, out_width, kFewElements);
+    return type != DGSP_F32 && dgsp::few_rows(rows, width, out_width, 2);
 }
 
 bool known_epilogue(int activation) { return known_activation(activation) || activation == DGSP_ACT_NONE; }

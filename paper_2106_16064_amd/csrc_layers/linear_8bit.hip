@@ -36,7 +36,7 @@ void launch8(const Cut& c, const ProductArgs<Pair8>& args, const Scales8& scales
 }  // namespace
 
 extern "C" int64_t dgsp_linear_8bit_workspace_bytes(int64_t rows, int64_t width, int64_t out_width) {
-    if (!extents(rows, width, out_width) || few_rows(rows, width, out_width, kFewBytes)) return 0;
+    if (!extents(rows, width, out_width) || few_rows(rows, width, out_width, 1)) return 0;
     return partial_bytes(cut8(rows, width, out_width), rows, out_width, 1);
 }
 
@@ -52,7 +52,7 @@ extern "C" int dgsp_linear_8bit(int64_t rows, int64_t width, int64_t out_width, 
         !enough(workspace, workspace_bytes, dgsp_linear_8bit_workspace_bytes(rows, width, out_width)))
         return DGSP_ERR_INVALID_ARG;
     const Scales8 scales{static_cast<const uint8_t*>(x_scales), static_cast<const uint8_t*>(weight_scales), rows, out_width, ceil_div(width, 4 * kBlock)};
-    if (few_rows(rows, width, out_width, kFewBytes))
+    if (few_rows(rows, width, out_width, 1))
         return with_type(type, [&](auto element) {
             using T = decltype(element);
             const LinearOut<T> out = linear_out<T>(y, ldy, bias, bias_type != type, residual, ldr, activation, nullptr, nullptr, out_width, nullptr);
