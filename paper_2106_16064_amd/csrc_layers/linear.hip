@@ -79,7 +79,7 @@ extern "C" int64_t dgsp_linear_workspace_bytes(int64_t rows, int64_t width, int6
 
 extern "C" int64_t dgsp_linear_backward_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type, int activation, int keep) {
     if (!linear_extents(rows, width, out_width, type) || !known_epilogue(activation) || !known_keep(keep)) return 0;
-    if (narrow_linear_fits(width, out_width, type)) return narrow_linear_backward_bytes(rows, width, out_width);
+    if (narrow_linear_fits(width, out_width, type)) return narrow_linear_backward_bytes(rows, width, out_width, type);
     Pieces pieces(nullptr);
     BackwardPieces need(pieces, rows, width, out_width, type, activation, keep);
     return pieces.used();
@@ -99,15 +99,14 @@ extern "C" int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int t
         !enough(workspace, workspace_bytes, dgsp_linear_workspace_bytes(rows, width, out_width, type)))
         return DGSP_ERR_INVALID_ARG;
     if (narrow_linear_fits(width, out_width, type)) {
-        const auto call = [&](auto element) {
+        return with_type(type, [&](auto element) {
             using T = decltype(element);
             return narrow_linear<T>({rows, width, out_width, activation, static_cast<const T*>(x), static_cast<const T*>(weight), ldx, ldw, bias, bias_type != type,
                                      static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, what == kZ ? static_cast<T*>(saved) : nullptr,
                                      what == kCodes ? static_cast<uint8_t*>(saved) : nullptr, padded(out_width, 8),
                                      x_values ? rows8(x_values, rows, width, ldv, x_scales) : Rows8{}, scale_range(DGSP_INT8, type)},
                                     static_cast<hipStream_t>(stream));
-        };
-        return type == DGSP_BF16 ? call(bf16_t{}) : call(f16_t{});
+        });
     }
     if (few_rows(rows, width, out_width, type)) {
         const auto call = [&](auto element) {
@@ -162,7 +161,7 @@ extern "C" int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_wid
         return DGSP_ERR_INVALID_ARG;
     if (narrow_linear_fits(width, out_width, type)) {
         if (!dx && !dweight && !dbias) return DGSP_OK;
-        const auto call = [&](auto element) {
+        return with_type(type, [&](auto element) {
             using T = decltype(element);
             return narrow_linear_backward<T>({rows, width, out_width, activation, in_8bit ? nullptr : static_cast<const T*>(x), static_cast<const T*>(weight),
                                               static_cast<const T*>(dy), ldx, ldw, lddy, what == kZ ? static_cast<const T*>(saved) : nullptr,
@@ -170,8 +169,7 @@ extern "C" int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_wid
                                               in_8bit && dweight ? rows8(const_cast<void*>(x), rows, width, ldx, const_cast<void*>(x_scales)) : Rows8{},
                                               static_cast<T*>(dx), nullptr, nullptr},
                                              dweight, dbias, bias_type != type, workspace, static_cast<hipStream_t>(stream));
-        };
-        return type == DGSP_BF16 ? call(bf16_t{}) : call(f16_t{});
+        });
     }
     Pieces pieces(workspace);
     const BackwardPieces at(pieces, rows, width, out_width, type, activation, keep);

@@ -5,13 +5,13 @@
 
 namespace dgsp {
 
-// 16-bit elements, both widths at most 128
+// both widths at most 128, of float 64
 bool narrow_linear_fits(int64_t width, int64_t out_width, int type);
 
 template <typename E>
 int narrow_linear(const NarrowLinearArgs<E>& args, hipStream_t stream);
 
-int64_t narrow_linear_backward_bytes(int64_t rows, int64_t width, int64_t out_width);
+int64_t narrow_linear_backward_bytes(int64_t rows, int64_t width, int64_t out_width, int type);
 // `dweight`, `dbias`: null where they are not wanted; args' sums are set here
 template <typename E>
 int narrow_linear_backward(NarrowLinearBackwardArgs<E> args, void* dweight, void* dbias, bool wide, void* workspace, hipStream_t stream);

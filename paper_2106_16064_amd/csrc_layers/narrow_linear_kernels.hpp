@@ -1,17 +1,20 @@
-// y = act(x w^T + bias) + residual where the weight fits a CU's LDS: the features of many vertices, narrow rows of 16-bit elements.  What bounds it is
+// y = act(x w^T + bias) + residual where the weight fits a CU's LDS: the features of many vertices in narrow rows.  What bounds it is
 // reading and writing the matrices that are as long as the rows, so each is touched once: the forward pass writes y and what is kept, x in 8 bits
 // among it, and the backward pass makes dz = dy act'(z) in registers and all three gradients of it.
 //
 // 2^20 vertices, bfloat16, with residual: 64 -> 64 forward 105 us (537 MB, 5.1 TB/s), gradient 127 us (537 MB, 4.2 TB/s); 128 -> 128 with
 // activations kept in 8 bits 250 us (1.08 GB, 4.3 TB/s; gelu and what becomes 8 bits are 150 us of vector instructions beside that) and
-// 215 to 250 us (0.81 GB).  The products of matrix_tiles.hpp one after the other: 183 and 270 us, 417 and 560 us.
+// 215 to 250 us (0.81 GB).  The products of matrix_tiles.hpp one after the other: 183 and 270 us, 417 and 560 us.  Float, gelu, 32 -> 32 forward 88 us
+// (403 MB, 4.6 TB/s), gradient 125 us (537 MB, 4.3 TB/s), by tiles of 64 167 and 325 us.
 //
 // A lane has a vertex (l % 16 of 16) and, q = l / 16, columns 32 t + 8 q ... + 7 of every 32: a piece of 16 bytes, which is also what the matrix
 // instructions take of it as an operand, and 16 lanes of a block of 32 columns are 64 bytes of a row.  The weight's rows are put in such an order
-// that a lane's results are neighbours as well: row 4 q + i of a 16 x 16 result is its column 32 t + 8 q + 4 h + i, for two results h.
+// that a lane's results are neighbours as well: row 4 q + i of a 16 x 16 result is its column 32 t + 8 q + 4 h + i, for two results h.  Float numbers are
+// three bf16 ones each, and their products six (float_tiles.hpp); weights and, for the weight's gradient, rows lie in LDS as planes of these.
 #pragma once
 
 #include "chunks.hpp"
+#include "float_tiles.hpp"
 #include "fragments.hpp"
 #include "lanes.hpp"
 #include "linear_kernels.hpp"
@@ -47,6 +50,53 @@ __device__ __forceinline__ s16x8 pack8(const float (&v)[kChunk]) {
     return join(pack<E>(f32x4{v[0], v[1], v[2], v[3]}), pack<E>(f32x4{v[4], v[5], v[6], v[7]}));
 }
 
+// Eight neighbours as the matrix instructions take them: 16-bit ones as they are, float ones as three bf16 numbers each (float_tiles.hpp).
+template <typename E>
+constexpr int kPlanes = sizeof(E) == 4 ? 3 : 1;
+
+template <int kCount>
+struct Planes {
+    s16x8 q[kCount];
+};
+
+template <typename E>
+__device__ __forceinline__ Planes<kPlanes<E>> planes_of(const RawChunk<E>& raw) {
+    Planes<kPlanes<E>> out;
+    if constexpr (kPlanes<E> == 3) {
+        u32x4 parts[3];
+        split_chunk(raw, parts);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) out.q[p] = __builtin_bit_cast(s16x8, parts[p]);
+    } else {
+        out.q[0] = __builtin_bit_cast(s16x8, raw.q[0]);
+    }
+    return out;
+}
+
+// of 16-bit types they are rounded
+template <typename E>
+__device__ __forceinline__ Planes<kPlanes<E>> planes_of(const float (&v)[kChunk]) {
+    if constexpr (kPlanes<E> == 3)
+        return planes_of<float>(RawChunk<float>{{__builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}), __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]})}});
+    else
+        return {{pack8<E>(v)}};
+}
+
+// c += a b, of float the six products that are larger than 2^-24 of it, the smallest first, or three where b is exact in bf16
+template <typename E, int kA, int kB>
+__device__ __forceinline__ f32x4 multiply_planes(const Planes<kA>& a, const Planes<kB>& b, f32x4 c) {
+    if constexpr (kA == 3 && kB == 3) {
+        constexpr int kFirst[6] = {1, 0, 2, 0, 1, 0}, kSecond[6] = {1, 2, 0, 1, 0, 0};
+#pragma unroll
+        for (int p = 0; p < 6; ++p) c = multiply<bf16_t>(a.q[kFirst[p]], b.q[kSecond[p]], c);
+        return c;
+    } else if constexpr (kA == 3) {
+        return multiply<bf16_t>(a.q[0], b.q[0], multiply<bf16_t>(a.q[1], b.q[0], multiply<bf16_t>(a.q[2], b.q[0], c)));
+    } else {
+        return multiply<E>(a.q[0], b.q[0], c);
+    }
+}
+
 // the largest of the four lanes that have a vertex's block
 __device__ __forceinline__ uint32_t vertex_max(uint32_t v) {
     const auto far = __builtin_amdgcn_permlane32_swap(v, v, false, false);
@@ -58,12 +108,19 @@ __device__ __forceinline__ uint32_t vertex_max(uint32_t v) {
 // A lane's eight elements of a vertex -> whole numbers of 8 bits, as to_8bit() of a row's four neighbouring lanes.
 template <typename E>
 __device__ __forceinline__ uint2 vertex_bytes(const RawChunk<E>& raw, ScaleRange range, uint32_t& scale) {
-    using Pair = uint16_t __attribute__((ext_vector_type(2)));
-    Pair most = {0, 0};                                        // magnitudes of 16-bit numbers are in the order of their bits
+    float amax;                                                // magnitudes are in the order of their bits
+    if constexpr (sizeof(E) == 4) {
+        uint32_t most = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(Pair, raw.q[0][j] & 0x7fff7fffu));
-    const uint32_t largest = vertex_max(max(most[0], most[1]));
-    const float amax = to_float(__builtin_bit_cast(E, (uint16_t)largest));
+        for (int j = 0; j < kChunk; ++j) most = max(most, raw.q[j / 4][j % 4] & 0x7fffffffu);
+        amax = __builtin_bit_cast(float, vertex_max(most));
+    } else {
+        using Pair = uint16_t __attribute__((ext_vector_type(2)));
+        Pair most = {0, 0};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(Pair, raw.q[0][j] & 0x7fff7fffu));
+        amax = to_float(__builtin_bit_cast(E, (uint16_t)vertex_max(max(most[0], most[1]))));
+    }
     const bool finite = amax < __builtin_inff();
     scale = scale_byte<false>(finite ? __builtin_bit_cast(uint32_t, amax) : 0u, range);
     const float inverse = __builtin_bit_cast(float, (254u - scale) << 23);
@@ -102,16 +159,20 @@ __device__ __forceinline__ RawChunk<E> row_chunk(const E* p, int64_t row, int64_
 
 // kP: width, kO: out_width, each padded to 32, 64 or 128; kX8: x is written in 8 bits; kWhole: nothing is padded
 template <typename E, int kP, int kO, bool kX8, bool kWhole>
-__global__ __launch_bounds__(256, kP * kO > 64 * 64 ? 3 : 4) void narrow_linear_kernel(NarrowLinearArgs<E> a) {
+__global__ __launch_bounds__(256, (kP * kO * kPlanes<E> > 64 * 64 ? 3 : 4)) void narrow_linear_kernel(NarrowLinearArgs<E> a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int kU = kP / 32, kT = kO / 32, kFragments = 2 * kT * kU;
-    __shared__ u32x4 weights[kFragments * 64];
+    constexpr int kU = kP / 32, kT = kO / 32, kFragments = 2 * kT * kU, kParts = kPlanes<E>;
+    constexpr bool kFloat = sizeof(E) == 4;
+    __shared__ u32x4 weights[kParts][kFragments * 64];
     __shared__ __attribute__((aligned(16))) float bias[kO];
     for (int c = threadIdx.x; c < kO; c += 256)
         bias[c] = !a.bias || c >= a.out_width ? 0.0f : a.wide ? static_cast<const float*>(a.bias)[c] : to_float(static_cast<const E*>(a.bias)[c]);
     for (int i = threadIdx.x; i < kFragments * 64; i += 256) {
         const int f = i / 64, l = i % 64, u = f % kU, out = f / kU / 2 * 32 + place_in_32(l % 16, f / kU % 2), k = 32 * u + l / 16 * 8;
-        weights[i] = out < a.out_width && k < a.width ? load_chunk(a.weight + out * a.ldw + k, a.width - k).q[0] : u32x4{0u, 0u, 0u, 0u};
+        const bool there = out < a.out_width && k < a.width;
+        const auto planes = planes_of<E>(load_chunk(a.weight + (there ? out * a.ldw + k : 0), there ? a.width - k : 0));
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) weights[p][i] = __builtin_bit_cast(u32x4, planes.q[p]);
     }
     __syncthreads();
     const int lane = threadIdx.x & 63, first = lane / 16 * 8;           // of the lane's columns in every 32
@@ -130,9 +191,9 @@ __global__ __launch_bounds__(256, kP * kO > 64 * 64 ? 3 : 4) void narrow_linear_
         if (a.residual)
 #pragma unroll
             for (int t = 0; t < kT; ++t) residual[t] = row_chunk<kWhole>(a.residual, row, a.ldr, 32 * t + first, out_width, inside);
-        s16x8 operand[kU];
+        Planes<kParts> operand[kU];
 #pragma unroll
-        for (int u = 0; u < kU; ++u) operand[u] = __builtin_bit_cast(s16x8, x[u].q[0]);
+        for (int u = 0; u < kU; ++u) operand[u] = planes_of<E>(x[u]);
         if constexpr (kX8) {
             uint32_t word = 0;
 #pragma unroll
@@ -147,15 +208,19 @@ __global__ __launch_bounds__(256, kP * kO > 64 * 64 ? 3 : 4) void narrow_linear_
         }
         ask(row + step);
         int piece = lane;                                               // of a fragment; read again for every row where all would not fit the registers
-        if constexpr (kP * kO >= 64 * 64) asm volatile("" : "+v"(piece));
+        if constexpr (kP * kO * kParts >= 64 * 64) asm volatile("" : "+v"(piece));
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
             f32x4 part[2] = {*reinterpret_cast<const f32x4*>(bias + 32 * t + piece / 16 * 8), *reinterpret_cast<const f32x4*>(bias + 32 * t + piece / 16 * 8 + 4)};
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int u = 0; u < kU; ++u)
-                    part[h] = multiply<E>(__builtin_bit_cast(s16x8, weights[((t * 2 + h) * kU + u) * 64 + piece]), operand[u], part[h]);
+                for (int u = 0; u < kU; ++u) {
+                    Planes<kParts> w;
+#pragma unroll
+                    for (int p = 0; p < kParts; ++p) w.q[p] = __builtin_bit_cast(s16x8, weights[p][((t * 2 + h) * kU + u) * 64 + piece]);
+                    part[h] = multiply_planes<E>(w, operand[u], part[h]);
+                }
             float z[kChunk], value[kChunk];
 #pragma unroll
             for (int j = 0; j < kChunk; ++j) z[j] = part[j / 4][j % 4];
@@ -163,11 +228,11 @@ __global__ __launch_bounds__(256, kP * kO > 64 * 64 ? 3 : 4) void narrow_linear_
             const bool store = inside && here > 0;
             if (a.codes) {
                 float slope[kChunk];
-                activate<false>(a.activation, z, value, slope);
+                activate<kFloat>(a.activation, z, value, slope);
                 const uint2 bytes = slope_bytes(slope);
                 if (store) *reinterpret_cast<uint2*>(a.codes + row * a.kept_ld + col) = bytes;
             } else {
-                activate_only<false>(a.activation, z, value);
+                activate_only<kFloat>(a.activation, z, value);
                 if (a.z && store) store_chunk(a.z + row * a.kept_ld + col, kChunk, z);
             }
             if (a.residual) {
@@ -197,35 +262,45 @@ struct NarrowLinearBackwardArgs {
     float *bias_sums;           // [workgroup][out_width]; null: not wanted
 };
 
-constexpr int kNarrowWaves = 8, kNarrowTile = 16 * kNarrowWaves;       // vertices of a workgroup
-
-// How the waves share the weight's gradient: kDown x kAcross of them have a block each, of kParts parts of the vertices.
-template <int kP, int kO>
+// How the waves share the weight's gradient: kDown x kAcross of them have a block each, of kParts parts of the vertices.  Of float rows
+// wider than 32 a workgroup has half as many vertices, so that two find room in LDS.
+template <typename E, int kP, int kO>
 struct NarrowShare {
-    static constexpr int kDown = 2, kAcross = kP / 16 < 4 ? kP / 16 : 4, kParts = kNarrowWaves / (kDown * kAcross);
+    static constexpr int kWaves = sizeof(E) == 4 && kP * kO > 32 * 32 ? 4 : 8, kTile = 16 * kWaves;          // kTile vertices of a workgroup
+    static constexpr int kDown = 2, kAcross = kP / 16 < kWaves / 2 ? kP / 16 : kWaves / 2, kParts = kWaves / (kDown * kAcross);
     static constexpr int kFragsO = kO / 16 / kDown, kFragsP = kP / 16 / kAcross;
     static constexpr int kLdO = kO + 8, kLdP = kP + 8;                  // rows of LDS start in different banks
-    static constexpr int kLds = 2 * kO * kP + 2 * kNarrowTile * (kLdO + kLdP);
+    static constexpr int kLds = kPlanes<E> * (2 * kO * kP + 2 * kTile * (kLdO + kLdP));
 };
 
 // dz stays in registers as an operand for dx; for the weight's gradient, a sum over the vertices, dz and x pass through LDS, which hands them out by
 // columns.  Sums over the vertices stay in registers until the end; the workgroups' are added in their order (column_sums.hpp).
 template <typename E, int kP, int kO, bool kX8, bool kWhole>
-__global__ __launch_bounds__(64 * kNarrowWaves, 2) void narrow_linear_backward_kernel(NarrowLinearBackwardArgs<E> a) {
+__global__ __launch_bounds__((64 * NarrowShare<E, kP, kO>::kWaves), 2) void narrow_linear_backward_kernel(NarrowLinearBackwardArgs<E> a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    using Share = NarrowShare<kP, kO>;
-    constexpr int kU = kP / 32, kT = kO / 32, kFragments = 2 * kT * kU;
-    __shared__ u32x4 weights[kFragments * 64];                          // by columns: 16 of width, 32 of out_width
-    __shared__ uint16_t dz_rows[kNarrowTile * Share::kLdO], x_rows[kNarrowTile * Share::kLdP];
+    using Share = NarrowShare<E, kP, kO>;
+    constexpr int kNarrowWaves = Share::kWaves, kNarrowTile = Share::kTile;
+    constexpr int kU = kP / 32, kT = kO / 32, kFragments = 2 * kT * kU, kParts = kPlanes<E>, kXParts = kX8 ? 1 : kParts;    // whole numbers are exact in bf16
+    constexpr bool kFloat = sizeof(E) == 4;
+    __shared__ u32x4 weights[kParts][kFragments * 64];                  // by columns: 16 of width, 32 of out_width
+    __shared__ uint16_t dz_rows[kParts][kNarrowTile * Share::kLdO], x_rows[kXParts][kNarrowTile * Share::kLdP];
     if (a.dx)
         for (int i = threadIdx.x; i < kFragments * 64; i += 64 * kNarrowWaves) {
             const int f = i / 64, l = i % 64, t = f % kT, k = f / kT / 2 * 32 + place_in_32(l % 16, f / kT % 2), out = 32 * t + l / 16 * 8;
-            u32x4 v = {0u, 0u, 0u, 0u};
+            RawChunk<E> v;
+#pragma unroll
+            for (int j = 0; j < RawChunk<E>::kQuads; ++j) v.q[j] = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
             for (int j = 0; j < kChunk; ++j)
-                if (k < a.width && out + j < a.out_width)
-                    v[j / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, a.weight[(out + j) * a.ldw + k]) << (j % 2 * 16);
-            weights[i] = v;
+                if (k < a.width && out + j < a.out_width) {
+                    if constexpr (kFloat)
+                        v.q[j / 4][j % 4] = __builtin_bit_cast(uint32_t, a.weight[(out + j) * a.ldw + k]);
+                    else
+                        v.q[0][j / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, a.weight[(out + j) * a.ldw + k]) << (j % 2 * 16);
+                }
+            const auto planes = planes_of<E>(v);
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) weights[p][i] = __builtin_bit_cast(u32x4, planes.q[p]);
         }
     __syncthreads();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = lane / 16 * 8;
@@ -272,7 +347,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves, 2) void narrow_linear_backward_k
     int64_t row = (int64_t)blockIdx.x * kNarrowTile + in_tile;
     ask(row);
     for (int64_t base = (int64_t)blockIdx.x * kNarrowTile; base < a.rows; base += step, row += step) {
-        s16x8 dz[kT];
+        Planes<kParts> dz[kT];
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
             float d[kChunk], slope[kChunk];
@@ -285,7 +360,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves, 2) void narrow_linear_backward_k
                 widen(z[t], at);
 #pragma unroll
                 for (int j = 0; j < kChunk; ++j) at[j] = inside_range<E>(at[j]);
-                activate<false>(a.activation, at, value, slope);
+                activate<kFloat>(a.activation, at, value, slope);
             } else {
 #pragma unroll
                 for (int j = 0; j < kChunk; ++j) slope[j] = 1.0f;
@@ -296,27 +371,31 @@ __global__ __launch_bounds__(64 * kNarrowWaves, 2) void narrow_linear_backward_k
                 d[j] = (kWhole ? here > 0 : j < here) ? d[j] * slope[j] : 0.0f;
                 db[t][j] += d[j];
             }
-            dz[t] = pack8<E>(d);
+            dz[t] = planes_of<E>(d);
         }
         if (a.weight_sums) {
-            s16x8 in[kU];
+            Planes<kXParts> in[kU];
 #pragma unroll
             for (int u = 0; u < kU; ++u) {
                 if constexpr (kX8) {
                     float v[kChunk];
                     from_8bit<false>(x8[u], scales >> (8 * u) & 0xffu, v);
-                    in[u] = pack8<E>(v);
+                    in[u] = {{pack8<std::conditional_t<kFloat, bf16_t, E>>(v)}};
                 } else {
-                    in[u] = __builtin_bit_cast(s16x8, x[u].q[0]);
+                    in[u] = planes_of<E>(x[u]);
                 }
                 // 0 times what a row that is not there, or columns behind a block's last, read instead could be NaN
-                if (row >= a.rows || !(kWhole || !kX8 || u < blocks)) in[u] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                if (row >= a.rows || !(kWhole || !kX8 || u < blocks)) in[u] = {};
             }
             __syncthreads();                                            // the tile before has been read
 #pragma unroll
-            for (int t = 0; t < kT; ++t) *reinterpret_cast<s16x8*>(dz_rows + in_tile * Share::kLdO + 32 * t + first) = dz[t];
+            for (int t = 0; t < kT; ++t)
 #pragma unroll
-            for (int u = 0; u < kU; ++u) *reinterpret_cast<s16x8*>(x_rows + in_tile * Share::kLdP + 32 * u + first) = in[u];
+                for (int p = 0; p < kParts; ++p) *reinterpret_cast<s16x8*>(dz_rows[p] + in_tile * Share::kLdO + 32 * t + first) = dz[t].q[p];
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+#pragma unroll
+                for (int p = 0; p < kXParts; ++p) *reinterpret_cast<s16x8*>(x_rows[p] + in_tile * Share::kLdP + 32 * u + first) = in[u].q[p];
         }
         ask(row + step);
         if (a.weight_sums) __syncthreads();
@@ -328,7 +407,12 @@ __global__ __launch_bounds__(64 * kNarrowWaves, 2) void narrow_linear_backward_k
                 for (int h = 0; h < 2; ++h) {
                     out[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int t = 0; t < kT; ++t) out[h] = multiply<E>(__builtin_bit_cast(s16x8, weights[((u * 2 + h) * kT + t) * 64 + lane]), dz[t], out[h]);
+                    for (int t = 0; t < kT; ++t) {
+                        Planes<kParts> w;
+#pragma unroll
+                        for (int p = 0; p < kParts; ++p) w.q[p] = __builtin_bit_cast(s16x8, weights[p][((u * 2 + h) * kT + t) * 64 + lane]);
+                        out[h] = multiply_planes<E>(w, dz[t], out[h]);
+                    }
                 }
                 float v[kChunk];
 #pragma unroll
@@ -338,21 +422,27 @@ __global__ __launch_bounds__(64 * kNarrowWaves, 2) void narrow_linear_backward_k
             }
         }
         if (a.weight_sums) {
-            auto columns = [&](const uint16_t* rows, int ld, int vertex, int column) {        // 16 columns of 32 vertices
-                const uint16_t* at = rows + (vertex + first) * ld + column;
-                return join(read_column(at, ld, lane), read_column(at + 4 * ld, ld, lane));
+            // 16 columns of 32 vertices, of each plane
+            auto columns = [&](const auto& rows, int ld, int vertex, int column) {
+                Planes<(int)std::extent_v<std::remove_reference_t<decltype(rows)>>> out;
+#pragma unroll
+                for (int p = 0; p < (int)std::extent_v<std::remove_reference_t<decltype(rows)>>; ++p) {
+                    const uint16_t* at = rows[p] + (vertex + first) * ld + column;
+                    out.q[p] = join(read_column(at, ld, lane), read_column(at + 4 * ld, ld, lane));
+                }
+                return out;
             };
 #pragma unroll
             for (int s = 0; s < kNarrowTile / 32 / Share::kParts; ++s) {
                 const int vertex = (part * (kNarrowTile / 32 / Share::kParts) + s) * 32;
-                s16x8 across_x[Share::kFragsP];
+                Planes<kXParts> across_x[Share::kFragsP];
 #pragma unroll
                 for (int j = 0; j < Share::kFragsP; ++j) across_x[j] = columns(x_rows, Share::kLdP, vertex, (across * Share::kFragsP + j) * 16);
 #pragma unroll
                 for (int i = 0; i < Share::kFragsO; ++i) {
-                    const s16x8 of_dz = columns(dz_rows, Share::kLdO, vertex, (down * Share::kFragsO + i) * 16);
+                    const auto of_dz = columns(dz_rows, Share::kLdO, vertex, (down * Share::kFragsO + i) * 16);
 #pragma unroll
-                    for (int j = 0; j < Share::kFragsP; ++j) sums[i][j] = multiply<E>(of_dz, across_x[j], sums[i][j]);
+                    for (int j = 0; j < Share::kFragsP; ++j) sums[i][j] = multiply_planes<E>(of_dz, across_x[j], sums[i][j]);
                 }
             }
         }

@@ -154,10 +154,10 @@ def test_products_of_more_than_2_to_the_31_elements(width, out, dtype, keep):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("keep", [False, True])
-def test_narrow_products_of_more_than_2_to_the_31_elements(keep):
-    show("narrow products of many elements", keep)
-    rows, width, out = (1 << 25) + 77, 64, 72
-    dtype = torch.bfloat16
+@pytest.mark.parametrize("dtype,out", [(torch.bfloat16, 72), (torch.float32, 64)], ids=str)
+def test_narrow_products_of_more_than_2_to_the_31_elements(dtype, out, keep):
+    show("narrow products of many elements", dtype, keep)
+    rows, width = (1 << 25) + 77, 64
     x, w, dy, r = normal((rows, width), dtype, 0), normal((out, width), dtype, 1, 0.125), normal((rows, out), dtype, 2), normal((rows, out), dtype, 3)
     leaves = [x.requires_grad_(True), w.requires_grad_(True)]
     y = layers.linear(*leaves, None, "silu", r, keep)
