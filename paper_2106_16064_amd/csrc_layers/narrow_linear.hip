@@ -27,12 +27,14 @@ void with_flags(bool first, bool second, F&& f) {
         second ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
 }
 
-// f(padded width, padded out_width); float has no kernels of 128
+constexpr int kMostFloat = 64 * 128;            // of float weights, padded: three planes of it, and of rows, fill LDS
+
+// f(padded width, padded out_width)
 template <typename E, typename F>
 void with_widths(int64_t width, int64_t out_width, F&& f) {
     with_width(width, [&](auto p) {
         with_width(out_width, [&](auto o) {
-            if constexpr (sizeof(E) == 2 || (decltype(p)::value <= 64 && decltype(o)::value <= 64)) f(p, o);
+            if constexpr (sizeof(E) == 2 || decltype(p)::value * decltype(o)::value <= kMostFloat) f(p, o);
         });
     });
 }
@@ -55,7 +57,7 @@ struct Backward {
 
 }  // namespace
 
-bool narrow_linear_fits(int64_t width, int64_t out_width, int type) { return std::max(width, out_width) <= (type == DGSP_F32 ? 64 : 128); }
+bool narrow_linear_fits(int64_t width, int64_t out_width, int type) { return width <= 128 && out_width <= 128 && (type != DGSP_F32 || padded_width(width) * padded_width(out_width) <= kMostFloat); }
 
 template <typename E>
 int narrow_linear(const NarrowLinearArgs<E>& args, hipStream_t stream) {

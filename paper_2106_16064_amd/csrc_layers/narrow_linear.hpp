@@ -5,7 +5,7 @@
 
 namespace dgsp {
 
-// both widths at most 128, of float 64
+// both widths at most 128, of float not both above 64
 bool narrow_linear_fits(int64_t width, int64_t out_width, int type);
 
 template <typename E>

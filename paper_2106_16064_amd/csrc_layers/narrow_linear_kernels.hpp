@@ -5,7 +5,7 @@
 // 2^20 vertices, bfloat16, with residual: 64 -> 64 forward 105 us (537 MB, 5.1 TB/s), gradient 127 us (537 MB, 4.2 TB/s); 128 -> 128 with
 // activations kept in 8 bits 250 us (1.08 GB, 4.3 TB/s; gelu and what becomes 8 bits are 150 us of vector instructions beside that) and
 // 215 to 250 us (0.81 GB).  The products of matrix_tiles.hpp one after the other: 183 and 270 us, 417 and 560 us.  Float, gelu, 32 -> 32 forward 88 us
-// (403 MB, 4.6 TB/s), gradient 125 us (537 MB, 4.3 TB/s), by tiles of 64 167 and 325 us.
+// (403 MB, 4.6 TB/s), gradient 125 us (537 MB, 4.3 TB/s), by tiles of 64 167 and 325 us; 64 -> 128 with residual 400 and 547 us, by tiles 428 and 762.
 //
 // A lane has a vertex (l % 16 of 16) and, q = l / 16, columns 32 t + 8 q ... + 7 of every 32: a piece of 16 bytes, which is also what the matrix
 // instructions take of it as an operand, and 16 lanes of a block of 32 columns are 64 bytes of a row.  The weight's rows are put in such an order
@@ -267,6 +267,7 @@ struct NarrowLinearBackwardArgs {
 template <typename E, int kP, int kO>
 struct NarrowShare {
     static constexpr int kWaves = sizeof(E) == 4 && kP * kO > 32 * 32 ? 4 : 8, kTile = 16 * kWaves;          // kTile vertices of a workgroup
+    static constexpr int kWavesASimd = sizeof(E) == 4 && kP * kO > 64 * 64 ? 1 : 2;
     static constexpr int kDown = 2, kAcross = kP / 16 < kWaves / 2 ? kP / 16 : kWaves / 2, kParts = kWaves / (kDown * kAcross);
     static constexpr int kFragsO = kO / 16 / kDown, kFragsP = kP / 16 / kAcross;
     static constexpr int kLdO = kO + 8, kLdP = kP + 8;                  // rows of LDS start in different banks
@@ -276,7 +277,7 @@ struct NarrowShare {
 // dz stays in registers as an operand for dx; for the weight's gradient, a sum over the vertices, dz and x pass through LDS, which hands them out by
 // columns.  Sums over the vertices stay in registers until the end; the workgroups' are added in their order (column_sums.hpp).
 template <typename E, int kP, int kO, bool kX8, bool kWhole>
-__global__ __launch_bounds__((64 * NarrowShare<E, kP, kO>::kWaves), 2) void narrow_linear_backward_kernel(NarrowLinearBackwardArgs<E> a) {
+__global__ __launch_bounds__((64 * NarrowShare<E, kP, kO>::kWaves), (NarrowShare<E, kP, kO>::kWavesASimd)) void narrow_linear_backward_kernel(NarrowLinearBackwardArgs<E> a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using Share = NarrowShare<E, kP, kO>;
     constexpr int kNarrowWaves = Share::kWaves, kNarrowTile = Share::kTile;
