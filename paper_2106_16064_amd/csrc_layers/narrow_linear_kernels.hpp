@@ -5,7 +5,8 @@
 // 2^20 vertices, bfloat16, with residual: 64 -> 64 forward 105 us (537 MB, 5.1 TB/s), gradient 127 us (537 MB, 4.2 TB/s); 128 -> 128 with
 // activations kept in 8 bits 250 us (1.08 GB, 4.3 TB/s; gelu and what becomes 8 bits are 150 us of vector instructions beside that) and
 // 215 to 250 us (0.81 GB).  The products of matrix_tiles.hpp one after the other: 183 and 270 us, 417 and 560 us.  Float, gelu, 32 -> 32 forward 88 us
-// (403 MB, 4.6 TB/s), gradient 125 us (537 MB, 4.3 TB/s), by tiles of 64 167 and 325 us; 64 -> 128 with residual 400 and 547 us, by tiles 428 and 762.
+// (403 MB, 4.6 TB/s), gradient 125 us (537 MB, 4.3 TB/s), by tiles of 64 167 and 325 us; 64 -> 128 with residual 400 and 550 to 570 us,
+// by tiles 428 and 762.
 //
 // A lane has a vertex (l % 16 of 16) and, q = l / 16, columns 32 t + 8 q ... + 7 of every 32: a piece of 16 bytes, which is also what the matrix
 // instructions take of it as an operand, and 16 lanes of a block of 32 columns are 64 bytes of a row.  The weight's rows are put in such an order
@@ -398,7 +399,8 @@ __global__ __launch_bounds__((64 * NarrowShare<E, kP, kO>::kWaves), (NarrowShare
 #pragma unroll
                 for (int p = 0; p < kXParts; ++p) *reinterpret_cast<s16x8*>(x_rows[p] + in_tile * Share::kLdP + 32 * u + first) = in[u].q[p];
         }
-        ask(row + step);
+        constexpr bool kLate = kFloat && kP * kO > 64 * 64 && kO > 64;         // the next rows and these ones' dz are more than the registers hold
+        if constexpr (!kLate) ask(row + step);
         if (a.weight_sums) __syncthreads();
         if (a.dx) {
 #pragma unroll
@@ -422,6 +424,7 @@ __global__ __launch_bounds__((64 * NarrowShare<E, kP, kO>::kWaves), (NarrowShare
                 if (row < a.rows && here > 0) store_chunk(a.dx + row * a.width + col, here, v);
             }
         }
+        if constexpr (kLate) ask(row + step);
         if (a.weight_sums) {
             // 16 columns of 32 vertices, of each plane
             auto columns = [&](const auto& rows, int ld, int vertex, int column) {
