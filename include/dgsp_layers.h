@@ -168,7 +168,7 @@ int dgsp_quantise(int64_t rows, int64_t width, int type, int kind, const void *x
 int dgsp_dequantise(int64_t rows, int64_t width, int type, int kind, const void *values, int64_t ldv, const void *scales, void *y,
                     int64_t ldy, void *stream);
 
-/* dgsp_rms_norm without dropout, y in DGSP_E4M3: made from y in 32 bits. */
+/* dgsp_rms_norm without dropout, y in DGSP_E4M3: made from s, which is held in 32 bits, in 64 bits and rounded once. */
 int dgsp_rms_norm_8bit(int64_t rows, int64_t width, int type, int param_type, const void *x, int64_t ldx, const void *residual,
                        int64_t ldr, const void *weight, float eps, void *values, int64_t ldv, void *scales, void *sum, int64_t lds,
                        void *stream);

@@ -34,10 +34,10 @@ struct Team {
         }
     }
     // Sums of kValues numbers over the team.  `turn` alternates, so that one barrier a sum is enough for a workgroup.
-    template <int kValues>
-    __device__ __forceinline__ void sum(float (&v)[kValues], int& turn) const {
+    template <typename V, int kValues>
+    __device__ __forceinline__ void sum(V (&v)[kValues], int& turn) const {
         if constexpr (kWhole) {
-            __shared__ float part[2][kValues][kMostWaves];
+            __shared__ V part[2][kValues][kMostWaves];
 #pragma unroll
             for (int i = 0; i < kValues; ++i) v[i] = lanes_sum(v[i], 64);
             const int waves = blockDim.x >> 6;
@@ -48,7 +48,7 @@ struct Team {
 #pragma unroll
             for (int i = 0; i < kValues; ++i) {             // a wave's sum a lane, in every 16 lanes: read one by one they took a third of the time
                 const int w = threadIdx.x % kMostWaves;
-                v[i] = lanes_sum(w < waves ? part[turn][i][w] : 0.0f, kMostWaves);
+                v[i] = lanes_sum(w < waves ? part[turn][i][w] : V(0), kMostWaves);
             }
             turn ^= 1;
         } else {

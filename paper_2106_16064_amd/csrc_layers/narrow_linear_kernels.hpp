@@ -268,7 +268,7 @@ struct NarrowLinearBackwardArgs {
 template <typename E, int kP, int kO>
 struct NarrowShare {
     static constexpr int kWaves = sizeof(E) == 4 && kP * kO > 32 * 32 ? 4 : 8, kTile = 16 * kWaves;          // kTile vertices of a workgroup
-    static constexpr int kWavesASimd = sizeof(E) == 4 && kP * kO > 64 * 64 ? 1 : 2;
+    static constexpr int kWavesASimd = sizeof(E) == 4 && (kP > 64 || kO > 64) ? 1 : 2;
     static constexpr int kDown = 2, kAcross = kP / 16 < kWaves / 2 ? kP / 16 : kWaves / 2, kParts = kWaves / (kDown * kAcross);
     static constexpr int kFragsO = kO / 16 / kDown, kFragsP = kP / 16 / kAcross;
     static constexpr int kLdO = kO + 8, kLdP = kP + 8;                  // rows of LDS start in different banks

@@ -29,12 +29,31 @@ struct RmsArgs {
 
 constexpr ScaleRange kE4m3Range{1, 246};
 
-// 1 / sqrt(mean + eps).  Before a rounding to 8 bits the last steps are made in 64 bits: an error of the mean's quotient or of the root would move a
-// whole row, and carry as many of its elements across a border between two steps as their own roundings do.
+// What the sum, the root and the products are made in.  Before a rounding to 8 bits 64 bits: an error of y is a hundred times as likely as its own size to
+// carry an element across a border between two steps (of 4099 x 1001 in 32 bits two or three; rounded from 64 to 32 in between, one).
+// Memory bounds the kernel either way.
 template <bool k8bit>
-__device__ __forceinline__ float reciprocal_root(float squares, int64_t width, float part, float eps) {
-    if constexpr (k8bit) return (float)(1.0 / sqrt((double)squares / (double)width + (double)eps));
-    return 1.0f / sqrtf(squares * part + eps);
+using Wide = std::conditional_t<k8bit, double, float>;
+
+// A number on its way to 8 bits: what 32 bits cannot hold of it leaves a 1 in the last place, so that the second rounding is that of the whole.
+__device__ __forceinline__ float narrowed(float v) { return v; }
+__device__ __forceinline__ float narrowed(double v) {
+    constexpr uint32_t kRest = (1u << 29) - 1;
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    const uint32_t low = (uint32_t)bits, odd = (((low & kRest) + kRest) | low) & ~kRest;
+    return (float)__builtin_bit_cast(double, (bits & ~0xffffffffull) | odd);
+}
+
+// 1 / sqrt(mean + eps); `part`: 1 / width.  In 64 bits by the hardware's first guess, good to 2^-24 or better, and a step of Newton's, which squares its error.
+template <bool k8bit>
+__device__ __forceinline__ Wide<k8bit> reciprocal_root(Wide<k8bit> squares, Wide<k8bit> part, float eps) {
+    const Wide<k8bit> mean = squares * part + eps;
+    if constexpr (k8bit) {
+        const double guess = __builtin_amdgcn_rsq(mean), better = guess + 0.5 * guess * fma(-mean * guess, guess, 1.0);
+        return guess > 0.0 && guess < __builtin_inf() ? better : guess;
+    } else {
+        return 1.0f / sqrtf(mean);
+    }
 }
 
 template <typename T, bool kWhole, bool kAdd, bool k8bit>
@@ -51,13 +70,14 @@ __global__ __launch_bounds__(kWhole ? 1024 : 256) void rms_norm_kernel(RmsArgs<T
     };
     ask(team.row);
     if (here > 0) load_params<T>(a.weight, a.wide, col, here, 1.0f, w);
-    const float part = 1.0f / (float)a.width;
+    const Wide<k8bit> part = Wide<k8bit>(1) / (Wide<k8bit>)a.width;
     int turn = 0;
     // all teams of a workgroup make the same number of turns
     const int64_t base = team.row - (kWhole ? 0 : threadIdx.x / team.lanes);
     for (int64_t at = base, row = team.row; at < a.rows; at += team.step, row += team.step) {
         const bool inside = row < a.rows && here > 0;
-        float s[kChunk], squares[1] = {0.0f};
+        float s[kChunk];
+        Wide<k8bit> squares[1] = {0};
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) s[j] = 0.0f;
         if (inside) {
@@ -72,12 +92,12 @@ __global__ __launch_bounds__(kWhole ? 1024 : 256) void rms_norm_kernel(RmsArgs<T
         }
         ask(row + team.step);
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) squares[0] += s[j] * s[j];
+        for (int j = 0; j < kChunk; ++j) squares[0] += (Wide<k8bit>)s[j] * (Wide<k8bit>)s[j];
         team.sum(squares, turn);
-        const float rstd = reciprocal_root<k8bit>(squares[0], a.width, part, a.eps);
+        const Wide<k8bit> rstd = reciprocal_root<k8bit>(squares[0], part, a.eps);
         float out[kChunk];
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) out[j] = inside && j < here ? s[j] * rstd * w[j] : 0.0f;
+        for (int j = 0; j < kChunk; ++j) out[j] = inside && j < here ? narrowed(s[j] * rstd * w[j]) : 0.0f;
         if constexpr (k8bit) {                              // all lanes of a block, of which the last may lie behind the row
             uint32_t scale;
             const uint2 bytes = to_8bit<true>(out, kE4m3Range, scale);
@@ -86,7 +106,7 @@ __global__ __launch_bounds__(kWhole ? 1024 : 256) void rms_norm_kernel(RmsArgs<T
         if (!inside) continue;
         if constexpr (!k8bit) store_chunk(a.y + row * a.ldy + col, here, out);
         if constexpr (kAdd) store_chunk(a.sum + row * a.lds + col, here, s);
-        if (a.rstd && team.lane == 0) a.rstd[row] = rstd;
+        if (a.rstd && team.lane == 0) a.rstd[row] = (float)rstd;
     }
 }
 
@@ -209,7 +229,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(RmsArgs<T> a) {
     const uint64_t offset = a.mask.device_offset ? *a.mask.device_offset : a.mask.offset;
     const Team<true> team(1024);
     int turn = 0;
-    const float part = 1.0f / (float)a.width;
+    const Wide<k8bit> part = Wide<k8bit>(1) / (Wide<k8bit>)a.width;
     const int64_t chunks = k8bit ? (a.rows8.blocks + 3) / 4 * 4 * kBlockLanes : (a.width + kChunk - 1) / kChunk;
     for (int64_t row = team.row; row < a.rows; row += team.step) {
         auto at = [&](int64_t chunk, float (&v)[kChunk]) {
@@ -221,13 +241,14 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(RmsArgs<T> a) {
             if (a.mask.dropped) drop(a.mask, offset, row, chunk, v);
             for (int j = 0; j < kChunk; ++j) v[j] += add[j];
         };
-        float squares[1] = {0.0f}, v[kChunk];
+        Wide<k8bit> squares[1] = {0};
+        float v[kChunk];
         for (int64_t c = threadIdx.x; c * kChunk < a.width; c += blockDim.x) {
             at(c, v);
-            for (int j = 0; j < kChunk; ++j) squares[0] += c * kChunk + j < a.width ? v[j] * v[j] : 0.0f;
+            for (int j = 0; j < kChunk; ++j) squares[0] += c * kChunk + j < a.width ? (Wide<k8bit>)v[j] * (Wide<k8bit>)v[j] : Wide<k8bit>(0);
         }
         team.sum(squares, turn);
-        const float rstd = reciprocal_root<k8bit>(squares[0], a.width, part, a.eps);
+        const Wide<k8bit> rstd = reciprocal_root<k8bit>(squares[0], part, a.eps);
         for (int64_t c = threadIdx.x; c < chunks; c += blockDim.x) {
             const int64_t col = c * kChunk, here = a.width - col;
             float w[kChunk], out[kChunk];
@@ -235,7 +256,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(RmsArgs<T> a) {
             if (here > 0) {
                 at(c, v);
                 load_params<T>(a.weight, a.wide, col, here, 1.0f, w);
-                for (int j = 0; j < kChunk; ++j) out[j] = j < here ? v[j] * rstd * w[j] : 0.0f;
+                for (int j = 0; j < kChunk; ++j) out[j] = j < here ? narrowed(v[j] * rstd * w[j]) : 0.0f;
             }
             if constexpr (k8bit) {
                 uint32_t scale;
@@ -246,7 +267,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(RmsArgs<T> a) {
             }
             if (a.sum && here > 0) store_chunk(a.sum + row * a.lds + col, here, v);
         }
-        if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+        if (a.rstd && threadIdx.x == 0) a.rstd[row] = (float)rstd;
     }
 }
 
