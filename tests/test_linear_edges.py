@@ -10,6 +10,7 @@ import linear_reference as lin
 from layer_reference import UNIT
 from paper_2106_16064_amd import layers
 from test_linear import check, inputs
+from test_linear_8bit import check as check_8bit
 
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 
@@ -248,9 +249,16 @@ def test_widest_products(width, out, rows, dtype):
 # ---------------------------------------------------------------- deep sums
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,width,out", [(2800, 8300, 2560), (200, 4096, 5000), (1, 20000, 300), (16, 4096, 1000), (33, 4096, 130)])
+def test_deep_sums_in_8_bits(rows, width, out):
+    show("deep sums in 8 bits", rows, width, out)
+    check_8bit(rows, width, out, torch.bfloat16, "silu", 300, at="cuda")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,rows,width,out", [
     (torch.bfloat16, 12000, 1500, 2000), (torch.float16, 10300, 1040, 1024), (torch.bfloat16, 8200, 1024, 4096), (torch.bfloat16, 50000, 301, 777),
-    (torch.bfloat16, 200, 4096, 5000), (torch.float32, 50000, 64, 64), (torch.float32, 40000, 33, 70), (torch.float32, 20001, 129, 130), (torch.float32, 8200, 128, 512),
+    (torch.bfloat16, 200, 4096, 5000), (torch.float16, 2800, 4104, 2560), (torch.bfloat16, 16, 16384, 520), (torch.float32, 50000, 64, 64), (torch.float32, 30000, 33, 128), (torch.float32, 40000, 33, 70), (torch.float32, 20001, 129, 130), (torch.float32, 8200, 128, 512),
     (torch.float32, 4100, 2048, 2050), (torch.float32, 3000, 31, 33), (torch.float32, 1000, 300, 200)], ids=str)
 def test_deep_sums(dtype, rows, width, out):
     """Weights' gradients that are split to fill the GPU, with tiles of each size, few and many splits and results; of float their bias's beside them."""
