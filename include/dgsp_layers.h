@@ -175,7 +175,7 @@ int dgsp_rms_norm_8bit(int64_t rows, int64_t width, int type, int param_type, co
 
 /*
  * What a product keeps for its backward pass.  DGSP_KEEP_WHOLE: x, and of z as much as the activation's derivative needs (z in
- * `type`; of relu the derivative in a byte; without an activation nothing).  DGSP_KEEP_8BIT: x in DGSP_INT8, and act'(z) in steps of
+ * `bias_type`, which is that of its gradient; of relu the derivative in a byte; without an activation nothing).  DGSP_KEEP_8BIT: x in DGSP_INT8, and act'(z) in steps of
  * 1/112 in a byte, which has 0 and 1 exactly and a code for NaN.
  */
 typedef enum { DGSP_KEEP_NOTHING = 0, DGSP_KEEP_WHOLE = 1, DGSP_KEEP_8BIT = 2 } dgsp_keep_t;
@@ -195,7 +195,7 @@ typedef enum { DGSP_KEEP_NOTHING = 0, DGSP_KEEP_WHOLE = 1, DGSP_KEEP_8BIT = 2 } 
 int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int type, int bias_type, int activation, int keep, const void *x,
                 int64_t ldx, const void *weight, int64_t ldw, const void *bias, const void *residual, int64_t ldr, void *y,
                 int64_t ldy, void *saved, void *x_values, int64_t ldv, void *x_scales, void *workspace, int64_t workspace_bytes, void *stream);
-int64_t dgsp_linear_saved_bytes(int64_t rows, int64_t out_width, int type, int activation, int keep);
+int64_t dgsp_linear_saved_bytes(int64_t rows, int64_t out_width, int type, int bias_type, int activation, int keep);
 int64_t dgsp_linear_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type);
 
 /*

@@ -64,10 +64,10 @@ struct BackwardPieces {
 
 }  // namespace
 
-extern "C" int64_t dgsp_linear_saved_bytes(int64_t rows, int64_t out_width, int type, int activation, int keep) {
-    if (!linear_extents(rows, 1, out_width, type) || !known_epilogue(activation) || !known_keep(keep)) return 0;
+extern "C" int64_t dgsp_linear_saved_bytes(int64_t rows, int64_t out_width, int type, int bias_type, int activation, int keep) {
+    if (!linear_extents(rows, 1, out_width, type) || (bias_type != type && bias_type != DGSP_F32) || !known_epilogue(activation) || !known_keep(keep)) return 0;
     const Left what = left(activation, keep);
-    return what == kNothing ? 0 : what == kCodes ? rows * padded(out_width, 8) : kept_bytes(rows, out_width, type);
+    return what == kNothing ? 0 : what == kCodes ? rows * padded(out_width, 8) : kept_bytes(rows, out_width, bias_type);
 }
 
 extern "C" int64_t dgsp_linear_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type) {
@@ -102,7 +102,7 @@ extern "C" int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int t
         return with_type(type, [&](auto element) {
             using T = decltype(element);
             return narrow_linear<T>({rows, width, out_width, activation, static_cast<const T*>(x), static_cast<const T*>(weight), ldx, ldw, bias, bias_type != type,
-                                     static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, what == kZ ? static_cast<T*>(saved) : nullptr,
+                                     static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, what == kZ ? saved : nullptr,
                                      what == kCodes ? static_cast<uint8_t*>(saved) : nullptr, padded(out_width, 8),
                                      x_values ? rows8(x_values, rows, width, ldv, x_scales) : Rows8{}, scale_range(DGSP_INT8, type)},
                                     static_cast<hipStream_t>(stream));
@@ -164,7 +164,7 @@ extern "C" int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_wid
         return with_type(type, [&](auto element) {
             using T = decltype(element);
             return narrow_linear_backward<T>({rows, width, out_width, activation, in_8bit ? nullptr : static_cast<const T*>(x), static_cast<const T*>(weight),
-                                              static_cast<const T*>(dy), ldx, ldw, lddy, what == kZ ? static_cast<const T*>(saved) : nullptr,
+                                              static_cast<const T*>(dy), ldx, ldw, lddy, what == kZ ? saved : nullptr, bias_type != type,
                                               what == kCodes ? static_cast<const uint8_t*>(saved) : nullptr, padded(out_width, 8),
                                               in_8bit && dweight ? rows8(const_cast<void*>(x), rows, width, ldx, const_cast<void*>(x_scales)) : Rows8{},
                                               static_cast<T*>(dx), nullptr, nullptr},
@@ -201,7 +201,7 @@ extern "C" int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_wid
         // the sums over the rows: with dz, or with the weight's gradient, or on their own
         const bool sums_beside = kFloat && activation == DGSP_ACT_NONE && dweight && dbias;
         if (rows > 0 && (activation != DGSP_ACT_NONE ? dx || dweight || dbias : dbias && !sums_beside)) {
-            const LinearSlopeArgs<T> args{rows, out_width, slices.lanes, static_cast<const T*>(dy), lddy, what == kZ ? static_cast<const T*>(saved) : nullptr,
+            const LinearSlopeArgs<T> args{rows, out_width, slices.lanes, static_cast<const T*>(dy), lddy, what == kZ ? saved : nullptr, bias_type != type,
                                           what == kCodes ? static_cast<const uint8_t*>(saved) : nullptr, kept_ld, activation,
                                           activation != DGSP_ACT_NONE && (dx || dweight) ? static_cast<T*>(at.dz) : nullptr,
                                           dbias ? static_cast<float*>(at.sums) : nullptr};

@@ -21,7 +21,7 @@ LinearOut<T> linear_out(void* y, int64_t ldy, const void* bias, bool wide, const
     out.residual = static_cast<const T*>(residual);
     out.ldr = ldr;
     out.activation = activation;
-    out.z = static_cast<T*>(z);
+    out.z = z;
     out.codes = static_cast<uint8_t*>(codes);
     out.kept_ld = padded(out_width, 8);
     out.partial = static_cast<float*>(partial);

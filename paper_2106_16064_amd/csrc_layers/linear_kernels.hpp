@@ -1,8 +1,8 @@
 // y = act(x w^T + bias) + residual on matrix_tiles.hpp: what becomes of the product of a tile, and what the backward pass makes of dy first.
 //
 // The epilogue adds the bias to the sum in 32 bits, applies the activation, adds the residual and rounds once.  For the backward pass it
-// leaves what the activation's derivative is made of: z in the matrix's type (its rounding moves act'(z) by |z act''(z)| half a step, a
-// fifth of what rounding dz itself costs), or act'(z) in steps of 1/112 in 8 bits, which has 0 and 1 exactly: all of relu's, and what gelu
+// leaves what the activation's derivative is made of: z in the bias's type (where that is 16 bits its rounding moves act'(z) by |z act''(z)| half
+// a step, a fifth of what rounding dz itself costs; a float bias's gradient is not rounded, and would lose by it), or act'(z) in steps of 1/112 in 8 bits, which has 0 and 1 exactly: all of relu's, and what gelu
 // (-0.13 ... 1.13) and silu (-0.10 ... 1.10) come to far from 0.
 //
 // What it costs beside the product, bfloat16, 8192 x 4096 -> 16384, gelu, z kept: 1050 to 1090 us against 900 of the product alone, of which
@@ -74,12 +74,12 @@ struct LinearOut {
     T* y;
     int64_t ldy;
     bool vectors, bias_vectors, residual_vectors;       // four neighbours may be read or written at once
-    bool wide;                  // the bias in float
+    bool wide;                  // the bias, and z, in float
     const void* bias;           // null: none
     const T* residual;          // null: none
     int64_t ldr;
     int activation;
-    T* z;                       // null: not wanted; ld is `kept_ld`, a multiple of 8
+    void* z;                    // in T or, if `wide`, in float; null: not wanted; ld is `kept_ld`, a multiple of 8
     uint8_t* codes;             // null: not wanted; likewise
     int64_t kept_ld;
     float* partial;             // not null: split results, [split][m][n padded to 4], for linear_join_kernel
@@ -108,8 +108,13 @@ struct LinearOut {
         } else {
             activate_only<sizeof(T) == 4>(activation, in, value);
         }
-        if (z) {
-            T* to = z + m * kept_ld + n;
+        if (z && wide) {
+            float* to = static_cast<float*>(z) + m * kept_ld + n;
+#pragma unroll
+            for (int j = 0; j < kCount; ++j)
+                if (kWhole || left > kStep * j) *reinterpret_cast<f32x4*>(to + kStep * j) = f32x4{in[4 * j], in[4 * j + 1], in[4 * j + 2], in[4 * j + 3]};
+        } else if (z) {
+            T* to = static_cast<T*>(z) + m * kept_ld + n;
 #pragma unroll
             for (int j = 0; j < kCount; ++j)
                 if (kWhole || left > kStep * j)
@@ -221,7 +226,8 @@ struct LinearSlopeArgs {
     int lanes;                  // of a row, a power of two up to 256
     const T* dy;
     int64_t lddy;
-    const T* z;                 // one of these two, or none: the slope is 1
+    const void* z;              // one of these two, or none: the slope is 1
+    bool wide;                  // z in float
     const uint8_t* codes;
     int64_t kept_ld;
     int activation;
@@ -249,9 +255,13 @@ __global__ __launch_bounds__(256) void linear_slope_kernel(LinearSlopeArgs<T> a)
                 for (int j = 0; j < kChunk; ++j) slope[j] = slope_of(codes, j);
             } else if (a.z) {
                 float z[kChunk], value[kChunk];
-                widen(load_chunk(a.z + row * a.kept_ld + col, kChunk), z);
+                if (a.wide) {
+                    widen(load_chunk(static_cast<const float*>(a.z) + row * a.kept_ld + col, kChunk), z);
+                } else {
+                    widen(load_chunk(static_cast<const T*>(a.z) + row * a.kept_ld + col, kChunk), z);
+                }
 #pragma unroll
-                for (int j = 0; j < kChunk; ++j) z[j] = inside_range<T>(z[j]);
+                for (int j = 0; j < kChunk; ++j) z[j] = a.wide ? inside_range<float>(z[j]) : inside_range<T>(z[j]);
                 activate<sizeof(T) == 4>(a.activation, z, value, slope);
             } else {
 #pragma unroll

@@ -86,8 +86,11 @@ int narrow_linear_backward(NarrowLinearBackwardArgs<E> args, void* dweight, void
         with_widths<E>(args.width, args.out_width, [&](auto p, auto o) {
             constexpr int kP = decltype(p)::value, kO = decltype(o)::value;
             with_flags(args.x8.values != nullptr, args.width == kP && args.out_width == kO, [&](auto x8, auto whole) {
-                narrow_linear_backward_kernel<E, kP, kO, decltype(x8)::value, decltype(whole)::value>
-                    <<<(unsigned)b.groups, 64 * NarrowShare<E, kP, kO>::kWaves, 0, stream>>>(args);
+                constexpr bool kX8 = decltype(x8)::value, kWhole = decltype(whole)::value;
+                const dim3 groups((unsigned)b.groups), threads(64 * NarrowShare<E, kP, kO>::kWaves);
+                if constexpr (sizeof(E) == 2 && !kX8)
+                    if (args.wide && args.z) return narrow_linear_backward_kernel<E, kP, kO, kX8, kWhole, float><<<groups, threads, 0, stream>>>(args);
+                narrow_linear_backward_kernel<E, kP, kO, kX8, kWhole, E><<<groups, threads, 0, stream>>>(args);
             });
         });
     if (dweight) launch_column_sums<E>(args.out_width * args.width, args.rows > 0 ? b.groups * b.parts : 0, args.weight_sums, dweight, false, stream);

@@ -30,12 +30,12 @@ struct NarrowLinearArgs {
     const E *x, *weight;
     int64_t ldx, ldw;
     const void* bias;
-    bool wide;                  // the bias in float
+    bool wide;                  // the bias, and z, in float
     const E* residual;
     int64_t ldr;
     E* y;
     int64_t ldy;
-    E* z;                       // kept: one of these two, or none; ld is `kept_ld`, a multiple of 8
+    void* z;                    // kept: one of these two, or none; ld is `kept_ld`, a multiple of 8
     uint8_t* codes;
     int64_t kept_ld;
     Rows8 x8;                   // x in whole numbers of 8 bits: written by the forward pass, read by the backward pass; or not
@@ -234,7 +234,12 @@ __global__ __launch_bounds__(256, (kP * kO * kPlanes<E> > 64 * 64 ? 3 : 4)) void
                 if (store) *reinterpret_cast<uint2*>(a.codes + row * a.kept_ld + col) = bytes;
             } else {
                 activate_only<kFloat>(a.activation, z, value);
-                if (a.z && store) store_chunk(a.z + row * a.kept_ld + col, kChunk, z);
+                if (a.z && store) {
+                    if (a.wide)
+                        store_chunk(static_cast<float*>(a.z) + row * a.kept_ld + col, kChunk, z);
+                    else
+                        store_chunk(static_cast<E*>(a.z) + row * a.kept_ld + col, kChunk, z);
+                }
             }
             if (a.residual) {
                 float add[kChunk];
@@ -254,7 +259,8 @@ struct NarrowLinearBackwardArgs {
     int activation;
     const E *x, *weight, *dy;
     int64_t ldx, ldw, lddy;
-    const E* z;                 // what was kept: one of these two, or none
+    const void* z;              // what was kept: one of these two, or none
+    bool wide;                  // z in float
     const uint8_t* codes;
     int64_t kept_ld;
     Rows8 x8;                   // in place of x
@@ -277,7 +283,8 @@ struct NarrowShare {
 
 // dz stays in registers as an operand for dx; for the weight's gradient, a sum over the vertices, dz and x pass through LDS, which hands them out by
 // columns.  Sums over the vertices stay in registers until the end; the workgroups' are added in their order (column_sums.hpp).
-template <typename E, int kP, int kO, bool kX8, bool kWhole>
+// Z: the type that z was kept in
+template <typename E, int kP, int kO, bool kX8, bool kWhole, typename Z>
 __global__ __launch_bounds__((64 * NarrowShare<E, kP, kO>::kWaves), (NarrowShare<E, kP, kO>::kWavesASimd)) void narrow_linear_backward_kernel(NarrowLinearBackwardArgs<E> a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using Share = NarrowShare<E, kP, kO>;
@@ -309,7 +316,8 @@ __global__ __launch_bounds__((64 * NarrowShare<E, kP, kO>::kWaves), (NarrowShare
     const int in_tile = wave * 16 + lane % 16;
     const int width = kWhole ? kP : (int)a.width, out_width = kWhole ? kO : (int)a.out_width, blocks = (width + kBlock - 1) / kBlock;
     const int down = wave % Share::kDown, across = wave / Share::kDown % Share::kAcross, part = wave / (Share::kDown * Share::kAcross);
-    RawChunk<E> dy[kT], z[kT], x[kU];
+    RawChunk<E> dy[kT], x[kU];
+    RawChunk<Z> z[kT];
     uint2 codes[kT], x8[kU];
     uint32_t scales = 0;
     auto ask = [&](int64_t row) {
@@ -321,7 +329,7 @@ __global__ __launch_bounds__((64 * NarrowShare<E, kP, kO>::kWaves), (NarrowShare
             const int64_t at = kWhole || col < out_width ? kept_row + col : 0;
             dy[t] = row_chunk<kWhole>(a.dy, row, a.lddy, col, out_width, inside);
             if (a.codes) codes[t] = *reinterpret_cast<const uint2*>(a.codes + at);
-            if (a.z) z[t] = load_chunk(a.z + at, kChunk);
+            if (a.z) z[t] = load_chunk(static_cast<const Z*>(a.z) + at, kChunk);
         }
         if (!a.weight_sums) return;
         if constexpr (kX8) scales = *reinterpret_cast<const uint32_t*>(a.x8.scales + (inside ? row * 4 : 0));
@@ -361,7 +369,7 @@ __global__ __launch_bounds__((64 * NarrowShare<E, kP, kO>::kWaves), (NarrowShare
                 float at[kChunk], value[kChunk];
                 widen(z[t], at);
 #pragma unroll
-                for (int j = 0; j < kChunk; ++j) at[j] = inside_range<E>(at[j]);
+                for (int j = 0; j < kChunk; ++j) at[j] = inside_range<Z>(at[j]);
                 activate<kFloat>(a.activation, at, value, slope);
             } else {
 #pragma unroll

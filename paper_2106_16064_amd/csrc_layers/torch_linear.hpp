@@ -54,7 +54,7 @@ LinearResult run_linear(const LinearCall& c, const at::Tensor& x, bool x_in_8bit
     const c10::DeviceGuard guard(x.device());
     const int64_t rows = c.rows(), width = c.width(), out_width = c.out_width();
     at::Tensor y = empty_on(with_last(x, out_width), x.scalar_type(), x), saved;
-    const int64_t kept = dgsp_linear_saved_bytes(rows, out_width, c.type, c.activation, c.keep);
+    const int64_t kept = dgsp_linear_saved_bytes(rows, out_width, c.type, c.bias_type, c.activation, c.keep);
     if (c.keep != DGSP_KEEP_NOTHING) saved = empty_bytes(kept, x);
     const int64_t bytes = dgsp_linear_workspace_bytes(rows, width, out_width, c.type);
     const at::Tensor workspace = bytes ? empty_bytes(bytes, x) : at::Tensor();
@@ -95,7 +95,8 @@ LinearGradient run_linear_backward(const at::Tensor& x, const at::Tensor& scales
         w = matrix_of(weight, "weight");
         if (w.rows != out_width || w.width != width) refuse("weight must have the shape it had");
     }
-    const int64_t kept = dgsp_linear_saved_bytes(rows, out_width, type, activation, keep);
+    const int to = bias_type == at::kFloat ? DGSP_F32 : type;
+    const int64_t kept = dgsp_linear_saved_bytes(rows, out_width, type, to, activation, keep);
     if (kept) check_left(saved, at::kByte, kept, dy, "saved");
     LinearGradient out;
     if (want_x) out.x = empty_on(with_last(dy, width), dy.scalar_type(), dy);
@@ -103,7 +104,7 @@ LinearGradient run_linear_backward(const at::Tensor& x, const at::Tensor& scales
     if (want_bias) out.bias = empty_on(at::IntArrayRef(&out_width, 1), bias_type, dy);
     const int64_t bytes = dgsp_linear_backward_workspace_bytes(rows, width, out_width, type, activation, keep);
     const at::Tensor workspace = bytes ? empty_bytes(bytes, dy) : at::Tensor();
-    check(dgsp_linear_backward(rows, width, out_width, type, bias_type == at::kFloat ? DGSP_F32 : type, activation, keep, at_or_null(in.t), in.ld,
+    check(dgsp_linear_backward(rows, width, out_width, type, to, activation, keep, at_or_null(in.t), in.ld,
                                at_or_null(in_scales), at_or_null(w.t), w.ld, at_or_null(saved), ptr(grad.t), grad.ld, at_or_null(out.x), at_or_null(out.weight),
                                at_or_null(out.bias), at_or_null(workspace), bytes, stream()),
           "dgsp_linear_backward");

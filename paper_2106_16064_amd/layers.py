@@ -85,7 +85,7 @@ def lib():
         L.dgsp_dequantise.argtypes = [i64, i64, ci, ci, vp, i64, vp, vp, i64, vp]
         L.dgsp_rms_norm_8bit.argtypes = [i64, i64, ci, ci, vp, i64, vp, i64, vp, cf, vp, i64, vp, vp, i64, vp]
         L.dgsp_linear.argtypes = [i64] * 3 + [ci] * 4 + [vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp]
-        L.dgsp_linear_saved_bytes.argtypes = [i64, i64, ci, ci, ci]
+        L.dgsp_linear_saved_bytes.argtypes = [i64, i64, ci, ci, ci, ci]
         L.dgsp_linear_workspace_bytes.argtypes = [i64, i64, i64, ci]
         L.dgsp_linear_backward.argtypes = [i64] * 3 + [ci] * 4 + [vp, i64, vp, vp, i64, vp, vp, i64, vp, vp, vp, vp, i64, vp]
         L.dgsp_linear_backward_workspace_bytes.argtypes = [i64, i64, i64, ci, ci, ci]

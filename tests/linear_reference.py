@@ -2,7 +2,7 @@
 
 Bounds, element by element, with e = 2^-24 and u half a step of the type: a sum of n products in 32 bits is off by (n + 4) e times the sum of
 the magnitudes; exp, erf and the reciprocal by 8 e of 1 + |z|, and the activations grow by at most 1.13 and their derivatives by 0.8 per unit
-of z; z is kept rounded (u |z|) or the derivative in steps of 1 / 112; dz is rounded (u |dz|) for the two products that read it."""
+of z; z is kept in the bias's type, rounded where that is (u |z|), or the derivative in steps of 1 / 112; dz is rounded (u |dz|) for the two products that read it."""
 import torch
 
 import layer_reference as ref
@@ -57,7 +57,7 @@ def backward(x, w, z, z_off, kind, dy, dtype, params, keep_8bit):
     elif kind == "relu":
         s_off = (z.abs() <= z_off).to(s.dtype)
     else:
-        s_off = 0.8 * (z_off + (0.0 if keep_8bit else u * z.abs() + TINY[dtype])) + 8 * EPS32 * (1 + z.abs()) + (0.5 / 112 if keep_8bit else 0.0)
+        s_off = 0.8 * (z_off + (0.0 if keep_8bit else UNIT[params] * z.abs() + TINY[params])) + 8 * EPS32 * (1 + z.abs()) + (0.5 / 112 if keep_8bit else 0.0)
     dz, dz_off = dy * s, dy.abs() * s_off + 2 * EPS32 * (dy * s).abs()
     rounded = 0.0 if dtype == torch.float32 or kind is None else u * (dz.abs() + dz_off) + TINY[dtype]
     off = dz_off + rounded

@@ -425,12 +425,14 @@ def test_sizes_without_a_gpu():
     L, most = layers.lib(), (1 << 31) - 1 - 4096
     for extents in ((-1, 8, 8), (most + 1, 8, 8), (8, 0, 8), (8, 8, 0), (8, 1 << 22, 8), (8, 8, 1 << 62)):
         assert L.dgsp_linear_workspace_bytes(*extents, 0) == 0 and L.dgsp_linear_backward_workspace_bytes(*extents, 0, 0, 1) == 0
-    assert L.dgsp_linear_saved_bytes(-1, 8, 0, 0, 1) == 0 and L.dgsp_linear_saved_bytes(8, 8, 0, 0, 9) == 0 and L.dgsp_linear_saved_bytes(8, 8, 0, 7, 1) == 0
+    assert L.dgsp_linear_saved_bytes(-1, 8, 0, 0, 0, 1) == 0 and L.dgsp_linear_saved_bytes(8, 8, 0, 0, 0, 9) == 0 and L.dgsp_linear_saved_bytes(8, 8, 0, 0, 7, 1) == 0
+    assert L.dgsp_linear_saved_bytes(8, 8, 0, 1, 0, 1) == 0
     for t, size in ((layers.F32, 4), (layers.BF16, 2), (layers.F16, 2)):
         for out, padded in ((1, 8), (8, 8), (33, 40)):
-            assert L.dgsp_linear_saved_bytes(10, out, t, layers.GELU, 1) == 10 * padded * size and L.dgsp_linear_saved_bytes(10, out, t, layers.GELU, 2) == 10 * padded
-            assert L.dgsp_linear_saved_bytes(10, out, t, layers.RELU, 1) == 10 * padded and L.dgsp_linear_saved_bytes(10, out, t, layers.SILU, 0) == 0
-            assert L.dgsp_linear_saved_bytes(10, out, t, layers.NO_ACTIVATION, 2) == 0
+            assert L.dgsp_linear_saved_bytes(10, out, t, t, layers.GELU, 1) == 10 * padded * size and L.dgsp_linear_saved_bytes(10, out, t, t, layers.GELU, 2) == 10 * padded
+            assert L.dgsp_linear_saved_bytes(10, out, t, layers.F32, layers.GELU, 1) == 10 * padded * 4
+            assert L.dgsp_linear_saved_bytes(10, out, t, layers.F32, layers.RELU, 1) == 10 * padded and L.dgsp_linear_saved_bytes(10, out, t, t, layers.SILU, 0) == 0
+            assert L.dgsp_linear_saved_bytes(10, out, t, t, layers.NO_ACTIVATION, 2) == 0
         for extents in ((0, 4096, 64), (0, 64, 4096), (0, 1, 1)):
             assert 0 <= L.dgsp_linear_workspace_bytes(*extents, t) <= L.dgsp_linear_workspace_bytes(1, *extents[1:], t)
             assert 0 <= L.dgsp_linear_backward_workspace_bytes(*extents, t, 0, 2) <= L.dgsp_linear_backward_workspace_bytes(1, *extents[1:], t, 0, 2)
