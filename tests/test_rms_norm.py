@@ -396,3 +396,18 @@ def test_sizes_and_refusals_without_a_gpu():
             call()
     assert L.dgsp_rms_norm(4, 8, 0, 0, None, 8, None, 0, None, None, 1e-5, None, 8, None, 0, None, None) == dg.ERR_INVALID_ARG
     assert L.dgsp_quantise(4, 8, 0, 0, None, 8, None, 32, None, None) == dg.ERR_INVALID_ARG
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,width", [(7, 24), (33, 64), (130, 513), (3, 1001), (300, 1001), (9, 2050), (3, 8192), (2, 8200), (2, 20000)])
+def test_sums_in_8_bits_are_rounded_once(rows, width, dtype):
+    """With a residual too every element is the nearest: s is the sum in 32 bits, and all that follows is made in 64."""
+    print("[case] add_rms_norm_8bit", rows, width, dtype, flush=True)
+    x, r, w = normal((rows, width), dtype, 95, 2.0), normal((rows, width), dtype, 96), normal((width,), torch.float32, 97, 0.2, 1.0)
+    y8, s = layers.add_rms_norm_8bit(x.cuda(), r.cuda(), w.cuda(), EPS)
+    S = x.float() + r.float()
+    assert torch.equal(s.cpu(), S.to(dtype))
+    values, exponents = ref8.quantised(definition(S.double(), torch.zeros_like(S, dtype=torch.float64), host(w), EPS)[0], "e4m3")
+    scale = y8.scales.cpu().transpose(0, 1).reshape(rows, -1)[:, :exponents.shape[1]].long() - 127
+    assert torch.equal(y8.values.cpu().double().view(values.shape), values) and torch.equal(scale, exponents.long())
