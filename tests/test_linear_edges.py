@@ -11,6 +11,7 @@ from layer_reference import UNIT
 from paper_2106_16064_amd import layers
 from test_linear import check, inputs
 from test_linear_8bit import check as check_8bit
+from test_rms_norm import gradient
 
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 
@@ -124,6 +125,22 @@ def test_norms_of_more_than_2_to_the_31_elements(dtype):
                 assert torch.equal(whole.values[part].view(torch.uint8), one.values.view(torch.uint8)) and torch.equal(whole.scales[:, part], one.scales)
                 assert torch.equal(back[part], layers.dequantise(one, dtype))
 
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_the_norms_weight_gradient_has_the_rows_at_both_ends_and_beyond_2_to_the_31(dtype):
+    """dy is zero but for some rows at the ends and around the 2^31st element, so that each of them counts: each adds its own term, and zeros, in
+    some thousand sums."""
+    show("rows that count", dtype)
+    rows, width = (1 << 20) + 77, 2056
+    x, dy = normal((rows, width), dtype, 0), torch.zeros((rows, width), dtype=dtype, device="cuda")
+    some = torch.cat([torch.arange(5), (1 << 31) // width + torch.arange(-3, 4), torch.arange(rows - 80, rows)]).cuda()
+    dy[some] = normal((len(some), width), dtype, 1)
+    w = normal((width,), dtype, 2).requires_grad_(True)
+    dw, = torch.autograd.grad(layers.rms_norm(x, w), w, dy)
+    S, G = x[some].double(), dy[some].double()
+    value, off = (t.cuda() for t in gradient(S.cpu(), torch.zeros_like(S.cpu()), w.detach().double().cpu(), G.cpu(), 1e-5)[2:])
+    within(dw, value, off * (1 + UNIT[dtype]) + UNIT[dtype] * value.abs(), "dw")
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("keep", [False, True])
