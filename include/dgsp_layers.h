@@ -205,7 +205,7 @@ int64_t dgsp_linear_workspace_bytes(int64_t rows, int64_t width, int64_t out_wid
  *   x, x_scales  DGSP_KEEP_WHOLE: the matrix, NULL.  DGSP_KEEP_8BIT: values and scales of x in DGSP_INT8; ldx is that of the values.
  *   dx, dweight, dbias   NULL: not wanted.  dx is rows x width, dweight out_width x width, both packed; dbias is of `bias_type`.
  * Of 16-bit types dz is rounded to `type`, as the matrix instructions take their operands (dbias is summed before that): in
- * float16 it becomes infinite beyond 65504 and loses bits below 2^-14.
+ * float16 it becomes infinite beyond 65504 and loses bits below 2^-14.  act'(z) of an infinite z is 1 or 0, whatever was kept.
  */
 int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_width, int type, int bias_type, int activation, int keep,
                          const void *x, int64_t ldx, const void *x_scales, const void *weight, int64_t ldw, const void *saved,

@@ -115,7 +115,7 @@ struct FewRows8Args {
 };
 
 template <typename T, int kSets, int kOuts, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, 4) void few_rows_8bit_kernel(FewRows8Args a, LinearOut<T> out) {
+__global__ __launch_bounds__(64 * kWaves, 4) void few_rows_8bit_kernel(FewRows8Args a, LinearOut<T, false> out) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int kAhead = kOuts * kSets > 2 ? 1 : kSets * kOuts > 1 ? 2 : 4;      // stages of 128 columns that are asked for together
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), chunk = lane / 16;

@@ -140,7 +140,7 @@ extern "C" int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int t
         launch<T, false, true, true>(at.up, args, out, on);
         if (x_values) launch_quantise<T>(DGSP_INT8, rows, width, static_cast<const T*>(x), ldx, rows8(x_values, rows, width, ldv, x_scales), on);
         if (out.partial)
-            linear_join_kernel<T><<<(unsigned)std::min<int64_t>(ceil_div(rows * ceil_div(out_width, 4), 256), 4096), 256, 0, on>>>(rows, out_width, at.up.splits, out);
+            linear_join_kernel<<<(unsigned)std::min<int64_t>(ceil_div(rows * ceil_div(out_width, 4), 256), 4096), 256, 0, on>>>(rows, out_width, at.up.splits, out);
         return launched();
     });
 }

@@ -55,7 +55,7 @@ extern "C" int dgsp_linear_8bit(int64_t rows, int64_t width, int64_t out_width, 
     if (few_rows(rows, width, out_width, 1))
         return with_type(type, [&](auto element) {
             using T = decltype(element);
-            const LinearOut<T> out = linear_out<T>(y, ldy, bias, bias_type != type, residual, ldr, activation, nullptr, nullptr, out_width, nullptr);
+            const LinearOut<T, false> out = linear_out<T, false>(y, ldy, bias, bias_type != type, residual, ldr, activation, nullptr, nullptr, out_width, nullptr);
             const FewRows8Args args{rows, rows8_bytes(width), out_width, static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(weight), rows == 1 ? 0 : ldx,
                                     out_width == 1 ? 0 : ldw, scales};
             with_few_rows(rows, out_width, true, [&](auto sets, auto outs, auto waves) {
@@ -72,11 +72,11 @@ extern "C" int dgsp_linear_8bit(int64_t rows, int64_t width, int64_t out_width, 
         ProductArgs<Pair8> args = product_args<Pair8>(c, rows, out_width, rows8_bytes(width) / 2, 1);
         args.a[0] = source8(x, rows, width, ldx);
         args.b[0] = source8(weight, out_width, width, ldw);
-        const LinearOut<T> out = linear_out<T>(y, ldy, bias, bias_type != type, residual, ldr, activation, nullptr, nullptr, out_width,
+        const LinearOut<T, false> out = linear_out<T, false>(y, ldy, bias, bias_type != type, residual, ldr, activation, nullptr, nullptr, out_width,
                                                c.splits > 1 ? workspace : nullptr);
         launch8(c, args, scales, out, on);
         if (out.partial)
-            linear_join_kernel<T><<<(unsigned)std::min<int64_t>(ceil_div(rows * ceil_div(out_width, 4), 256), 4096), 256, 0, on>>>(rows, out_width, c.splits, out);
+            linear_join_kernel<<<(unsigned)std::min<int64_t>(ceil_div(rows * ceil_div(out_width, 4), 256), 4096), 256, 0, on>>>(rows, out_width, c.splits, out);
         return launched();
     });
 }

@@ -6,11 +6,11 @@
 
 namespace dgsp {
 
-template <typename T>
-LinearOut<T> linear_out(void* y, int64_t ldy, const void* bias, bool wide, const void* residual, int64_t ldr, int activation, void* z, void* codes, int64_t out_width,
+template <typename T, bool kKeeps = true>
+LinearOut<T, kKeeps> linear_out(void* y, int64_t ldy, const void* bias, bool wide, const void* residual, int64_t ldr, int activation, void* z, void* codes, int64_t out_width,
                         void* partial) {
     const auto four = [](const void* p, int64_t ld, int64_t size) { return ld % 4 == 0 && aligned(p, 4 * size); };
-    LinearOut<T> out{};
+    LinearOut<T, kKeeps> out{};
     out.y = static_cast<T*>(y);
     out.ldy = ldy;
     out.vectors = four(y, ldy, sizeof(T));

@@ -10,6 +10,7 @@
 #pragma once
 
 #include "product_kernels.hpp"
+#include "rows8.hpp"
 
 namespace dgsp {
 
@@ -29,6 +30,25 @@ __device__ __forceinline__ void activate_only(int kind, const float (&z)[kCount]
 
 // A NaN has a code of its own, below all slopes.
 __device__ __forceinline__ uint32_t slope_code(float slope) { return slope == slope ? (uint32_t)(int)rintf(slope * kSlopeSteps) & 0xffu : 0x80u; }
+
+// the codes of groups of four, together where none is NaN
+template <int kCount>
+__device__ __forceinline__ void slope_words(const float (&slope)[4 * kCount], uint32_t (&words)[kCount]) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kCount; ++j) {
+        words[j] = whole_word({slope[4 * j], slope[4 * j + 1], slope[4 * j + 2], slope[4 * j + 3]}, kSlopeSteps);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += slope[4 * j + r];
+    }
+    if (__builtin_amdgcn_ballot_w64(sum != sum) == 0) return;
+#pragma unroll
+    for (int j = 0; j < kCount; ++j) {
+        words[j] = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) words[j] |= slope_code(slope[4 * j + r]) << (8 * r);
+    }
+}
 
 // of eight codes the j-th
 __device__ __forceinline__ float slope_of(uint2 codes, int j) {
@@ -68,7 +88,8 @@ __device__ __forceinline__ f32x4 load4(const T* p, bool vectors, int here) {
     return v;
 }
 
-template <typename T>
+// kKeeps: may something be left for a backward pass?  What cannot be is not compiled: the kernels in 8 bits have no registers to spare.
+template <typename T, bool kKeeps = true>
 struct LinearOut {
     static constexpr bool kReadLate = true;
     T* y;
@@ -94,26 +115,24 @@ struct LinearOut {
     __device__ __forceinline__ void finish(int64_t m, int64_t n, int left, const float (&in)[4 * kCount], const f32x4 (&add)[kCount]) const {
         using T4 = T __attribute__((ext_vector_type(4)));
         float value[4 * kCount];
-        if (codes) {
+        if (kKeeps && codes) {
             float slope[4 * kCount];
-            activate<sizeof(T) == 4>(activation, in, value, slope);
+            uint32_t words[kCount];
+            activate<sizeof(T) == 4, true>(activation, in, value, slope);
+            slope_words(slope, words);
             uint8_t* to = codes + m * kept_ld + n;
 #pragma unroll
-            for (int j = 0; j < kCount; ++j) {
-                uint32_t word = 0;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) word |= slope_code(slope[4 * j + r]) << (8 * r);
-                if (kWhole || left > kStep * j) *reinterpret_cast<uint32_t*>(to + kStep * j) = word;
-            }
+            for (int j = 0; j < kCount; ++j)
+                if (kWhole || left > kStep * j) *reinterpret_cast<uint32_t*>(to + kStep * j) = words[j];
         } else {
             activate_only<sizeof(T) == 4>(activation, in, value);
         }
-        if (z && wide) {
+        if (kKeeps && z && wide) {
             float* to = static_cast<float*>(z) + m * kept_ld + n;
 #pragma unroll
             for (int j = 0; j < kCount; ++j)
                 if (kWhole || left > kStep * j) *reinterpret_cast<f32x4*>(to + kStep * j) = f32x4{in[4 * j], in[4 * j + 1], in[4 * j + 2], in[4 * j + 3]};
-        } else if (z) {
+        } else if (kKeeps && z) {
             T* to = static_cast<T*>(z) + m * kept_ld + n;
 #pragma unroll
             for (int j = 0; j < kCount; ++j)
@@ -196,8 +215,8 @@ struct LinearOut {
 };
 
 // The sum of the splits, in order, and the epilogue.
-template <typename T>
-__global__ __launch_bounds__(256) void linear_join_kernel(int64_t m, int64_t n, int splits, LinearOut<T> out) {
+template <typename T, bool kKeeps>
+__global__ __launch_bounds__(256) void linear_join_kernel(int64_t m, int64_t n, int splits, LinearOut<T, kKeeps> out) {
     const int64_t quads = (n + 3) / 4, count = m * quads, step = (int64_t)gridDim.x * blockDim.x;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < count; i += step) {
         const int64_t row = i / quads, col = (i - row * quads) * 4;

@@ -135,18 +135,30 @@ __device__ __forceinline__ uint2 vertex_bytes(const RawChunk<E>& raw, ScaleRange
     return bytes;
 }
 
-// slope_code() of eight, together where none is NaN
+// slope_words() of eight neighbours
 __device__ __forceinline__ uint2 slope_bytes(const float (&slope)[kChunk]) {
-    uint2 bytes = whole_bytes(slope, kSlopeSteps, false);
-    float sum = 0.0f;
+    uint32_t words[2];
+    slope_words(slope, words);
+    return {words[0], words[1]};
+}
+
+// Value and derivative, the one at an infinity as well, in kPieces, one after the other: together eight of them take more registers than the widest rows leave.
+template <int kPieces, bool kFloat>
+__device__ __forceinline__ void activate_in(int kind, const float (&z)[kChunk], float (&value)[kChunk], float (&slope)[kChunk]) {
+    constexpr int kEach = kChunk / kPieces;
 #pragma unroll
-    for (int j = 0; j < kChunk; ++j) sum += slope[j];
-    if (__builtin_amdgcn_ballot_w64(sum != sum) != 0) {
-        bytes = {0u, 0u};
+    for (int p = 0; p < kPieces; ++p) {
+        float in[kEach], v[kEach], s[kEach];
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) (j < 4 ? bytes.x : bytes.y) |= slope_code(slope[j]) << (8 * (j % 4));
+        for (int j = 0; j < kEach; ++j) in[j] = z[p * kEach + j];
+        activate<kFloat, true>(kind, in, v, s);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            value[p * kEach + j] = v[j];
+            slope[p * kEach + j] = s[j];
+        }
+        if constexpr (kPieces > 1) __builtin_amdgcn_sched_barrier(0);
     }
-    return bytes;
 }
 
 // A lane's eight elements of a row at `col`.  Where rows are whole, rows that are not there are read as the first one, and what comes of them is
@@ -229,7 +241,7 @@ __global__ __launch_bounds__(256, (kP * kO * kPlanes<E> > 64 * 64 ? 3 : 4)) void
             const bool store = inside && here > 0;
             if (a.codes) {
                 float slope[kChunk];
-                activate<kFloat>(a.activation, z, value, slope);
+                activate_in<(kFloat && !kWhole && kP * kO > 64 * 64 && kP > kO ? 4 : 1), kFloat>(a.activation, z, value, slope);
                 const uint2 bytes = slope_bytes(slope);
                 if (store) *reinterpret_cast<uint2*>(a.codes + row * a.kept_ld + col) = bytes;
             } else {

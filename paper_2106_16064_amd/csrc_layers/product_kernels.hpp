@@ -12,8 +12,9 @@ namespace dgsp {
 // (one unit in the last place of float each; the argument of the exponential is off by g 2^-24), and erf to 1.5e-7 (Abramowitz, Stegun,
 // Handbook of Mathematical Functions, 7.1.26), which is what 1 + erf(z) keeps of it in float anyway.  A third of the instructions of
 // the library's functions, which took longer than the products where the depth is small.  kFloat: results are float, and the rounding of
-// the sigmoid's argument is made up for; the sigmoid counts as 0 from -87.3 on below, where silu is less than 1.1e-36.
-template <bool kFloat, int kCount>
+// the sigmoid's argument is made up for; the sigmoid counts as 0 from -87.3 on below, where silu is less than 1.1e-36.  kInfinite: the
+// derivative at an infinity is that of the largest number, 1 or 0, and not 0 times the infinity.
+template <bool kFloat, bool kInfinite = false, int kCount>
 __device__ __forceinline__ void activate(int kind, const float (&g)[kCount], float (&value)[kCount], float (&slope)[kCount]) {
     if (kind == DGSP_ACT_RELU) {
 #pragma unroll
@@ -34,7 +35,7 @@ __device__ __forceinline__ void activate(int kind, const float (&g)[kCount], flo
                 s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g[i]));
             }
             value[i] = g[i] * s;
-            slope[i] = s + value[i] * (1.0f - s);
+            slope[i] = s + (kInfinite && fabsf(g[i]) == __builtin_inff() ? 0.0f : value[i]) * (1.0f - s);
         }
     } else {
 #pragma unroll
@@ -44,7 +45,7 @@ __device__ __forceinline__ void activate(int kind, const float (&g)[kCount], flo
             const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
             const float c = g[i] < 0.0f ? tail : 1.0f - tail;
             value[i] = g[i] * c;
-            slope[i] = c + g[i] * e * 0.39894228f;
+            slope[i] = c + (kInfinite ? __builtin_amdgcn_fmed3f(g[i], -3.40282347e38f, 3.40282347e38f) : g[i]) * e * 0.39894228f;     // c keeps a NaN
         }
     }
 }

@@ -53,22 +53,30 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax, ScaleRange range) 
     return amax == 0 ? 127u : (uint32_t)min(max(exponent - (kE4m3 ? 8 : 6) + up, range.least), range.most);
 }
 
-// Eight numbers times `inverse` as whole numbers in a byte each, to nearest even.  Adding 1.5 * 2^23 in the same step rounds to whole numbers, which are
-// then the lowest byte.  `cut`: some may lie beyond 127 (a scale at the end of its range).
+// four numbers as floats whose lowest byte they are -> the bytes
+__device__ __forceinline__ uint32_t lowest_bytes(const uint32_t (&bits)[4]) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(bits[3], bits[2], 0x0c0c0400u), __builtin_amdgcn_perm(bits[1], bits[0], 0x0c0c0400u), 0x05040100u);
+}
+
+// Four numbers times `factor` as whole numbers in a byte each, to nearest even.  Adding 1.5 * 2^23 in the same step rounds to whole numbers, which are
+// then the lowest byte.
+__device__ __forceinline__ uint32_t whole_word(const float (&v)[4], float factor) {
+    uint32_t bits[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) bits[j] = __builtin_bit_cast(uint32_t, fmaf(v[j], factor, 12582912.0f));
+    return lowest_bytes(bits);
+}
+
+// Eight of them; `cut`: some may lie beyond 127 (a scale at the end of its range).
 __device__ __forceinline__ uint2 whole_bytes(const float (&v)[kChunk], float inverse, bool cut) {
-    uint32_t bits[kChunk];
-    if (cut) {
-#pragma unroll
-        for (int j = 0; j < kChunk; ++j) bits[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(rintf(v[j] * inverse), -127.0f, 127.0f) + 12582912.0f);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kChunk; ++j) bits[j] = __builtin_bit_cast(uint32_t, fmaf(v[j], inverse, 12582912.0f));
-    }
+    if (!cut) return {whole_word({v[0], v[1], v[2], v[3]}, inverse), whole_word({v[4], v[5], v[6], v[7]}, inverse)};
     uint32_t out[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        const uint32_t low = __builtin_amdgcn_perm(bits[4 * q + 1], bits[4 * q], 0x0c0c0400u), high = __builtin_amdgcn_perm(bits[4 * q + 3], bits[4 * q + 2], 0x0c0c0400u);
-        out[q] = __builtin_amdgcn_perm(high, low, 0x05040100u);
+        uint32_t bits[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) bits[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(rintf(v[4 * q + j] * inverse), -127.0f, 127.0f) + 12582912.0f);
+        out[q] = lowest_bytes(bits);
     }
     return {out[0], out[1]};
 }

@@ -443,3 +443,29 @@ def test_sizes_without_a_gpu():
         layers.linear(x, x)
     with pytest.raises(dg.DgspError, match="silu, gelu, relu"):
         layers.linear(x, x, activation="tanh")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS[1:])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,width,out", [(70, 64, 72), (70, 64, 64), (70, 200, 300), (9, 520, 40), (300, 2048, 260)])
+def test_infinite_z_has_the_slope_of_a_number_far_from_zero(rows, width, out, dtype, kind):
+    """1 or 0, whichever form is kept.  Of -1, 0 and 1, so that the columns that are not infinite have exact sums: the two forms keep the same x."""
+    print("[case] infinite z", rows, width, out, dtype, kind, flush=True)
+    x, w, dy = (torch.randint(-1, 2, shape, generator=gen(130 + i)).to(dtype).cuda() for i, shape in enumerate([(rows, width), (out, width), (rows, out)]))
+    b = torch.zeros(out)
+    b[1], b[5], b[out - 1], b[out - 2] = float("inf"), float("-inf"), float("inf"), float("-inf")
+    found = []
+    for params in (dtype, torch.float32):
+        for keep in (False, True):
+            leaves = [t.clone().requires_grad_(True) for t in (x, w, b.to(params).cuda())]
+            y = layers.linear(*leaves, kind, keep_8bit=keep)
+            found.append([g.detach() for g in torch.autograd.grad(y, leaves, dy)])
+        saved = layers.native().linear_forward(x, w, b.to(params).cuda(), layers._epilogue(kind), None, True)[1]
+        codes = saved.view(torch.int8).view(rows, -1)[:, :out]
+        assert (codes[:, [1, out - 1]] == 112).all() and (codes[:, [5, out - 2]] == 0).all()
+    for dx, dw, db in found:
+        assert torch.isfinite(dx).all() and torch.isfinite(dw).all() and torch.isfinite(db).all()
+        for column, slope in ((1, 1), (5, 0), (out - 1, 1), (out - 2, 0)):
+            assert torch.equal(dw[column], (slope * dy[:, column].double() @ x.double()).to(dtype))
+            assert float(db[column]) == slope * float(dy[:, column].double().sum())
