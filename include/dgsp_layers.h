@@ -129,6 +129,7 @@ int64_t dgsp_gated_ff_backward_workspace_bytes(int64_t rows, int64_t width, int6
 /*
  * Root-mean-square norm over the rows of s, where s = x, or s = residual + dropout(x) if residual is not NULL:
  *     y = s / sqrt(mean(s^2) + eps) * weight
+ * Any finite s has its norm: squares that 32 bits cannot hold are summed in 64.
  *   rstd   a float a row, 1 / sqrt(mean(s^2) + eps), for the backward pass; NULL: not wanted
  * The other arguments and the limits are those of dgsp_layer_norm.
  */

@@ -29,9 +29,12 @@ struct RmsArgs {
 
 constexpr ScaleRange kE4m3Range{1, 246};
 
-// What the sum, the root and the products are made in.  Before a rounding to 8 bits 64 bits: an error of y is a hundred times as likely as its own size to
+// The squares of a row held in registers, their sum and the root are made in 64 bits: the squares of numbers from 2^64 on, and of those below 2^-75, have no place in
+// 32.  Memory bounds the kernels either way (2^20 rows of 32 floats 41.5 us both, 8192 rows of 8192 bfloat16 44 in 32 bits and 45.5; with a second sum only where
+// the one in 32 bits says that it is needed 43 and 45).
+
+// What the products of s, the root and the weight are made in.  Before a rounding to 8 bits 64 bits: an error of y is a hundred times as likely as its own size to
 // carry an element across a border between two steps (of 4099 x 1001 in 32 bits two or three; rounded from 64 to 32 in between, one).
-// Memory bounds the kernel either way.
 template <bool k8bit>
 using Wide = std::conditional_t<k8bit, double, float>;
 
@@ -44,16 +47,10 @@ __device__ __forceinline__ float narrowed(double v) {
     return (float)__builtin_bit_cast(double, (bits & ~0xffffffffull) | odd);
 }
 
-// 1 / sqrt(mean + eps); `part`: 1 / width.  In 64 bits by the hardware's first guess, good to 2^-24 or better, and a step of Newton's, which squares its error.
-template <bool k8bit>
-__device__ __forceinline__ Wide<k8bit> reciprocal_root(Wide<k8bit> squares, Wide<k8bit> part, float eps) {
-    const Wide<k8bit> mean = squares * part + eps;
-    if constexpr (k8bit) {
-        const double guess = __builtin_amdgcn_rsq(mean), better = guess + 0.5 * guess * fma(-mean * guess, guess, 1.0);
-        return guess > 0.0 && guess < __builtin_inf() ? better : guess;
-    } else {
-        return 1.0f / sqrtf(mean);
-    }
+// 1 / sqrt(mean + eps); `part`: 1 / width.  By the hardware's first guess, good to 2^-24 or better, and a step of Newton's, which squares its error.
+__device__ __forceinline__ double reciprocal_root(double squares, double part, float eps) {
+    const double mean = squares * part + eps, guess = __builtin_amdgcn_rsq(mean), better = guess + 0.5 * guess * fma(-mean * guess, guess, 1.0);
+    return guess > 0.0 && guess < __builtin_inf() ? better : guess;
 }
 
 template <typename T, bool kWhole, bool kAdd, bool k8bit>
@@ -70,14 +67,14 @@ __global__ __launch_bounds__(kWhole ? 1024 : 256) void rms_norm_kernel(RmsArgs<T
     };
     ask(team.row);
     if (here > 0) load_params<T>(a.weight, a.wide, col, here, 1.0f, w);
-    const Wide<k8bit> part = Wide<k8bit>(1) / (Wide<k8bit>)a.width;
+    const double part = 1.0 / (double)a.width;
     int turn = 0;
     // all teams of a workgroup make the same number of turns
     const int64_t base = team.row - (kWhole ? 0 : threadIdx.x / team.lanes);
     for (int64_t at = base, row = team.row; at < a.rows; at += team.step, row += team.step) {
         const bool inside = row < a.rows && here > 0;
         float s[kChunk];
-        Wide<k8bit> squares[1] = {0};
+        double squares[1] = {0.0};
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) s[j] = 0.0f;
         if (inside) {
@@ -92,9 +89,9 @@ __global__ __launch_bounds__(kWhole ? 1024 : 256) void rms_norm_kernel(RmsArgs<T
         }
         ask(row + team.step);
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) squares[0] += (Wide<k8bit>)s[j] * (Wide<k8bit>)s[j];
+        for (int j = 0; j < kChunk; ++j) squares[0] += (double)s[j] * (double)s[j];
         team.sum(squares, turn);
-        const Wide<k8bit> rstd = reciprocal_root<k8bit>(squares[0], part, a.eps);
+        const auto rstd = (Wide<k8bit>)reciprocal_root(squares[0], part, a.eps);
         float out[kChunk];
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) out[j] = inside && j < here ? narrowed(s[j] * rstd * w[j]) : 0.0f;
@@ -223,13 +220,18 @@ __global__ __launch_bounds__(kWhole ? 1024 : 256) void rms_norm_backward_kernel(
 
 // ---------------------------------------------------------------- rows beyond what registers hold
 
-// One workgroup a row, which it reads twice.
+// Squares in 32 bits have lost some: at the upper end, or, where eps does not outweigh it, below 2^-90, where steps of 2^-149 for each of up to 2^31 elements
+// are no longer small beside the sum.
+__device__ __forceinline__ bool beyond_32_bits(float squares, float eps) { return !(squares < __builtin_inff()) || (squares < 0x1p-90f && eps < 0x1p-60f); }
+
+// One workgroup a row, which it reads twice.  Not into 8 bits the squares are held in 32, and made again where that says so (4096 x 16384 bfloat16 65 us;
+// held in 64 at all times 69, in 32 alone 63).
 template <typename T, bool k8bit>
 __global__ __launch_bounds__(1024) void rms_norm_long_kernel(RmsArgs<T> a) {
     const uint64_t offset = a.mask.device_offset ? *a.mask.device_offset : a.mask.offset;
     const Team<true> team(1024);
     int turn = 0;
-    const Wide<k8bit> part = Wide<k8bit>(1) / (Wide<k8bit>)a.width;
+    const double part = 1.0 / (double)a.width;
     const int64_t chunks = k8bit ? (a.rows8.blocks + 3) / 4 * 4 * kBlockLanes : (a.width + kChunk - 1) / kChunk;
     for (int64_t row = team.row; row < a.rows; row += team.step) {
         auto at = [&](int64_t chunk, float (&v)[kChunk]) {
@@ -248,7 +250,18 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(RmsArgs<T> a) {
             for (int j = 0; j < kChunk; ++j) squares[0] += c * kChunk + j < a.width ? (Wide<k8bit>)v[j] * (Wide<k8bit>)v[j] : Wide<k8bit>(0);
         }
         team.sum(squares, turn);
-        const Wide<k8bit> rstd = reciprocal_root<k8bit>(squares[0], part, a.eps);
+        Wide<k8bit> rstd = (Wide<k8bit>)reciprocal_root(squares[0], part, a.eps);
+        if constexpr (!k8bit) {
+            if (__builtin_amdgcn_ballot_w64(beyond_32_bits(squares[0], a.eps)) != 0) {          // all waves see the same sum
+                double again[1] = {0.0};
+                for (int64_t c = threadIdx.x; c * kChunk < a.width; c += blockDim.x) {
+                    at(c, v);
+                    for (int j = 0; j < kChunk; ++j) again[0] += c * kChunk + j < a.width ? (double)v[j] * (double)v[j] : 0.0;
+                }
+                team.sum(again, turn);
+                rstd = (float)reciprocal_root(again[0], part, a.eps);
+            }
+        }
         for (int64_t c = threadIdx.x; c < chunks; c += blockDim.x) {
             const int64_t col = c * kChunk, here = a.width - col;
             float w[kChunk], out[kChunk];

@@ -411,3 +411,24 @@ def test_sums_in_8_bits_are_rounded_once(rows, width, dtype):
     values, exponents = ref8.quantised(definition(S.double(), torch.zeros_like(S, dtype=torch.float64), host(w), EPS)[0], "e4m3")
     scale = y8.scales.cpu().transpose(0, 1).reshape(rows, -1)[:, :exponents.shape[1]].long() - 127
     assert torch.equal(y8.values.cpu().double().view(values.shape), values) and torch.equal(scale, exponents.long())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("width", [3, 32, 300, 1001, 8200])
+def test_rows_whose_squares_32_bits_cannot_hold(width, dtype, monkeypatch):
+    """Large and small rows without eps: what counts is the sum of the squares, which passes 2^128 or ends below 2^-149.  Gradients of the largest row,
+    some 1e-37 times differences of numbers near 1, may end below 2^-126, where steps stay as they are: 2^-149 in 32 bits, which the result is made in,
+    and 2^-133 in bfloat16, half of which each rounding may take."""
+    print("[case] range", width, dtype, flush=True)
+    monkeypatch.setitem(TINY, dtype, 2.0 ** -150 + (2.0 ** -134 if dtype == torch.bfloat16 else 0.0))
+    size = torch.tensor([1e25, 1e18, 1e37, 1.0, 1e-19, 1e-25, 1e-35], dtype=torch.float64)[:, None]
+    x, r = ((normal((7, width), torch.float64, 90 + i) * size).to(dtype) for i in range(2))
+    w, dy = normal((width,), dtype, 92, 0.2, 1.0), normal((7, width), dtype, 93)
+    ds = (normal((7, width), torch.float64, 94) / size).to(dtype)
+    check(x, None, w, dy, None, eps=0.0)
+    check(x, r, w, dy, ds, eps=0.0)
+    check(x, r, None, dy, ds, 0.25, eps=1e-30)
+    with torch.no_grad():
+        want = layers.rms_norm(x.cuda(), w.cuda(), 0.0)
+        assert torch.isfinite(want).all() and (want != 0).any(1).all()
