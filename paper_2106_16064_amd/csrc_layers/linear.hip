@@ -79,7 +79,7 @@ extern "C" int64_t dgsp_linear_workspace_bytes(int64_t rows, int64_t width, int6
 
 extern "C" int64_t dgsp_linear_backward_workspace_bytes(int64_t rows, int64_t width, int64_t out_width, int type, int activation, int keep) {
     if (!linear_extents(rows, width, out_width, type) || !known_epilogue(activation) || !known_keep(keep)) return 0;
-    if (narrow_linear_fits(width, out_width, type)) return narrow_linear_backward_bytes(rows, width, out_width, type);
+    if (narrow_linear_fits(width, out_width, type)) return narrow_linear_backward_bytes(rows, width, out_width, type, keep == DGSP_KEEP_8BIT);
     Pieces pieces(nullptr);
     BackwardPieces need(pieces, rows, width, out_width, type, activation, keep);
     return pieces.used();
@@ -168,7 +168,7 @@ extern "C" int dgsp_linear_backward(int64_t rows, int64_t width, int64_t out_wid
                                               what == kCodes ? static_cast<const uint8_t*>(saved) : nullptr, padded(out_width, 8),
                                               in_8bit && dweight ? rows8(const_cast<void*>(x), rows, width, ldx, const_cast<void*>(x_scales)) : Rows8{},
                                               static_cast<T*>(dx), nullptr, nullptr},
-                                             dweight, dbias, bias_type != type, workspace, static_cast<hipStream_t>(stream));
+                                             in_8bit, dweight, dbias, bias_type != type, workspace, static_cast<hipStream_t>(stream));
         });
     }
     Pieces pieces(workspace);

@@ -39,17 +39,19 @@ void with_widths(int64_t width, int64_t out_width, F&& f) {
     });
 }
 
-// Of the backward pass: workgroups, as many as are resident together, and the sums that each leaves.
+// Of the backward pass: workgroups, as many as are resident together, and the sums that each leaves.  `in_8bit`: x was kept so.
 struct Backward {
     int64_t groups = 1, parts = 1;
     template <typename E>
-    static Backward of(int64_t rows, int64_t width, int64_t out_width) {
+    static Backward of(int64_t rows, int64_t width, int64_t out_width, bool in_8bit) {
         Backward b;
         with_widths<E>(width, out_width, [&](auto p, auto o) {
-            using Share = NarrowShare<E, decltype(p)::value, decltype(o)::value>;
-            const int64_t a_cu = std::min<int64_t>(2, 163840 / (Share::kLds + 4096));
-            b.groups = std::max<int64_t>(1, std::min(ceil_div(rows, Share::kTile), kCus * a_cu));
-            b.parts = Share::kParts;
+            constexpr int kP = decltype(p)::value, kO = decltype(o)::value;
+            with_flags(in_8bit, width == kP && out_width == kO, [&](auto x8, auto whole) {
+                using Share = NarrowShare<E, kP, kO, decltype(x8)::value, decltype(whole)::value>;
+                b.groups = std::max<int64_t>(1, std::min(ceil_div(rows, Share::kTile), kCus * Share::kGroups));
+                b.parts = Share::kParts;
+            });
         });
         return b;
     }
@@ -71,14 +73,14 @@ int narrow_linear(const NarrowLinearArgs<E>& args, hipStream_t stream) {
     return launched();
 }
 
-int64_t narrow_linear_backward_bytes(int64_t rows, int64_t width, int64_t out_width, int type) {
-    const Backward b = type == DGSP_F32 ? Backward::of<float>(rows, width, out_width) : Backward::of<bf16_t>(rows, width, out_width);
+int64_t narrow_linear_backward_bytes(int64_t rows, int64_t width, int64_t out_width, int type, bool in_8bit) {
+    const Backward b = type == DGSP_F32 ? Backward::of<float>(rows, width, out_width, in_8bit) : Backward::of<bf16_t>(rows, width, out_width, in_8bit);
     return b.groups * (b.parts * out_width * width + out_width) * 4;
 }
 
 template <typename E>
-int narrow_linear_backward(NarrowLinearBackwardArgs<E> args, void* dweight, void* dbias, bool wide, void* workspace, hipStream_t stream) {
-    const Backward b = Backward::of<E>(args.rows, args.width, args.out_width);
+int narrow_linear_backward(NarrowLinearBackwardArgs<E> args, bool in_8bit, void* dweight, void* dbias, bool wide, void* workspace, hipStream_t stream) {
+    const Backward b = Backward::of<E>(args.rows, args.width, args.out_width, in_8bit);
     float* const sums = static_cast<float*>(workspace);
     args.weight_sums = dweight ? sums : nullptr;
     args.bias_sums = dbias ? sums + b.groups * b.parts * args.out_width * args.width : nullptr;
@@ -87,7 +89,7 @@ int narrow_linear_backward(NarrowLinearBackwardArgs<E> args, void* dweight, void
             constexpr int kP = decltype(p)::value, kO = decltype(o)::value;
             with_flags(args.x8.values != nullptr, args.width == kP && args.out_width == kO, [&](auto x8, auto whole) {
                 constexpr bool kX8 = decltype(x8)::value, kWhole = decltype(whole)::value;
-                const dim3 groups((unsigned)b.groups), threads(64 * NarrowShare<E, kP, kO>::kWaves);
+                const dim3 groups((unsigned)b.groups), threads(64 * NarrowShare<E, kP, kO, kX8, kWhole>::kWaves);
                 if constexpr (sizeof(E) == 2 && !kX8)
                     if (args.wide && args.z) return narrow_linear_backward_kernel<E, kP, kO, kX8, kWhole, float><<<groups, threads, 0, stream>>>(args);
                 narrow_linear_backward_kernel<E, kP, kO, kX8, kWhole, E><<<groups, threads, 0, stream>>>(args);
@@ -100,7 +102,7 @@ int narrow_linear_backward(NarrowLinearBackwardArgs<E> args, void* dweight, void
 
 #define NARROW(E)                                                            \
     template int narrow_linear<E>(const NarrowLinearArgs<E>&, hipStream_t); \
-    template int narrow_linear_backward<E>(NarrowLinearBackwardArgs<E>, void*, void*, bool, void*, hipStream_t);
+    template int narrow_linear_backward<E>(NarrowLinearBackwardArgs<E>, bool, void*, void*, bool, void*, hipStream_t);
 NARROW(float)
 NARROW(bf16_t)
 NARROW(f16_t)

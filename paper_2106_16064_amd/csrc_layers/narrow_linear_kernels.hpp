@@ -282,26 +282,29 @@ struct NarrowLinearBackwardArgs {
 };
 
 // How the waves share the weight's gradient: kDown x kAcross of them have a block each, of kParts parts of the vertices.  Of float rows
-// wider than 32 a workgroup has half as many vertices, so that two find room in LDS.
-template <typename E, int kP, int kO>
+// wider than 32 a workgroup has half as many vertices, so that two find room in LDS.  kGroups: workgroups that a CU has room for, which is what LDS and, of the eight
+// waves of 16-bit rows, registers leave; the compiler is told.  With one of two left out (2^20 rows 64 -> 64 float, kept in 8 bits) the gradient takes
+// 175 us in place of 150; with one too many, which waits for its turn, (2^20 rows 64 -> 128 bfloat16) 232 in place of 223.
+template <typename E, int kP, int kO, bool kX8, bool kWhole>
 struct NarrowShare {
     static constexpr int kWaves = sizeof(E) == 4 && kP * kO > 32 * 32 ? 4 : 8, kTile = 16 * kWaves;          // kTile vertices of a workgroup
-    static constexpr int kWavesASimd = sizeof(E) == 4 && (kP > 64 || kO > 64) ? 1 : 2;
     static constexpr int kDown = 2, kAcross = kP / 16 < kWaves / 2 ? kP / 16 : kWaves / 2, kParts = kWaves / (kDown * kAcross);
     static constexpr int kFragsO = kO / 16 / kDown, kFragsP = kP / 16 / kAcross;
     static constexpr int kLdO = kO + 8, kLdP = kP + 8;                  // rows of LDS start in different banks
-    static constexpr int kLds = kPlanes<E> * (2 * kO * kP + 2 * kTile * (kLdO + kLdP));
+    static constexpr int kXParts = kX8 ? 1 : kPlanes<E>;                // whole numbers are exact in bf16
+    static constexpr int kLds = kPlanes<E> * 2 * kO * kP + 2 * kTile * (kPlanes<E> * kLdO + kXParts * kLdP) + 4 * kWaves * kO;
+    static constexpr int kGroups = 2 * kLds <= 163840 && (sizeof(E) == 4 || (kO <= 64 && kP * kO <= (kWhole || kO < 64 ? 64 * 64 : 32 * 64))) ? 2 : 1;
 };
 
 // dz stays in registers as an operand for dx; for the weight's gradient, a sum over the vertices, dz and x pass through LDS, which hands them out by
 // columns.  Sums over the vertices stay in registers until the end; the workgroups' are added in their order (column_sums.hpp).
 // Z: the type that z was kept in
 template <typename E, int kP, int kO, bool kX8, bool kWhole, typename Z>
-__global__ __launch_bounds__((64 * NarrowShare<E, kP, kO>::kWaves), (NarrowShare<E, kP, kO>::kWavesASimd)) void narrow_linear_backward_kernel(NarrowLinearBackwardArgs<E> a) {
+__global__ __launch_bounds__((64 * NarrowShare<E, kP, kO, kX8, kWhole>::kWaves), (NarrowShare<E, kP, kO, kX8, kWhole>::kGroups * NarrowShare<E, kP, kO, kX8, kWhole>::kWaves / 4)) void narrow_linear_backward_kernel(NarrowLinearBackwardArgs<E> a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    using Share = NarrowShare<E, kP, kO>;
+    using Share = NarrowShare<E, kP, kO, kX8, kWhole>;
     constexpr int kNarrowWaves = Share::kWaves, kNarrowTile = Share::kTile;
-    constexpr int kU = kP / 32, kT = kO / 32, kFragments = 2 * kT * kU, kParts = kPlanes<E>, kXParts = kX8 ? 1 : kParts;    // whole numbers are exact in bf16
+    constexpr int kU = kP / 32, kT = kO / 32, kFragments = 2 * kT * kU, kParts = kPlanes<E>, kXParts = Share::kXParts;
     constexpr bool kFloat = sizeof(E) == 4;
     __shared__ u32x4 weights[kParts][kFragments * 64];                  // by columns: 16 of width, 32 of out_width
     __shared__ uint16_t dz_rows[kParts][kNarrowTile * Share::kLdO], x_rows[kXParts][kNarrowTile * Share::kLdP];

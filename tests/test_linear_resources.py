@@ -5,6 +5,7 @@ import re
 
 import pytest
 
+from paper_2106_16064_amd import layers
 from test_layers_resources import objects, registers, tool  # noqa: F401
 
 
@@ -78,3 +79,38 @@ def test_vector_registers_are_not_spilled(objects, kernel):  # noqa: F811
                 assert int(m[2]) == 0, name
                 count += 1
     assert count >= 2, os.listdir(os.path.dirname(objects[0]))
+
+
+def notes(objects):  # noqa: F811
+    """Of each kernel what its notes say."""
+    found = {}
+    for code in objects:
+        for entry in re.split(r"\n  - ", tool("llvm-readelf", "--notes", code)):
+            name = re.search(r"^ +\.name: +(_Z\S+)", entry, re.M)
+            if name:
+                found[name[1]] = {key: int(value) for key, value in re.findall(r"^ *\.(\w+): +(\d+)$", entry, re.M)}
+    return found
+
+
+def test_as_many_workgroups_of_the_narrow_gradient_as_a_cu_holds(objects):  # noqa: F811
+    """Registers and LDS of each kernel against what the workspace is for: a workgroup too few leaves room that nothing uses, one too many waits for its turn.
+    Types of 16 bits and forms of x and z share a number."""
+    L = layers.lib()
+    fits = {}
+    for name, note in notes(objects).items():
+        m = re.search(r"29narrow_linear_backward_kernelI(f|DF16b|DF16_)Li(\d+)ELi(\d+)ELb(\d)ELb(\d)E", name)
+        if not m:
+            continue
+        wide, width, out, x8, whole = m[1] == "f", int(m[2]), int(m[3]), int(m[4]), int(m[5])
+        waves = note["max_flat_workgroup_size"] // 64
+        room = min(163840 // note["group_segment_fixed_size"], 512 // (-(-note["vgpr_count"] // 8) * 8) * 4 // waves, 2)
+        key = (wide, width, out, x8 if wide else None, whole)
+        fits[key] = min(fits.get(key, 2), room)
+    assert len(fits) == 8 * 4 + 9 * 2                                # 128 x 128 floats take tiles
+    for (wide, width, out, x8, whole), most in fits.items():
+        w, o = (width, out) if whole else (width - 1, out - 1)
+        for keep in (layers.KEEP_WHOLE, layers.KEEP_8BIT) if x8 is None else (layers.KEEP_8BIT,) if x8 else (layers.KEEP_WHOLE,):
+            for number in (layers.F32,) if wide else (layers.BF16, layers.F16):
+                size = L.dgsp_linear_backward_workspace_bytes(1 << 24, w, o, number, layers.GELU, keep)
+                found = [groups for groups in (256, 512) for parts in (1, 2, 4) if size == groups * (parts * o * w + o) * 4]
+                assert found == [256 * most], (wide, width, out, x8, whole)
