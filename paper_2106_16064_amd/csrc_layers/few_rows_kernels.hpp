@@ -166,18 +166,22 @@ __global__ __launch_bounds__(64 * kWaves, 4) void few_rows_8bit_kernel(FewRows8A
 }
 
 // Where one launch without splits of the sum is faster than tiles, which split it and read a row of the weight once for 64 rows of x.  Against it are
-// deep sums of few columns, which few workgroups add up, the deeper the more rows there are, and, from some rows on, weights that are long in
-// coming.  bfloat16, us, this and tiles:
-//     1 row     4096 -> 16384 22 and 25    4096 -> 1024 7.3 and 7.9     8192 -> 4096 15 and 16       8192 -> 256 11.3 and 7.7     16384 -> 512 21 and 12
-//     16 rows   4096 -> 16384 31 and 26    4096 -> 4096 10.4 and 12.6   8192 -> 2048 17 and 13       2048 -> 256 5.9 and 7.1
-//     32 rows   1024 -> 16384 11 and 14    2048 -> 4096 9.0 and 11.2    2048 -> 512 7.9 and 7.2      4096 -> 512 13 and 8
-//     64 rows   512 -> 16384 9.6 and 8.5   1024 -> 8192 9.3 and 14.0    1024 -> 1024 7.2 and 7.6     2048 -> 512 11.4 and 7.5
+// deep sums of few columns, which few workgroups add up, the deeper the more rows there are; from some rows on weights that are long in coming; and short
+// sums of so many columns that its workgroups, each of which waits once for all it reads, take turns.  bfloat16, us, this and tiles, a new weight a call:
+//     1 row     4096 -> 16384 22 and 25    4096 -> 1024 7.3 and 7.9     8192 -> 4096 15 and 16       8192 -> 256 11.3 and 7.7     256 -> 16384 4.8 and 5.8     256 -> 65536 13 and 12     1024 -> 65536 30 and 34
+//     16 rows   4096 -> 16384 31 and 26    4096 -> 4096 10.4 and 12.6   8192 -> 2048 17 and 13       2048 -> 256 5.9 and 7.1      512 -> 20000 9.9 and 8.7    128 -> 65536 15 and 9
+//     24 rows   2048 -> 512 7.1 and 7.2    2048 -> 4096 8.3 and 10.8    4096 -> 512 12 and 8.6       256 -> 20000 6.1 and 6.9     256 -> 32768 9.7 and 7.5
+//     32 rows   1024 -> 16384 14 and 15    2048 -> 4096 9.2 and 11.4    2048 -> 512 7.7 and 7.2      2048 -> 2048 8.8 and 9.0     512 -> 16384 7.7 and 8.2
+//     48 rows   512 -> 16384 8.8 and 8.4   256 -> 16384 6.3 and 6.5     1024 -> 8192 8.6 and 12.9    256 -> 24576 10.4 and 7.4
+//     64 rows   512 -> 16384 9.7 and 8.1   1024 -> 8192 9.3 and 14.0    1024 -> 1024 7.2 and 7.6     2048 -> 512 11.4 and 7.5     512 -> 10240 9.3 and 7.8
 // In 8 bits the same holds of widths twice as large: 1 row 8192 -> 1024 7.6 and 8.1, 16384 -> 512 12 and 9; 64 rows 2048 -> 2048 8.0 and 8.5, 4096 -> 1024 13.5 and 8.6.
+// Of 970 sizes measured the choice costs more than 7 % in 21, the most 4 rows in 8 bits 2048 -> 32768 (22 and 17) and 4 rows 512 -> 16384 (7.5 and 6.2).
 inline bool few_rows(int64_t rows, int64_t width, int64_t out_width, int64_t element_bytes) {
     const int64_t depth = width * element_bytes, weight = depth * out_width;
-    if (rows <= 16) return (out_width >= 4096 || depth * (rows <= 4 ? 1 : 2) < 16384) && (rows <= 8 || weight < (64 << 20));
-    if (rows <= 32) return depth <= 4096 && weight <= (32 << 20);
-    return rows <= kFewRows && depth <= 2048 && weight <= (16 << 20);
+    if (rows <= 16)
+        return (out_width <= 16384 || depth >= 2048) && (out_width >= 4096 || depth * (rows <= 4 ? 1 : 2) < 16384) && (rows <= 8 || weight < (64 << 20));
+    if (rows <= 32) return out_width <= 24576 && depth <= 4096 && weight <= (32 << 20) && (rows * depth <= 24 * 4096 || out_width >= 2048);
+    return rows <= kFewRows && depth <= 2048 && weight <= (16 << 20) && (out_width <= 8192 || (out_width <= 16384 && rows * depth <= 48 * 512));
 }
 
 // launch(sets, outs, waves): how the rows and columns are cut.  Columns beyond 8192 fill the GPU by workgroups of 8 waves; fewer take 16 (one token, bfloat16,

@@ -469,3 +469,25 @@ def test_infinite_z_has_the_slope_of_a_number_far_from_zero(rows, width, out, dt
         for column, slope in ((1, 1), (5, 0), (out - 1, 1), (out - 2, 0)):
             assert torch.equal(dw[column], (slope * dy[:, column].double() @ x.double()).to(dtype))
             assert float(db[column]) == slope * float(dy[:, column].double().sum())
+
+
+# rows, width, out: which of the two is faster by more than the clock's noise, bfloat16 (few_rows_kernels.hpp has the times)
+FASTER_WITHOUT_TILES = [(1, 4096, 16384), (1, 4096, 1024), (16, 4096, 4096), (16, 2048, 256), (24, 2048, 4096), (24, 256, 20000), (32, 2048, 4096), (32, 1024, 16384),
+                        (48, 1024, 8192), (64, 1024, 8192), (64, 1024, 1024), (1, 1024, 65536)]
+FASTER_ON_TILES = [(1, 8192, 256), (1, 128, 65536), (16, 4096, 16384), (16, 512, 20000), (24, 4096, 512), (24, 256, 32768), (32, 2048, 256), (32, 2048, 512), (32, 2048, 1024),
+                   (48, 512, 16384), (48, 256, 24576), (64, 512, 16384), (64, 512, 10240), (64, 2048, 512)]
+
+
+@pytest.mark.parametrize("rows,width,out", FASTER_WITHOUT_TILES + FASTER_ON_TILES)
+def test_few_rows_take_the_kernel_that_is_faster(rows, width, out):
+    """Only tiles have a workspace."""
+    assert (layers.lib().dgsp_linear_workspace_bytes(rows, width, out, layers.BF16) > 0) == ((rows, width, out) in FASTER_ON_TILES)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,width,out", [(1, 130, 40000), (16, 128, 20000), (20, 136, 24580), (24, 2040, 500), (30, 2048, 515), (40, 512, 10240), (64, 264, 16390)])
+def test_few_rows_of_many_columns_and_deep_sums(rows, width, out):
+    print("[case] few", rows, width, out, flush=True)
+    check(inputs(rows, width, out, torch.bfloat16, torch.float32, 500), "gelu", at="cuda")
+    x, w, b, r, dy = inputs(rows, width, out, torch.float16, torch.float16, 510)
+    check((x, w, None, None, dy), None, keep=True, at="cuda")
