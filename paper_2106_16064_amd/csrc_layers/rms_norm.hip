@@ -14,10 +14,15 @@ bool norm_extents(int64_t rows, int64_t width, int type, int param_type) {
 
 template <typename T, bool k8bit>
 void launch_norm(const Hold& hold, const RmsArgs<T>& args, hipStream_t stream) {
-    // As many workgroups as are resident together, which go on to further rows; of hardly more rows than that one for each, so that none has two
-    // where most have one (4099 rows of 1001: 10.9 us with 4096 workgroups).
+    // As many workgroups as 2048 threads a CU are, which go on to further rows that they have asked for before.  Two to four times as many rows with a workgroup
+    // each take longer, but for float with the residual's addition, whose four matrices come from memory.  us, so and with a workgroup a row:
+    //     float16   262144 x 32 9.2 and 10.2      8192 x 1001 10.1 and 10.7, into 8 bits 13.0 and 13.3    4096 x 4096 14.5 and 17.4, into 8 bits 19.2 and 22.2
+    //               with the residual: 16384 x 300 15.9 and 16.5    8192 x 2048 26.8 and 24.6, into 8 bits 25.7 and 29.5    2048 x 8192 26.9 and 35.3
+    //     float     262144 x 32 12.9 and 14.7     8192 x 1001 12.9 and 13.3                               4096 x 4096 26.1 and 26.2, into 8 bits 22.2 and 25.7
+    //               with the residual: 262144 x 32 27.3 and 25.5    8192 x 1001 27.2 and 26.1    4096 x 4096 45.4 and 44.9    2048 x 8192 49 and 52
     const int64_t needed = ceil_div(args.rows, hold.rows_a_group()), resident = kCus * 2048 / hold.threads;
-    const unsigned groups = (unsigned)(needed <= 4 * resident ? needed : resident);
+    const bool four = args.residual && !k8bit && sizeof(T) == 4 && hold.threads <= 512;
+    const unsigned groups = (unsigned)(needed <= (four ? 4 : 1) * resident ? needed : resident);
     if (!hold.fits)
         rms_norm_long_kernel<T, k8bit><<<(unsigned)std::min<int64_t>(args.rows, kCus * 2), 1024, 0, stream>>>(args);
     else if (hold.whole && args.residual)
