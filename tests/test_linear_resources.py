@@ -114,3 +114,21 @@ def test_as_many_workgroups_of_the_narrow_gradient_as_a_cu_holds(objects):  # no
                 size = L.dgsp_linear_backward_workspace_bytes(1 << 24, w, o, number, layers.GELU, keep)
                 found = [groups for groups in (256, 512) for parts in (1, 2, 4) if size == groups * (parts * o * w + o) * 4]
                 assert found == [256 * most], (wide, width, out, x8, whole)
+
+
+# Where a row's ends are looked at one by one, or a row is read twice, comparisons and addresses are more than the scalar registers hold: so many at most go to
+# lanes of vector registers.
+SCALARS = {"rms_norm_kernel": 26, "rms_norm_backward_kernel": 23, "rms_norm_long_kernel": 51, "rms_norm_backward_long_kernel": 19, "narrow_linear_kernel": 62,
+           "narrow_linear_backward_kernel": 132}
+NONE = ["few_rows_kernel", "few_rows_8bit_kernel", "linear_join_kernel", "join_kernel", "join_deep_kernel", "linear_slope_kernel", "quantise_kernel", "dequantise_kernel",
+        "column_sums_kernel", "product_8bit_kernel", "tile_kernel", "float_tile_kernel", "rms_norm_long_params_kernel", "lay_out_kernel"]
+
+
+@pytest.mark.parametrize("kernel", [*SCALARS, *NONE])
+def test_nothing_is_spilled_to_memory(objects, kernel):  # noqa: F811
+    found = {name: note for name, note in notes(objects).items() if re.search(rf"\d{kernel}I", name)}
+    assert len(found) >= 2
+    for name, note in found.items():
+        assert note["vgpr_spill_count"] == 0 and note["private_segment_fixed_size"] == 0, name
+        whole = re.search(r"Li(32|64|128)ELi(32|64|128)ELb[01]ELb1E", name) if "narrow" in kernel else None
+        assert note["sgpr_spill_count"] <= (0 if whole else SCALARS.get(kernel, 0)), name
