@@ -202,7 +202,11 @@ def linear(x, weight, bias=None, activation=None, residual=None, keep_8bit=False
     ``weight`` is out_width x width in the type of ``x``; ``bias`` has one axis of out_width, in the type of ``x`` or float32;
     ``residual`` has the shape and type of the result.  ``keep_8bit``: what the backward pass needs of the activations is kept in 8 bits,
     ``x`` as whole numbers with a scale for every 32 columns and the activation's derivative in steps of 1/112.  The result is the same; the
-    weight's gradient is that of the ``x`` kept, and those of ``x``, weight and bias are made with the derivative kept."""
+    weight's gradient is that of the ``x`` kept, and those of ``x``, weight and bias are made with the derivative kept.
+
+    Without it ``x`` is kept, and of silu and gelu ``x weight^T + bias`` in the type of ``bias`` (of ``x`` if there is none): a float32 bias of
+    16-bit matrices has an exact gradient for twice the memory.  With it the backward pass of 16-bit matrices wider than 128 lays the ``x`` kept
+    out in their type while it runs."""
     act = _epilogue(activation)
     y = (_native or native()).linear(x, weight, bias, act, residual, bool(keep_8bit))
     return _functions().linear.apply(x, weight, bias, act, residual, bool(keep_8bit)) if y is None else y

@@ -491,3 +491,22 @@ def test_few_rows_of_many_columns_and_deep_sums(rows, width, out):
     check(inputs(rows, width, out, torch.bfloat16, torch.float32, 500), "gelu", at="cuda")
     x, w, b, r, dy = inputs(rows, width, out, torch.float16, torch.float16, 510)
     check((x, w, None, None, dy), None, keep=True, at="cuda")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("width,out", [(512, 256), (64, 64)])
+def test_what_a_float_bias_keeps(width, out):
+    """z in the bias's type, as its gradient is; kept in 8 bits, nothing more than with a bias of 16 bits."""
+    print("[case] memory, float bias", width, out, flush=True)
+    rows, dtype = 4096, torch.bfloat16
+    w = torch.randn((out, width), device="cuda").to(dtype).requires_grad_(True)
+    for params, of_z in ((dtype, 2), (torch.float32, 4)):
+        b = torch.randn(out, device="cuda").to(params).requires_grad_(True)
+        for keep in (False, True):
+            x = torch.randn((rows, width), device="cuda").to(dtype).requires_grad_(True)
+            before = torch.cuda.memory_allocated()
+            y = layers.linear(x * 1.0, w, b, "gelu", keep_8bit=keep)
+            used = torch.cuda.memory_allocated() - before - y.numel() * y.element_size()
+            assert used == (rows * (width + out) + rows * 4 * -(-width // 128) if keep else rows * (2 * width + of_z * out)), (params, keep)
+            assert torch.autograd.grad(y.sum(), b)[0].dtype == params
+            del x, y
