@@ -129,7 +129,7 @@ int64_t dgsp_gated_ff_backward_workspace_bytes(int64_t rows, int64_t width, int6
 /*
  * Root-mean-square norm over the rows of s, where s = x, or s = residual + dropout(x) if residual is not NULL:
  *     y = s / sqrt(mean(s^2) + eps) * weight
- * Any finite s has its norm: squares that 32 bits cannot hold are summed in 64.
+ * Squares that 32 bits cannot hold are summed in 64, so that any finite s has its norm; rstd itself passes their range where mean(s^2) + eps is below 2^-256.
  *   rstd   a float a row, 1 / sqrt(mean(s^2) + eps), for the backward pass; NULL: not wanted
  * The other arguments and the limits are those of dgsp_layer_norm.
  */
@@ -190,7 +190,8 @@ typedef enum { DGSP_KEEP_NOTHING = 0, DGSP_KEEP_WHOLE = 1, DGSP_KEEP_8BIT = 2 } 
  *   activation  DGSP_ACT_...
  *   saved       dgsp_linear_saved_bytes(...) bytes, 16-byte aligned, for the backward pass; not looked at if that is 0
  *   x_values, x_scales   x in DGSP_INT8 for the backward pass, only with DGSP_KEEP_8BIT; NULL: not wanted
- *   workspace   dgsp_linear_workspace_bytes(...) bytes, 16-byte aligned; not looked at if that is 0
+ *   workspace   dgsp_linear_workspace_bytes(...) bytes, 16-byte aligned; not looked at if that is 0.  Sizes are for operands that lie anywhere: of 16-bit types
+ *               there is room for a copy of each, used where rows are no whole 16-byte pieces
  * z, act(z) and the sum with the residual are held in 32 bits.  Float matrices, infinities, NaN and limits: as in dgsp_gated_ff.
  */
 int dgsp_linear(int64_t rows, int64_t width, int64_t out_width, int type, int bias_type, int activation, int keep, const void *x,

@@ -1,12 +1,12 @@
 // y = act(x w^T + bias) + residual on matrix_tiles.hpp: what becomes of the product of a tile, and what the backward pass makes of dy first.
 //
 // The epilogue adds the bias to the sum in 32 bits, applies the activation, adds the residual and rounds once.  For the backward pass it
-// leaves what the activation's derivative is made of: z in the bias's type (where that is 16 bits its rounding moves act'(z) by |z act''(z)| half
-// a step, a fifth of what rounding dz itself costs; a float bias's gradient is not rounded, and would lose by it), or act'(z) in steps of 1/112 in 8 bits, which has 0 and 1 exactly: all of relu's, and what gelu
-// (-0.13 ... 1.13) and silu (-0.10 ... 1.10) come to far from 0.
+// leaves what the activation's derivative is made of: z in the bias's type, or act'(z) in steps of 1/112 in 8 bits, which has 0 and 1 exactly: all of relu's, and what
+// gelu (-0.13 ... 1.13) and silu (-0.10 ... 1.10) come to far from 0.  Where z is kept in 16 bits its rounding moves act'(z) by |z act''(z)| half a step, about a third of
+// what rounding dz itself costs (z of deviation 0.5 to 2: 0.27 to 0.38 of it); a float bias's gradient is not rounded, and would lose by it.
 //
-// What it costs beside the product, bfloat16, 8192 x 4096 -> 16384, gelu, z kept: 1050 to 1090 us against 900 of the product alone, of which
-// 110 is writing y and z; nothing runs beside it, as a tile of 256 takes a CU.  dz, from dy and z: 200 us, 4.0 TB/s.
+// What it costs beside the product, bfloat16, 8192 x 4096 -> 16384, gelu, z kept: 1010 to 1100 us against 900 of the product alone, of which
+// 110 is writing y and z (960 without z); nothing runs beside it, as a tile of 256 takes a CU.  dz, from dy and z: 200 us, 4.0 TB/s.
 #pragma once
 
 #include "product_kernels.hpp"

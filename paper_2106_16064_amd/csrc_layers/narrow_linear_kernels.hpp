@@ -2,10 +2,10 @@
 // reading and writing the matrices that are as long as the rows, so each is touched once: the forward pass writes y and what is kept, x in 8 bits
 // among it, and the backward pass makes dz = dy act'(z) in registers and all three gradients of it.
 //
-// 2^20 vertices, bfloat16, with residual: 64 -> 64 forward 105 us (537 MB, 5.1 TB/s), gradient 127 us (537 MB, 4.2 TB/s); 128 -> 128 with
-// activations kept in 8 bits 250 us (1.08 GB, 4.3 TB/s; gelu and what becomes 8 bits are 150 us of vector instructions beside that) and
-// 215 to 250 us (0.81 GB).  The products of matrix_tiles.hpp one after the other: 183 and 270 us, 417 and 560 us.  Float, gelu, 32 -> 32 forward 88 us
-// (403 MB, 4.6 TB/s), gradient 125 us (537 MB, 4.3 TB/s), by tiles of 64 167 and 325 us; 64 -> 128 with residual 400 and 550 to 570 us,
+// 2^20 vertices, bfloat16, with residual: 64 -> 64 forward 105 us (537 MB, 5.1 TB/s), gradient 128 us (537 MB, 4.2 TB/s); 128 -> 128 with
+// activations kept in 8 bits 250 to 265 us (1.08 GB, 4.1 to 4.3 TB/s; gelu and what becomes 8 bits are 150 us of vector instructions beside that) and
+// 220 to 270 us (0.81 GB).  The products of matrix_tiles.hpp one after the other: 183 and 270 us, 417 and 560 us.  Float, gelu, 32 -> 32 forward 92 us
+// (403 MB, 4.4 TB/s), gradient 116 us (537 MB, 4.6 TB/s), by tiles of 64 167 and 325 us; 64 -> 64 166 and 224 us; 64 -> 128 with residual 371 and 467 us,
 // by tiles 428 and 762.
 //
 // A lane has a vertex (l % 16 of 16) and, q = l / 16, columns 32 t + 8 q ... + 7 of every 32: a piece of 16 bytes, which is also what the matrix

@@ -5,7 +5,7 @@
 // is what the matrix instructions read; whole numbers are nearer to what they stand for (an error of at most amax / 127 against
 // 2^-4 of the element), and are what activations are kept in.
 //
-// Memory bounds both ways (bfloat16, 8192 x 4096: to whole numbers 19 us, 5.3 TB/s, to e4m3 22 us, 4.6, back 17 us, 5.9).
+// Memory bounds both ways (bfloat16, 8192 x 4096: to whole numbers 18.5 us, 5.5 TB/s, to e4m3 20.5 us, 4.9, back 17 us, 5.9).
 //
 // Values: rows of whole blocks, the last one filled up with zeros.  Scales: bytes b for 2^(b - 127); block k of row r at
 // ((k / 4) * ld + r) * 4 + k % 4, so that what a product's stage of 128 columns reads lies together.  Places of a group of four

@@ -2,7 +2,7 @@
 // scales with the elements, 128 columns at a time.
 //
 // What bounds it: the matrix instructions, at the clock that the card holds under them; reading the fragments from LDS takes as long.  8192 x 8192 x 8192
-// 432 us, 2.5 PFLOP/s, 8192 x 4096 x 16384 495 us, 2.2 (a library's: 2.7 and 2.5); of a few rows the weights' way from memory.
+// 455 us, 2.4 PFLOP/s, 8192 x 4096 x 16384 530 to 560 us by the card's power, 2.0 to 2.1 (a library's: 2.7 and 2.5); of a few rows the weights' way from memory.
 //
 // As in matrix_tiles.hpp, whose loaders move a stage of 128 bytes a row: here 128 columns, with four scales a row, which go to LDS beside it.
 // Lane l of a fragment has row l % 16, of the 16-byte chunks of its stage those numbered l / 16 and l / 16 + 4, exchanged by the row as the loader
@@ -138,7 +138,7 @@ struct Tile8Product {
                             *(Byte)(uintptr_t)(at.scale + i * 64)};
         };
         // Fragments of B stay for a stage and have a second place for the next one's; the two change roles from stage to stage (moving them
-        // instead took a tenth of the time: 8192 x 4096 x 16384 590 us against 495).  Those of A come kAhead rows before they are multiplied; when
+        // instead took a fifth more time).  Those of A come kAhead rows before they are multiplied; when
         // the last ones of a stage are there all waves meet, and from then on fragments are read of the next stage, which has arrived, while
         // the last rows are multiplied, and the buffer takes the stage after that.
         constexpr int kAhead = 2, kRows = Shape::kFragsM, kPieces = (kOfAStage + kAhead - 1) / kAhead;
